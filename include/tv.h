@@ -76,7 +76,8 @@ typedef enum tv_status {
 
 typedef enum tv_dtype {
   TV_DTYPE_BF16 = 0,       /* bfloat16 logits (uint16 bit patterns) */
-  TV_DTYPE_F32 = 1         /* float32 logits */
+  TV_DTYPE_F32 = 1,        /* float32 logits */
+  TV_DTYPE_F16 = 2         /* IEEE half, queries, keys and values of tv_tree_attention */
 } tv_dtype_t;
 
 /*
@@ -130,6 +131,13 @@ enum {
 #define TV_NUM_COUNTERS 4
 #define TV_MAX_LMHEAD_ROWS (1 << 18)    /* rows of one tv_lmhead_stats call */
 #define TV_MAX_HIDDEN (1 << 16)         /* hidden size of tv_lmhead_stats */
+#define TV_MAX_HEAD_DIM 128             /* head size of tv_tree_attention */
+#define TV_MIN_PAGE 16                  /* tokens of a cache page, a power of two */
+#define TV_MAX_PAGE 1024
+#define TV_MAX_HISTORY (1 << 24)        /* tokens of one request's history */
+#define TV_MAX_BIAS (1 << 16)           /* biased tokens of one request */
+#define TV_MAX_NEW (1 << 20)            /* positions appended to one request by one call */
+#define TV_MAX_LAYERS 4096              /* layers of one tv_cache_commit call */
 
 /*
  * Bytes of device workspace tv_verify / tv_verify_tokenlevel need for these
@@ -336,6 +344,182 @@ int tv_commit_paths(int32_t batch, int32_t num_nodes, const int32_t* parents,
                     const int32_t* tokens, const int32_t* accepted_node,
                     const int32_t* bonus_token, const int32_t* status, int32_t max_len,
                     int32_t* path_nodes, int32_t* path_tokens, int32_t* path_len,
+                    hipStream_t stream);
+
+/*
+ * The target model's pass over the trees, and the cache behind it. A request
+ * holds the tokens of its committed sequence in a paged cache: page p of one
+ * layer is [kv_heads][page_size][head_dim] at p * page_stride, and position x
+ * of request b is row x % page_size of page block_table[b][x / page_size].
+ * ctx_len counts the positions in the cache: all committed tokens but the last,
+ * which is the tree's root. The keys and values of the tree's nodes (the root
+ * among them) stay outside until they are accepted: tv_tree_attention reads
+ * them where the projection wrote them, tv_cache_extend grows every request by
+ * the length tv_commit_paths gave, and tv_cache_commit writes the root and the
+ * accepted nodes into the cache, so a rejected node never touches it.
+ */
+
+/*
+ * Attention of all nodes of a batch of trees (Def. de_tree, Sec. 3.3: the
+ * target's distribution at node i is the one after the path root..i). With
+ * query head h reading key head h / (heads / kv_heads),
+ *   s(i, x) = scale * <q[b][i][h], key x>
+ *   out[b][i][h] = sum_x exp(s(i, x)) value x / sum_x exp(s(i, x))
+ * over the cached positions 0 .. ctx_len[b] - 1, node i's ancestors and node i
+ * itself. num_nodes = 1 is decoding of single tokens.
+ *
+ * Inputs (device): parents int32 [batch][num_nodes] as for tv_verify (a link
+ * that does not point back ends the path there; NULL if num_nodes is 1);
+ * q [batch][num_nodes][heads][head_dim] and k_new, v_new
+ * [batch][num_nodes][kv_heads][head_dim] of type dtype (TV_DTYPE_BF16 or
+ * TV_DTYPE_F16), consecutive nodes q_stride and kv_stride elements apart (so
+ * that all three may lie in one projection's output); k_cache, v_cache of the
+ * same type, num_pages pages page_stride elements apart; block_table int32
+ * [batch][table_width]; ctx_len int32 [batch], negative for a tree that takes
+ * no part: its outputs are left as they were. Sums are formed in fp32 from
+ * products on the matrix cores; weights are rounded to dtype before they
+ * multiply values.
+ *
+ * A common prefix: the first prefix_len positions (a multiple of page_size, 0
+ * for none) lie on the same pages for every tree with ctx_len >= prefix_len.
+ * They are read once for the batch, from prefix_pages int32
+ * [prefix_len / page_size] (any such tree's row of the block table will do),
+ * and those trees' own entries for them are not read. A tree with a shorter
+ * context is computed from its own entries alone.
+ *
+ * A tree whose block table names a page outside [0, num_pages) for a position
+ * below ctx_len, or whose ctx_len exceeds table_width * page_size, gets NaN in
+ * every output.
+ *
+ * head_dim: a multiple of 8 up to TV_MAX_HEAD_DIM; heads a multiple of
+ * kv_heads; heads * head_dim at most TV_MAX_HIDDEN; page_size a power of two
+ * from TV_MIN_PAGE to TV_MAX_PAGE; scale positive and finite; q, k_new, v_new,
+ * caches and out 16-byte aligned, strides multiples of 8; the nodes of a tree,
+ * and a page, at most 2^30 bytes. out dtype [batch][num_nodes][heads][head_dim].
+ * workspace: tv_tree_attention_workspace_size() bytes (0 for invalid sizes),
+ * 256-byte aligned. Nothing is allocated. Returns a tv_status_t; argument errors
+ * launch nothing.
+ */
+size_t tv_tree_attention_workspace_size(int32_t batch, int32_t num_nodes, int32_t heads,
+                                        int32_t kv_heads, int32_t head_dim, int32_t prefix_len);
+int tv_tree_attention(int32_t batch, int32_t num_nodes, int32_t heads, int32_t kv_heads,
+                      int32_t head_dim, int32_t dtype, const int32_t* parents, const void* q,
+                      int64_t q_stride, const void* k_new, const void* v_new, int64_t kv_stride,
+                      const void* k_cache, const void* v_cache, int64_t page_stride,
+                      int32_t num_pages, int32_t page_size, const int32_t* block_table,
+                      int32_t table_width, const int32_t* ctx_len, const int32_t* prefix_pages,
+                      int32_t prefix_len, float scale, void* out, void* workspace,
+                      size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Penalties, biases and masks on the logits of tree nodes, between the LM head
+ * and tv_verify_stats, with the row statistics of the result (those of
+ * tv_lmhead_stats no longer hold once logits change). The text before node i's
+ * next token is the request's history (prompt and generated tokens, the tree's
+ * root the last of them) and the drafted tokens on the path to node i. For token
+ * t, with n its number of occurrences among the generated and the drafted ones
+ * and seen = n > 0 or t in the prompt,
+ *   z1 = seen ? (z > 0 ? z / repetition[b] : z * repetition[b]) : z
+ *   z2 = z1 - (presence[b] * (n > 0) + frequency[b] * n - bias_b(t))
+ *   out = z2 where the node's mask allows t, else -inf
+ * in fp32, rounded to dtype, and as in tv_lmhead_stats
+ *   row_max = max_t out,  row_sum = sum_t exp((out - row_max) / temperature).
+ *
+ * logits, out: dtype (TV_DTYPE_BF16 or TV_DTYPE_F32) [batch][num_nodes][vocab],
+ * the same buffer or apart; only the rows of nodes first_node ..
+ * first_node + num_rows - 1 of every tree are read and written (a level of a
+ * tree that is still being drafted, say), in row_max float and row_sum double
+ * [batch][num_nodes] as well (both NULL: no statistics). parents, tokens int32
+ * [batch][num_nodes] as for tv_verify (links that do not point back end a path;
+ * both NULL: the paths count nothing). history int32 [batch][max_history], of
+ * which history_len[b] tokens are there and the first prompt_len[b] are the
+ * prompt (prompt_len NULL: no prompt; history NULL: none at all). repetition,
+ * presence, frequency float [batch], each NULL for no such penalty; repetition
+ * positive and finite, the others finite. bias_tokens int32, bias_values float
+ * [batch][max_bias] (NULL: none); of several entries for a token the last
+ * counts. masks uint32 [num_masks][(vocab + 31) / 32], bit t % 32 of word t / 32
+ * set where t is allowed; mask_index int32 [batch][num_nodes] the mask of each
+ * node, negative for none (NULL: no masks); num_masks or more allows nothing.
+ * Tokens outside [0, vocab) in tokens, history and bias_tokens are passed over;
+ * lengths outside [0, max_history] count as the nearer end.
+ * workspace: tv_process_logits_workspace_size() bytes (0 for invalid sizes),
+ * 256-byte aligned, not needed without statistics. Nothing is allocated. Returns
+ * a tv_status_t; argument errors launch nothing.
+ */
+size_t tv_process_logits_workspace_size(int32_t batch, int32_t num_nodes, int32_t vocab);
+int tv_process_logits(int32_t batch, int32_t num_nodes, int32_t vocab, int32_t first_node,
+                      int32_t num_rows, const void* logits, int32_t dtype, float temperature,
+                      const int32_t* parents, const int32_t* tokens, const int32_t* history,
+                      int32_t max_history, const int32_t* history_len, const int32_t* prompt_len,
+                      const float* repetition, const float* presence, const float* frequency,
+                      const int32_t* bias_tokens, const float* bias_values, int32_t max_bias,
+                      const uint32_t* masks, int32_t num_masks, const int32_t* mask_index,
+                      void* out, float* row_max, double* row_sum, void* workspace,
+                      size_t workspace_bytes, hipStream_t stream);
+
+/* new_len value of tv_cache_extend: the request ends and gives its pages back */
+#define TV_CACHE_RELEASE INT32_MIN
+
+/* Per-request status of tv_cache_extend. A request whose status is not
+   TV_CACHE_OK is left as it was (its slots are -1). */
+enum {
+  TV_CACHE_OK = 0,
+  TV_CACHE_FULL = 1,       /* the free pages do not suffice */
+  TV_CACHE_OVERFLOW = 2,   /* new_len > max_new, or the block table's row is too short */
+  TV_CACHE_BAD_LENGTH = 3  /* seq_len negative or beyond the block table's row */
+};
+
+/*
+ * Growth of the requests by the tokens of a decoding cycle, with the pages they
+ * need. new_len int32 [batch] is the number of positions to append, as
+ * tv_commit_paths writes path_len (0 and its negative codes append nothing), or
+ * TV_CACHE_RELEASE. Request b holds the pages of its seq_len[b] positions.
+ * free_pages int32 [num_pages] is a stack of free_count[0] pages. In order of b,
+ * first every request that ends pushes its pages (in table order, but those of
+ * the first prefix_len positions if seq_len >= prefix_len: these are shared and
+ * not its own), then every other request pops what it lacks from the top; once
+ * the pages do not suffice for a request, every later one that needs any fails
+ * too (TV_CACHE_FULL).
+ * Outputs: the new entries of block_table int32 [batch][table_width] (a row's
+ * own entries are set to -1 on release); slots int32 [batch][max_new], page *
+ * page_size + row of every appended position, then -1; new_seq_len int32 [batch]
+ * and new_free_count int32 [1], which may be seq_len and free_count themselves;
+ * status int32 [batch]. Pages pushed past num_pages are dropped, and a
+ * free_count outside [0, num_pages] counts as the nearer end. page_size a power
+ * of two from TV_MIN_PAGE to TV_MAX_PAGE, prefix_len a multiple of it; num_pages *
+ * page_size and table_width * page_size at most 2^31 - 1; slots may be NULL if
+ * max_new is 0. No workspace; nothing is allocated. Returns a tv_status_t;
+ * argument errors launch nothing.
+ */
+int tv_cache_extend(int32_t batch, const int32_t* new_len, int32_t max_new,
+                    const int32_t* seq_len, int32_t* new_seq_len, int32_t* block_table,
+                    int32_t table_width, int32_t page_size, int32_t prefix_len,
+                    int32_t* free_pages, int32_t num_pages, const int32_t* free_count,
+                    int32_t* new_free_count, int32_t* slots, int32_t* status,
+                    hipStream_t stream);
+
+/*
+ * Writes the keys and values of committed nodes into the cache, all layers at
+ * once: for k < min(new_len[b], max_new) with slots[b][k] = s >= 0, node
+ * (k == 0 ? 0 : path_nodes[b][k - 1]) of tree b into row s % page_size of page
+ * s / page_size. path_nodes int32 [batch][path_width] as tv_commit_paths wrote
+ * it, or NULL for node k itself (prompts). Nodes outside [0, num_nodes) and slots
+ * outside the cache are passed over. The slots of a call must differ (those of
+ * tv_cache_extend do).
+ * Any element type: sizes and strides are in bytes. k_new, v_new: layers
+ * new_layer_stride apart, nodes node_stride apart (trees num_nodes *
+ * node_stride), each node [kv_heads][head_bytes]. k_cache, v_cache: layers
+ * cache_layer_stride apart, pages page_stride, each [kv_heads][page_size]
+ * [head_bytes]. head_bytes a multiple of 16 up to 4096; strides multiples of
+ * 16, pointers 16-byte aligned. No workspace; nothing is allocated. Returns a
+ * tv_status_t; argument errors launch nothing.
+ */
+int tv_cache_commit(int32_t layers, int32_t batch, int32_t num_nodes, int32_t kv_heads,
+                    int32_t head_bytes, const void* k_new, const void* v_new,
+                    int64_t new_layer_stride, int64_t node_stride, void* k_cache, void* v_cache,
+                    int64_t cache_layer_stride, int64_t page_stride, int32_t num_pages,
+                    int32_t page_size, const int32_t* new_len, int32_t max_new,
+                    const int32_t* slots, const int32_t* path_nodes, int32_t path_width,
                     hipStream_t stream);
 
 /* Static, human-readable name of a tv_status_t value ("unknown status" otherwise). */

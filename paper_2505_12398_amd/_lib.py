@@ -9,7 +9,7 @@ from dataclasses import dataclass
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtv.so")
 
 TV_OK, TV_ERR_INVALID_ARG, TV_ERR_UNSUPPORTED, TV_ERR_WORKSPACE, TV_ERR_HIP = range(5)
-TV_DTYPE_BF16, TV_DTYPE_F32 = 0, 1
+TV_DTYPE_BF16, TV_DTYPE_F32, TV_DTYPE_F16 = 0, 1, 2
 TV_SIBLINGS_WITHOUT_REPLACEMENT, TV_SIBLINGS_WITH_REPLACEMENT = 0, 1
 (TV_TREE_OK, TV_TREE_BAD_PARENT, TV_TREE_BAD_TOKEN, TV_TREE_DUP_SIBLING, TV_TREE_NONFINITE,
  TV_TREE_DEGENERATE, TV_TREE_ABORTED) = range(7)
@@ -21,6 +21,14 @@ TV_MAX_VOCAB_F32 = 1 << 19
 TV_NUM_COUNTERS = 4
 TV_MAX_LMHEAD_ROWS = 1 << 18
 TV_MAX_HIDDEN = 1 << 16
+TV_MAX_HEAD_DIM = 128
+TV_MIN_PAGE, TV_MAX_PAGE = 16, 1024
+TV_MAX_HISTORY = 1 << 24
+TV_MAX_BIAS = 1 << 16
+TV_MAX_NEW = 1 << 20
+TV_MAX_LAYERS = 4096
+TV_CACHE_RELEASE = -(1 << 31)
+TV_CACHE_OK, TV_CACHE_FULL, TV_CACHE_OVERFLOW, TV_CACHE_BAD_LENGTH = range(4)
 
 
 class TvError(RuntimeError):
@@ -79,6 +87,25 @@ def load_library(path: str = LIB_PATH):
         lib.tv_commit_paths.argtypes = [ctypes.c_int32, ctypes.c_int32] + \
             [ctypes.c_void_p] * 5 + [ctypes.c_int32] + [ctypes.c_void_p] * 4
         lib.tv_commit_paths.restype = ctypes.c_int
+        i32, i64, ptr, size = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t
+        lib.tv_tree_attention_workspace_size.argtypes = [i32] * 6
+        lib.tv_tree_attention_workspace_size.restype = size
+        lib.tv_tree_attention.argtypes = (
+            [i32] * 6 + [ptr, ptr, i64, ptr, ptr, i64, ptr, ptr, i64, i32, i32, ptr, i32, ptr, ptr,
+                         i32, ctypes.c_float, ptr, ptr, size, ptr])
+        lib.tv_tree_attention.restype = ctypes.c_int
+        lib.tv_process_logits_workspace_size.argtypes = [i32] * 3
+        lib.tv_process_logits_workspace_size.restype = size
+        lib.tv_process_logits.argtypes = (
+            [i32] * 5 + [ptr, i32, ctypes.c_float, ptr, ptr, ptr, i32] + [ptr] * 7 +
+            [i32, ptr, i32] + [ptr] * 5 + [size, ptr])
+        lib.tv_process_logits.restype = ctypes.c_int
+        lib.tv_cache_extend.argtypes = [i32, ptr, i32, ptr, ptr, ptr, i32, i32, i32, ptr, i32] + \
+            [ptr] * 5
+        lib.tv_cache_extend.restype = ctypes.c_int
+        lib.tv_cache_commit.argtypes = ([i32] * 5 + [ptr, ptr, i64, i64, ptr, ptr, i64, i64, i32,
+                                                     i32, ptr, i32, ptr, ptr, i32, ptr])
+        lib.tv_cache_commit.restype = ctypes.c_int
         lib.tv_status_string.argtypes = [ctypes.c_int]
         lib.tv_status_string.restype = ctypes.c_char_p
         _lib = lib
@@ -281,6 +308,309 @@ def commit_paths(parents, tokens, out: "VerifyOutputs", max_len: int, stream=Non
     if st != TV_OK:
         raise TvError(st, "tv_commit_paths")
     return pn[:, :max_len], pt, pl
+
+
+def tv_tree_attention_workspace_size(batch, num_nodes, heads, kv_heads, head_dim,
+                                     prefix_len=0) -> int:
+    return int(load_library().tv_tree_attention_workspace_size(
+        batch, num_nodes, heads, kv_heads, head_dim, prefix_len))
+
+
+def tv_tree_attention(batch, num_nodes, heads, kv_heads, head_dim, dtype, parents, q, q_stride,
+                      k_new, v_new, kv_stride, k_cache, v_cache, page_stride, num_pages, page_size,
+                      block_table, table_width, ctx_len, prefix_pages, prefix_len, scale, out,
+                      workspace, workspace_bytes, stream=None) -> int:
+    """C-ABI ``tv_tree_attention``: pointers may be torch tensors or raw ints;
+    returns the status."""
+    return int(load_library().tv_tree_attention(
+        int(batch), int(num_nodes), int(heads), int(kv_heads), int(head_dim), int(dtype),
+        _ptr(parents), _ptr(q), int(q_stride), _ptr(k_new), _ptr(v_new), int(kv_stride),
+        _ptr(k_cache), _ptr(v_cache), int(page_stride), int(num_pages), int(page_size),
+        _ptr(block_table), int(table_width), _ptr(ctx_len), _ptr(prefix_pages), int(prefix_len),
+        float(scale), _ptr(out), _ptr(workspace), int(workspace_bytes), _ptr(stream)))
+
+
+def tv_process_logits_workspace_size(batch, num_nodes, vocab) -> int:
+    return int(load_library().tv_process_logits_workspace_size(batch, num_nodes, vocab))
+
+
+def tv_process_logits(batch, num_nodes, vocab, first_node, num_rows, logits, dtype, temperature,
+                      parents, tokens, history, max_history, history_len, prompt_len, repetition,
+                      presence, frequency, bias_tokens, bias_values, max_bias, masks, num_masks,
+                      mask_index, out, row_max, row_sum, workspace, workspace_bytes,
+                      stream=None) -> int:
+    """C-ABI ``tv_process_logits``: pointers may be torch tensors or raw ints;
+    returns the status."""
+    return int(load_library().tv_process_logits(
+        int(batch), int(num_nodes), int(vocab), int(first_node), int(num_rows), _ptr(logits),
+        int(dtype), float(temperature), _ptr(parents), _ptr(tokens), _ptr(history),
+        int(max_history), _ptr(history_len), _ptr(prompt_len), _ptr(repetition), _ptr(presence),
+        _ptr(frequency), _ptr(bias_tokens), _ptr(bias_values), int(max_bias), _ptr(masks),
+        int(num_masks), _ptr(mask_index), _ptr(out), _ptr(row_max), _ptr(row_sum),
+        _ptr(workspace), int(workspace_bytes), _ptr(stream)))
+
+
+def tv_cache_extend(batch, new_len, max_new, seq_len, new_seq_len, block_table, table_width,
+                    page_size, prefix_len, free_pages, num_pages, free_count, new_free_count,
+                    slots, status, stream=None) -> int:
+    """C-ABI ``tv_cache_extend``: pointers may be torch tensors or raw ints;
+    returns the status."""
+    return int(load_library().tv_cache_extend(
+        int(batch), _ptr(new_len), int(max_new), _ptr(seq_len), _ptr(new_seq_len),
+        _ptr(block_table), int(table_width), int(page_size), int(prefix_len), _ptr(free_pages),
+        int(num_pages), _ptr(free_count), _ptr(new_free_count), _ptr(slots), _ptr(status),
+        _ptr(stream)))
+
+
+def tv_cache_commit(layers, batch, num_nodes, kv_heads, head_bytes, k_new, v_new,
+                    new_layer_stride, node_stride, k_cache, v_cache, cache_layer_stride,
+                    page_stride, num_pages, page_size, new_len, max_new, slots, path_nodes,
+                    path_width, stream=None) -> int:
+    """C-ABI ``tv_cache_commit`` (sizes and strides in bytes): pointers may be
+    torch tensors or raw ints; returns the status."""
+    return int(load_library().tv_cache_commit(
+        int(layers), int(batch), int(num_nodes), int(kv_heads), int(head_bytes), _ptr(k_new),
+        _ptr(v_new), int(new_layer_stride), int(node_stride), _ptr(k_cache), _ptr(v_cache),
+        int(cache_layer_stride), int(page_stride), int(num_pages), int(page_size), _ptr(new_len),
+        int(max_new), _ptr(slots), _ptr(path_nodes), int(path_width), _ptr(stream)))
+
+
+def _check(dev, **tensors):
+    """Each (tensor, shape, dtype) contiguous on ``dev`` with that shape and type (None passes)."""
+    for name, (t, shape, dtype) in tensors.items():
+        if t is None:
+            continue
+        if t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+        if t.device != dev or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous on {dev}")
+
+
+def _on(dev):
+    """The device as the current one while a call is enqueued on it."""
+    import contextlib
+
+    import torch
+    return torch.cuda.device(dev) if dev.type == "cuda" else contextlib.nullcontext()
+
+
+def _stream_of(dev, stream):
+    import torch
+    if stream is None and dev.type == "cuda":
+        return torch.cuda.current_stream(dev).cuda_stream
+    return stream
+
+
+def _workspace(need, workspace, dev):
+    import torch
+    if workspace is None:
+        return torch.empty(max(need, 1), dtype=torch.uint8, device=dev), need
+    if workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous on {dev}")
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def _rows(name, t, dev, dtype):
+    """Stride between the nodes of a [B, N+1, heads, head_dim] tensor whose nodes follow each
+    other evenly, each node's heads together (a slice of a projection's output)."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    B, n1, H, D = t.shape
+    stride = t.stride(1) if n1 > 1 else t.stride(0) if B > 1 else H * D
+    if t.device != dev or t.stride(3) != 1 and D > 1 or t.stride(2) != D and H > 1 or \
+            t.stride(0) != n1 * stride and B > 1:
+        raise ValueError(f"{name}: nodes must lie evenly spaced on {dev}, their heads contiguous")
+    return stride
+
+
+def _pages(name, t, dev, dtype):
+    """Stride between the pages of a [pages, kv_heads, page_size, head_dim] cache."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    P, KH, ps, D = t.shape
+    if t.device != dev or (t.stride(3) != 1 and D > 1) or t.stride(2) != D or \
+            (t.stride(1) != ps * D and KH > 1):
+        raise ValueError(f"{name}: pages must be contiguous on {dev}")
+    return t.stride(0) if P > 1 else KH * ps * D
+
+
+def tree_attention(q, k_new, v_new, parents, k_cache, v_cache, block_table, ctx_len, scale,
+                   prefix_len=0, prefix_pages=None, out=None, stream=None, workspace=None):
+    """Attention of all tree nodes over the paged cache and their ancestors
+    (``tv_tree_attention``): q [B, N+1, heads, D], k_new and v_new
+    [B, N+1, kv_heads, D] (bfloat16 or float16; views of one projection's output
+    will do), k_cache and v_cache [pages, kv_heads, page_size, D], block_table
+    [B, width] and ctx_len [B] int32. ``prefix_pages`` [prefix_len / page_size]
+    int32 are the pages of the common prefix (default: those of tree 0). Returns
+    out [B, N+1, heads, D]; raises on a non-OK return."""
+    import torch
+    if q.dim() != 4 or k_new.dim() != 4 or k_cache.dim() != 4:
+        raise ValueError("q, k_new, v_new and the caches have four dimensions")
+    B, n1, H, D = q.shape
+    KH, ps = k_cache.shape[1], k_cache.shape[2]
+    dev = q.device
+    if q.dtype not in (torch.bfloat16, torch.float16):
+        raise TypeError(f"q must be bfloat16 or float16, got {q.dtype}")
+    for name, t, shape in (("k_new", k_new, (B, n1, KH, D)), ("v_new", v_new, (B, n1, KH, D)),
+                           ("k_cache", k_cache, (k_cache.shape[0], KH, ps, D)),
+                           ("v_cache", v_cache, tuple(k_cache.shape))):
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    q_stride = _rows("q", q, dev, q.dtype)
+    kv_stride = _rows("k_new", k_new, dev, q.dtype)
+    if _rows("v_new", v_new, dev, q.dtype) != kv_stride:
+        raise ValueError("k_new and v_new must have the same strides")
+    page_stride = _pages("k_cache", k_cache, dev, q.dtype)
+    if _pages("v_cache", v_cache, dev, q.dtype) != page_stride:
+        raise ValueError("k_cache and v_cache must have the same strides")
+    if prefix_len and prefix_pages is None:
+        prefix_pages = block_table[0, :prefix_len // ps]
+    if out is None:
+        out = torch.empty((B, n1, H, D), dtype=q.dtype, device=dev)
+    _check(dev, parents=(parents, (B, n1), torch.int32),
+           block_table=(block_table, (B, block_table.shape[-1]), torch.int32),
+           ctx_len=(ctx_len, (B,), torch.int32), out=(out, (B, n1, H, D), q.dtype),
+           prefix_pages=(prefix_pages, (prefix_len // ps,), torch.int32))
+    with _on(dev):
+        need = tv_tree_attention_workspace_size(B, n1, H, KH, D, prefix_len)
+        workspace, nbytes = _workspace(need, workspace, dev)
+        st = tv_tree_attention(
+            B, n1, H, KH, D, TV_DTYPE_BF16 if q.dtype == torch.bfloat16 else TV_DTYPE_F16, parents,
+            q, q_stride, k_new, v_new, kv_stride, k_cache, v_cache, page_stride,
+            k_cache.shape[0], ps, block_table, block_table.shape[1], ctx_len, prefix_pages,
+            prefix_len, scale, out, workspace, nbytes, _stream_of(dev, stream))
+    if st != TV_OK:
+        raise TvError(st, "tv_tree_attention")
+    return out
+
+
+def process_logits(logits, temperature, parents=None, tokens=None, history=None, history_len=None,
+                   prompt_len=None, repetition=None, presence=None, frequency=None,
+                   bias_tokens=None, bias_values=None, masks=None, mask_index=None, nodes=None,
+                   out=None, want_stats=True, stream=None, workspace=None):
+    """Penalties, biases and masks on the logits [B, N+1, V] of tree nodes
+    (``tv_process_logits``; bfloat16 or float32), into ``out`` (which may be
+    ``logits``). ``nodes`` = (first, count) restricts the call to those nodes of
+    every tree. Returns (out, row_max [B, N+1] float32, row_sum [B, N+1] float64),
+    the statistics ``verify_batch`` takes (None without ``want_stats``); rows of
+    other nodes are left as they were. Raises on a non-OK return."""
+    import torch
+    B, n1, V = logits.shape
+    dev = logits.device
+    first, count = (0, n1) if nodes is None else nodes
+    dtype = _dtype_code(logits)
+    if out is None:
+        out = torch.empty_like(logits)
+    i32, f32 = torch.int32, torch.float32
+    H = history.shape[-1] if history is not None else 0
+    nb = bias_tokens.shape[-1] if bias_tokens is not None else 0
+    nm = masks.shape[0] if masks is not None else 0
+    _check(dev, logits=(logits, (B, n1, V), logits.dtype), out=(out, (B, n1, V), logits.dtype),
+           parents=(parents, (B, n1), i32), tokens=(tokens, (B, n1), i32),
+           history=(history, (B, H), i32), history_len=(history_len, (B,), i32),
+           prompt_len=(prompt_len, (B,), i32), repetition=(repetition, (B,), f32),
+           presence=(presence, (B,), f32), frequency=(frequency, (B,), f32),
+           bias_tokens=(bias_tokens, (B, nb), i32), bias_values=(bias_values, (B, nb), f32),
+           masks=(masks, (nm, (V + 31) // 32), i32), mask_index=(mask_index, (B, n1), i32))
+    row_max = row_sum = None
+    with _on(dev):
+        need = 0
+        if want_stats:
+            row_max = torch.empty((B, n1), dtype=torch.float32, device=dev)
+            row_sum = torch.empty((B, n1), dtype=torch.float64, device=dev)
+            need = tv_process_logits_workspace_size(B, n1, V)
+        workspace, nbytes = _workspace(need, workspace, dev)
+        st = tv_process_logits(
+            B, n1, V, first, count, logits, dtype, temperature, parents, tokens, history, H,
+            history_len, prompt_len, repetition, presence, frequency, bias_tokens, bias_values, nb,
+            masks, nm, mask_index, out, row_max, row_sum, workspace, nbytes,
+            _stream_of(dev, stream))
+    if st != TV_OK:
+        raise TvError(st, "tv_process_logits")
+    return out, row_max, row_sum
+
+
+@dataclass
+class CacheGrowth:
+    slots: object        # [B, max_new] int32
+    seq_len: object      # [B] int32
+    free_count: object   # [1] int32
+    status: object       # [B] int32, TV_CACHE_*
+
+
+def cache_extend(new_len, seq_len, block_table, free_pages, free_count, page_size, max_new,
+                 prefix_len=0, out: CacheGrowth | None = None, stream=None) -> CacheGrowth:
+    """Growth of all requests by ``new_len`` positions (``tv_cache_extend``; int32
+    tensors): writes the block table's new entries in place and returns slots,
+    new lengths, the new count of free pages and the requests' statuses (``out``
+    may hold ``seq_len`` and ``free_count`` themselves). Raises on a non-OK
+    return."""
+    import torch
+    B, dev = new_len.shape[0], block_table.device
+    i32 = torch.int32
+    if out is None:
+        if B == 0:
+            return CacheGrowth(new_len.new_empty((0, max_new)), seq_len.clone(),
+                               free_count.clone(), new_len.new_empty(0))
+        out = CacheGrowth(*(torch.empty(s, dtype=i32, device=dev)
+                            for s in ((B, max_new), (B,), (1,), (B,))))
+    _check(dev, new_len=(new_len, (B,), i32), seq_len=(seq_len, (B,), i32),
+           block_table=(block_table, (B, block_table.shape[-1]), i32),
+           free_pages=(free_pages, (free_pages.shape[0],), i32), free_count=(free_count, (1,), i32),
+           slots=(out.slots, (B, max_new), i32), out_seq_len=(out.seq_len, (B,), i32),
+           out_free_count=(out.free_count, (1,), i32), status=(out.status, (B,), i32))
+    with _on(dev):
+        st = tv_cache_extend(B, new_len, max_new, seq_len, out.seq_len, block_table,
+                             block_table.shape[1], page_size, prefix_len, free_pages,
+                             free_pages.shape[0], free_count, out.free_count, out.slots,
+                             out.status, _stream_of(dev, stream))
+    if st != TV_OK:
+        raise TvError(st, "tv_cache_extend")
+    return out
+
+
+def cache_commit(k_new, v_new, k_cache, v_cache, new_len, slots, path_nodes=None, stream=None):
+    """Writes the committed nodes' keys and values of all layers into the cache
+    (``tv_cache_commit``): k_new and v_new [layers, B, N+1, kv_heads, D], k_cache
+    and v_cache [layers, pages, kv_heads, page_size, D] of any one type, new_len
+    [B] and slots [B, max_new] as ``cache_extend`` took and gave them, path_nodes
+    [B, width] from ``commit_paths`` (None: node k goes to slot k). Raises on a
+    non-OK return."""
+    import torch
+    if k_new.dim() != 5 or k_cache.dim() != 5:
+        raise ValueError("k_new, v_new and the caches have five dimensions")
+    L, B, n1, KH, D = k_new.shape
+    P, ps = k_cache.shape[1], k_cache.shape[3]
+    dev, dt, i32 = k_cache.device, k_cache.dtype, torch.int32
+    if tuple(k_cache.shape) != (L, P, KH, ps, D):
+        raise ValueError(f"k_cache has shape {tuple(k_cache.shape)}, expected {(L, P, KH, ps, D)}")
+    strides = {}
+    for name, t, like in (("k_new", k_new, k_new), ("v_new", v_new, k_new),
+                          ("k_cache", k_cache, k_cache), ("v_cache", v_cache, k_cache)):
+        if t.shape != like.shape:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(like.shape)}")
+        if L == 0:
+            return
+        one = _rows(name, t[0], dev, dt) if like is k_new else _pages(name, t[0], dev, dt)
+        strides[name] = (t.stride(0) if L > 1 else 0, one)
+    if strides["k_new"] != strides["v_new"] or strides["k_cache"] != strides["v_cache"]:
+        raise ValueError("keys and values must have the same strides")
+    most = slots.shape[-1]
+    width = path_nodes.shape[-1] if path_nodes is not None else 0
+    if path_nodes is not None and path_nodes.dim() == 2 and path_nodes.stride(0) != width:
+        path_nodes = path_nodes.contiguous()
+    _check(dev, new_len=(new_len, (B,), i32), slots=(slots, (B, most), i32),
+           path_nodes=(path_nodes, (B, width), i32))
+    e = k_new.element_size()
+    with _on(dev):
+        st = tv_cache_commit(L, B, n1, KH, D * e, k_new, v_new, strides["k_new"][0] * e,
+                             strides["k_new"][1] * e, k_cache, v_cache, strides["k_cache"][0] * e,
+                             strides["k_cache"][1] * e, P, ps, new_len, most, slots, path_nodes,
+                             width, _stream_of(dev, stream))
+    if st != TV_OK:
+        raise TvError(st, "tv_cache_commit")
 
 
 def workspace_tensor(batch: int, num_nodes: int, vocab: int, device):

@@ -10,7 +10,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libtv.so")
 
-SOURCES = ["tv_abi.cpp", "tv_kernels.hip", "tv_commit.hip", "tv_lmhead.hip"]
+SOURCES = ["tv_abi.cpp", "tv_ops_abi.cpp", "tv_kernels.hip", "tv_commit.hip", "tv_lmhead.hip",
+           "tv_logits.hip", "tv_cache.hip", "tv_attention.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -162,6 +162,124 @@ int validate_sample(const SampleArgs& a);
 // Enqueue the draft-tree token sampler on `stream` (arguments validated).
 int launch_sample(const SampleArgs& a, hipStream_t stream);
 
+// Attention of tree nodes over a paged cache (tv_tree_attention).
+struct AttentionArgs {
+  int32_t batch, num_nodes, heads, kv_heads, head_dim;
+  int32_t dtype;                // TV_DTYPE_BF16 or TV_DTYPE_F16
+  const int32_t* parents;
+  const void* q;
+  int64_t q_stride;             // elements between nodes
+  const void* k_new;
+  const void* v_new;
+  int64_t kv_stride;
+  const void* k_cache;
+  const void* v_cache;
+  int64_t page_stride;          // elements
+  int32_t num_pages, page_size;
+  const int32_t* block_table;
+  int32_t table_width;
+  const int32_t* ctx_len;
+  const int32_t* prefix_pages;
+  int32_t prefix_len;
+  float scale;
+  void* out;
+};
+
+// Bytes of workspace of an attention call (sizes validated).
+size_t attention_workspace(int32_t batch, int32_t num_nodes, int32_t heads, int32_t kv_heads,
+                           int32_t head_dim, int32_t prefix_len);
+
+// Enqueue the attention on `stream` (arguments validated).
+int launch_attention(const AttentionArgs& a, void* workspace, hipStream_t stream);
+
+// Penalties, biases and masks on logits (tv_process_logits).
+struct LogitsArgs {
+  int32_t batch, num_nodes, vocab, first_node, num_rows;
+  const void* logits;
+  int32_t dtype;                // TV_DTYPE_BF16 or TV_DTYPE_F32
+  float temperature;
+  const int32_t* parents;
+  const int32_t* tokens;
+  const int32_t* history;
+  int32_t max_history;
+  const int32_t* history_len;
+  const int32_t* prompt_len;
+  const float* repetition;
+  const float* presence;
+  const float* frequency;
+  const int32_t* bias_tokens;
+  const float* bias_values;
+  int32_t max_bias;
+  const uint32_t* masks;
+  int32_t num_masks;
+  const int32_t* mask_index;
+  void* out;
+  float* row_max;
+  double* row_sum;
+};
+
+constexpr int kLogitsChunk = 8192;    // tokens whose counts a workgroup holds
+constexpr int kLogitsWaves = 4;       // wavefronts of a workgroup
+
+// Workspace of tv_process_logits: one (max, sum) partial per row, chunk and
+// wavefront.
+struct LogitsLayout {
+  int chunks;
+  size_t off_max, off_sum, bytes;
+};
+inline LogitsLayout logits_layout(int32_t batch, int32_t num_nodes, int32_t vocab) {
+  LogitsLayout L{};
+  L.chunks = (vocab + kLogitsChunk - 1) / kLogitsChunk;
+  const size_t n = static_cast<size_t>(batch) * num_nodes * L.chunks * kLogitsWaves * sizeof(float);
+  L.off_max = 0;
+  L.off_sum = align256(n);
+  L.bytes = align256(L.off_sum + n);
+  return L;
+}
+
+// Enqueue the logits' processing on `stream` (arguments validated).
+int launch_logits(const LogitsArgs& a, void* workspace, hipStream_t stream);
+
+// Growth of block tables (tv_cache_extend).
+struct ExtendArgs {
+  int32_t batch;
+  const int32_t* new_len;
+  int32_t max_new;
+  const int32_t* seq_len;
+  int32_t* new_seq_len;
+  int32_t* block_table;
+  int32_t table_width, page_size, prefix_len;
+  int32_t* free_pages;
+  int32_t num_pages;
+  const int32_t* free_count;
+  int32_t* new_free_count;
+  int32_t* slots;
+  int32_t* status;
+};
+
+// Enqueue the growth on `stream` (arguments validated).
+int launch_extend(const ExtendArgs& a, hipStream_t stream);
+
+// Committed keys and values into the cache (tv_cache_commit). Sizes in bytes.
+struct CacheCommitArgs {
+  int32_t layers, batch, num_nodes, kv_heads, head_bytes;
+  const void* k_new;
+  const void* v_new;
+  int64_t new_layer_stride, node_stride;
+  void* k_cache;
+  void* v_cache;
+  int64_t cache_layer_stride, page_stride;
+  int32_t num_pages, page_size;
+  const int32_t* new_len;
+  int32_t max_new;
+  const int32_t* slots;
+  const int32_t* path_nodes;
+  int32_t path_width;
+};
+
+// Enqueue the writes on `stream` (arguments validated).
+int launch_cache_commit(const CacheCommitArgs& a, hipStream_t stream);
+
 // Enqueue the verification on `stream` (an initialisation kernel, then the
 // verifier). Arguments already validated. Returns a tv_status_t.
 int launch(const VerifyArgs& a, Algo algo, void* workspace, hipStream_t stream);

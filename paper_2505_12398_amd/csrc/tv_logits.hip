@@ -1,0 +1,396 @@
+// Penalties, biases and masks on the logits of tree nodes, with the statistics
+// of the resulting rows (tv_process_logits).
+//
+// A workgroup holds kLogitsChunk tokens of the vocabulary for one tree: it counts
+// the history's tokens among them once, in LDS, and then streams its part of the
+// tree's rows, so the history is read once for many rows and a row costs one read
+// and one write. What bounds it is HBM. Every thread owns the same 32 tokens in
+// every row: what the history and the biases take off their logits stays in its
+// registers. The drafted tokens on a node's path change few logits: their owners
+// compute those again.
+//
+// The statistics are a maximum and a sum of 2^((z - max) k), k = log2(e)/T, per
+// wavefront and row, in fp32 in the frame of the maximum; a second kernel merges
+// them in fp64.
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include "tv.h"
+#include "tv_launch.h"
+
+namespace {
+
+constexpr int kWaves = tv::kLogitsWaves, kThreads = 64 * kWaves;
+constexpr int kChunk = tv::kLogitsChunk;
+constexpr int kGroups = kChunk / (8 * kThreads);   // groups of 8 consecutive tokens of a thread
+constexpr int kOwn = 8 * kGroups;                  // tokens of a thread
+static_assert(kOwn == 32, "a thread's tokens are the bits of a word");
+constexpr uint32_t kTold = 0x80000000u;            // in the prompt; below it the count
+
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+// vectors of rows that need not start on 16 bytes
+typedef u32x4 __attribute__((aligned(2))) u32x4_any2;
+typedef u32x4 __attribute__((aligned(4))) u32x4_any4;
+
+// eight logits as they are stored
+template <class T> struct Raw;
+template <> struct Raw<uint16_t> {
+  u32x4 w;
+  __device__ __forceinline__ void load(const uint16_t* p) {
+    w = *reinterpret_cast<const u32x4_any2*>(p);
+  }
+  __device__ __forceinline__ float at(int i) const {
+    const uint32_t u = w[i >> 1];
+    return __uint_as_float(i & 1 ? u & 0xffff0000u : u << 16);
+  }
+};
+template <> struct Raw<float> {
+  u32x4 w[2];
+  __device__ __forceinline__ void load(const float* p) {
+    w[0] = *reinterpret_cast<const u32x4_any4*>(p);
+    w[1] = *reinterpret_cast<const u32x4_any4*>(p + 4);
+  }
+  __device__ __forceinline__ float at(int i) const { return __uint_as_float(w[i >> 2][i & 3]); }
+};
+
+__device__ __forceinline__ float value(uint16_t x) { return __uint_as_float(uint32_t{x} << 16); }
+__device__ __forceinline__ float value(float x) { return x; }
+template <class T> __device__ __forceinline__ T stored(float x);
+template <> __device__ __forceinline__ uint16_t stored<uint16_t>(float x) {
+  return __builtin_bit_cast(uint16_t, static_cast<__bf16>(x));   // to nearest even
+}
+template <> __device__ __forceinline__ float stored<float>(float x) { return x; }
+
+__device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    w[i] = uint32_t{stored<uint16_t>(v[2 * i])} | uint32_t{stored<uint16_t>(v[2 * i + 1])} << 16;
+  *reinterpret_cast<u32x4_any2*>(p) = w;
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[4 * h + i]);
+    *reinterpret_cast<u32x4_any4*>(p + 4 * h) = w;
+  }
+}
+
+struct Penalties {
+  float rho, inv, alpha, beta;
+};
+
+// z / rho or z * rho. The quotient is the product with 1 / rho corrected by its
+// own remainder, which rounds as the division does.
+__device__ __forceinline__ float repeated(float z, const Penalties& p) {
+  const float q = z * p.inv;
+  const float d = __builtin_amdgcn_div_fixupf(fmaf(fmaf(-q, p.rho, z), p.inv, q), p.rho, z);
+  return z > 0.0f ? d : z * p.rho;
+}
+
+// what presence, frequency and bias take off (each operation rounded by itself)
+__device__ __forceinline__ float taken(int n, float bias, const Penalties& p) {
+#pragma clang fp contract(off)
+  const float a = n > 0 ? p.alpha : 0.0f;
+  const float b = p.beta * static_cast<float>(n);
+  return (a + b) - bias;
+}
+
+struct Params {
+  tv::LogitsArgs a;
+  int chunks, slabs, rows;   // rows of a slab
+  float* part_max;           // [batch][num_nodes][chunks][wavefront]
+  float* part_sum;
+  float k32;                 // log2(e) / T rounded to fp32
+};
+
+template <class T>
+__global__ void __launch_bounds__(kThreads) logits_kernel(Params P) {
+  const tv::LogitsArgs& a = P.a;
+  __shared__ uint32_t words[kChunk];
+  __shared__ int32_t toks[TV_MAX_NODES];   // place in this chunk, or -1
+  __shared__ int16_t ups[TV_MAX_NODES];    // nearest proper ancestor with a token in this chunk, or 0
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int chunk = blockIdx.x % P.chunks, rest = blockIdx.x / P.chunks;
+  const int slab = rest % P.slabs, b = rest / P.slabs;
+  const int V = a.vocab, n1 = a.num_nodes;
+  const int base = chunk * kChunk, width = min(kChunk, V - base);
+  const Penalties pen = {a.repetition ? a.repetition[b] : 1.0f,
+                         1.0f / (a.repetition ? a.repetition[b] : 1.0f),
+                         a.presence ? a.presence[b] : 0.0f, a.frequency ? a.frequency[b] : 0.0f};
+  auto clear = [&] {
+    for (int i = tid; i < kChunk / 4; i += kThreads)
+      *reinterpret_cast<u32x4*>(&words[4 * i]) = u32x4{0, 0, 0, 0};
+  };
+  // token e of this thread (e < 32): its place in the chunk
+  auto place = [&](int e) { return ((e >> 3) * kThreads + tid) * 8 + (e & 7); };
+
+  // biases: of several entries for a token the last one
+  float off[kOwn];
+#pragma unroll
+  for (int e = 0; e < kOwn; ++e) off[e] = 0.0f;
+  const float* bias = a.bias_values + static_cast<size_t>(b) * a.max_bias;
+  const int32_t* bias_at = a.bias_tokens + static_cast<size_t>(b) * a.max_bias;
+  const int nbias = a.bias_tokens ? a.max_bias : 0;
+  clear();
+  if (nbias) {
+    __syncthreads();
+    for (int j = tid; j < nbias; j += kThreads) {
+      const unsigned t = static_cast<unsigned>(bias_at[j]) - base;
+      if (t < static_cast<unsigned>(width)) atomicMax(&words[t], static_cast<uint32_t>(j + 1));
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < kOwn; ++e) {
+      const uint32_t j = words[place(e)];
+      if (j) off[e] = bias[j - 1];
+    }
+    __syncthreads();
+    clear();
+  }
+  // the tree's tokens that lie in this chunk, and the links between them
+  if (a.parents)
+    for (int i = tid; i < n1; i += kThreads) {
+      const size_t at = static_cast<size_t>(b) * n1 + i;
+      const unsigned t = static_cast<unsigned>(a.tokens[at]) - base;
+      toks[i] = i > 0 && t < static_cast<unsigned>(width) ? static_cast<int>(t) : -1;
+      const int p = a.parents[at];
+      ups[i] = static_cast<int16_t>(p > 0 && p < i ? p : 0);
+    }
+  __syncthreads();
+  if (a.history) {
+    const int32_t* h = a.history + static_cast<size_t>(b) * a.max_history;
+    const int n = min(max(a.history_len[b], 0), a.max_history);
+    const int np = a.prompt_len ? min(max(a.prompt_len[b], 0), n) : 0;
+    for (int j = tid; j < n; j += kThreads) {
+      const unsigned t = static_cast<unsigned>(h[j]) - base;
+      if (t < static_cast<unsigned>(width)) {
+        if (j < np)
+          atomicOr(&words[t], kTold);
+        else
+          atomicAdd(&words[t], 1u);
+      }
+    }
+  }
+  // links skip nodes whose token is elsewhere (any ancestor read meanwhile is one)
+  if (a.parents) {
+    bool more;
+    do {
+      more = false;
+      for (int i = tid; i < n1; i += kThreads) {
+        const int u = ups[i];
+        if (u > 0 && toks[u] < 0) {
+          ups[i] = ups[u];
+          more = true;
+        }
+      }
+      more = __syncthreads_or(more);
+    } while (more);
+  } else {
+    __syncthreads();
+  }
+  uint32_t seen = 0;
+#pragma unroll
+  for (int e = 0; e < kOwn; ++e) {
+    const uint32_t w = words[place(e)];
+    seen |= static_cast<uint32_t>(w != 0) << e;
+    off[e] = taken(static_cast<int>(w & ~kTold), off[e], pen);
+  }
+
+  const T* const in = static_cast<const T*>(a.logits);
+  T* const to = static_cast<T*>(a.out);
+  const int mask_words = (V + 31) / 32;
+  const int r0 = a.first_node + slab * P.rows;
+  const int r1 = min(r0 + P.rows, a.first_node + a.num_rows);
+  const T ninf = stored<T>(-INFINITY);
+  auto row_of = [&](int i) { return static_cast<size_t>(b) * n1 + i; };
+  auto load = [&](int i, Raw<T> (&raw)[kGroups]) {
+    const T* p = in + row_of(i) * V + base;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const int at = (g * kThreads + tid) * 8;
+      if (at + 8 <= width) {
+        raw[g].load(p + at);
+      } else {
+        // a row's last few tokens
+        T x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = at + e < width ? p[at + e] : ninf;
+        __builtin_memcpy(&raw[g], x, sizeof x);
+      }
+    }
+  };
+  Raw<T> next[kGroups];
+  load(r0, next);
+  for (int i = r0; i < r1; ++i) {
+    Raw<T> raw[kGroups];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) raw[g] = next[g];
+    if (i + 1 < r1) load(i + 1, next);
+    const size_t row = row_of(i);
+    // this thread's tokens that are on the path
+    uint32_t mine = 0;
+    int first = 0;
+    if (a.parents) {
+      first = toks[i] >= 0 ? i : ups[i];
+      for (int x = first; x > 0; x = ups[x]) {
+        const int t = toks[x];
+        if (((t >> 3) & (kThreads - 1)) == tid) mine |= 1u << (t / (8 * kThreads) * 8 + (t & 7));
+      }
+    }
+    // this thread's allowed tokens
+    uint32_t allowed = ~0u;
+    if (a.mask_index) {
+      const int m = a.mask_index[row];
+      if (m >= a.num_masks) {
+        allowed = 0;
+      } else if (m >= 0) {
+        const uint8_t* bytes = reinterpret_cast<const uint8_t*>(
+            a.masks + static_cast<size_t>(m) * mask_words) + base / 8;
+        allowed = 0;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g)
+          if ((g * kThreads + tid) * 8 < width)
+            allowed |= uint32_t{bytes[g * kThreads + tid]} << (8 * g);
+      }
+    }
+    float v[kGroups][8];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float z = raw[g].at(e);
+        const float x = (seen >> (8 * g + e) & 1 ? repeated(z, pen) : z) - off[8 * g + e];
+        v[g][e] = allowed >> (8 * g + e) & 1 ? x : -INFINITY;
+      }
+    for (uint32_t left = mine & allowed; left; left &= left - 1) {
+      const int e = __builtin_ctz(left), t = place(e);
+      int n = static_cast<int>(words[t] & ~kTold);
+      for (int x = first; x > 0; x = ups[x]) n += toks[x] == t;
+      float add = 0.0f;
+      for (int j = nbias - 1; j >= 0; --j)
+        if (bias_at[j] == base + t) {
+          add = bias[j];
+          break;
+        }
+      const float x = repeated(value(in[row * V + base + t]), pen) - taken(n, add, pen);
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[g][k] = 8 * g + k == e ? x : v[g][k];
+    }
+    T* q = to + row * V + base;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const int at = (g * kThreads + tid) * 8;
+      if (at + 8 <= width) {
+        store8(q + at, v[g]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (at + e < width) q[at + e] = stored<T>(v[g][e]);
+      }
+    }
+    if (!P.part_max) continue;
+    float mx = -INFINITY;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[g][e] = value(stored<T>(v[g][e]));
+        const int at = (g * kThreads + tid) * 8 + e;
+        if (at >= width) v[g][e] = -INFINITY;
+        mx = fmaxf(mx, v[g][e]);
+      }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+    // a row with no finite value keeps the frame 0, so its terms are 0 as well
+    const float c = mx > -INFINITY ? -mx * P.k32 : 0.0f;
+    float s = 0.0f;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s += __builtin_amdgcn_exp2f(fmaf(v[g][e], P.k32, c));
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    if (lane == 0) {
+      const size_t part = (row * P.chunks + chunk) * kWaves + wave;
+      P.part_max[part] = mx;
+      P.part_sum[part] = s;
+    }
+  }
+}
+
+// Merges a row's partials, a wavefront a row: each moves from its frame, the fp32
+// product -max k, to that of the row's maximum.
+__global__ void __launch_bounds__(kThreads) logits_merge_kernel(Params P) {
+  const tv::LogitsArgs& a = P.a;
+  const int lane = threadIdx.x & 63;
+  const long long r = static_cast<long long>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
+  if (r >= static_cast<long long>(a.batch) * a.num_rows) return;
+  const long long b = r / a.num_rows;
+  const size_t row = static_cast<size_t>(b) * a.num_nodes + a.first_node + (r - b * a.num_rows);
+  const int parts = P.chunks * kWaves;
+  const float* pm = P.part_max + row * parts;
+  const float* ps = P.part_sum + row * parts;
+  float m = -INFINITY;
+  for (int t = lane; t < parts; t += 64) m = fmaxf(m, pm[t]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  const double cm = static_cast<double>(-m * P.k32);
+  double s = 0.0;
+  for (int t = lane; t < parts; t += 64) {
+    const float mt = pm[t];
+    const double st = static_cast<double>(ps[t]);
+    s += mt > -INFINITY ? st * exp2(cm - static_cast<double>(-mt * P.k32)) : st;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  if (lane == 0) {
+    a.row_max[row] = m;
+    // from the rounded frame to the exact one of the maximum
+    a.row_sum[row] = m > -INFINITY && isfinite(m)
+                         ? s * exp2(-(cm + static_cast<double>(m) * static_cast<double>(P.k32)))
+                         : s;
+  }
+}
+
+// Workgroups that fill the device a few times over.
+constexpr int kEnough = 2048;
+
+}  // namespace
+
+namespace tv {
+
+int launch_logits(const LogitsArgs& a, void* workspace, hipStream_t stream) {
+  const LogitsLayout L = logits_layout(a.batch, a.num_nodes, a.vocab);
+  Params P{};
+  P.a = a;
+  P.chunks = L.chunks;
+  if (a.row_max) {
+    P.part_max = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + L.off_max);
+    P.part_sum = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + L.off_sum);
+  }
+  P.k32 = static_cast<float>(1.4426950408889634 / static_cast<double>(a.temperature));
+  const int64_t per = static_cast<int64_t>(a.batch) * P.chunks;
+  const int64_t want = (kEnough + per - 1) / per;
+  P.slabs = static_cast<int>(want < a.num_rows ? want : a.num_rows);
+  P.rows = (a.num_rows + P.slabs - 1) / P.slabs;
+  P.slabs = (a.num_rows + P.rows - 1) / P.rows;
+  if (per * P.slabs > INT32_MAX) return TV_ERR_UNSUPPORTED;
+  const dim3 grid(static_cast<unsigned>(per * P.slabs));
+  if (a.dtype == TV_DTYPE_BF16)
+    hipLaunchKernelGGL((logits_kernel<uint16_t>), grid, dim3(kThreads), 0, stream, P);
+  else
+    hipLaunchKernelGGL((logits_kernel<float>), grid, dim3(kThreads), 0, stream, P);
+  if (hipGetLastError() != hipSuccess) return TV_ERR_HIP;
+  if (!a.row_max) return TV_OK;
+  const int64_t rows = static_cast<int64_t>(a.batch) * a.num_rows;
+  hipLaunchKernelGGL(logits_merge_kernel, dim3(static_cast<unsigned>((rows + kWaves - 1) / kWaves)),
+                     dim3(kThreads), 0, stream, P);
+  return hipGetLastError() == hipSuccess ? TV_OK : TV_ERR_HIP;
+}
+
+}  // namespace tv
