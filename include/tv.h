@@ -389,15 +389,17 @@ int tv_commit_paths(int32_t batch, int32_t num_nodes, const int32_t* parents,
  *
  * A tree whose block table names a page outside [0, num_pages) for a position
  * below ctx_len, or whose ctx_len exceeds table_width * page_size, gets NaN in
- * every output.
+ * every output. The order of a tree's sums, and so its last bits, depends on the
+ * lengths of all trees of the call; the same call gives the same bits.
  *
  * head_dim: a multiple of 8 up to TV_MAX_HEAD_DIM; heads a multiple of
  * kv_heads; heads * head_dim at most TV_MAX_HIDDEN; page_size a power of two
  * from TV_MIN_PAGE to TV_MAX_PAGE; scale positive and finite; q, k_new, v_new,
  * caches and out 16-byte aligned, strides multiples of 8; the nodes of a tree,
- * and a page, at most 2^30 bytes. out dtype [batch][num_nodes][heads][head_dim].
- * workspace: tv_tree_attention_workspace_size() bytes (0 for invalid sizes),
- * 256-byte aligned. Nothing is allocated. Returns a tv_status_t; argument errors
+ * and a page, at most 2^29 bytes; batch * num_nodes * heads at most 2^31 - 1.
+ * out dtype [batch][num_nodes][heads][head_dim]. workspace:
+ * tv_tree_attention_workspace_size() bytes (0 for invalid sizes), 256-byte
+ * aligned. Nothing is allocated. Returns a tv_status_t; argument errors
  * launch nothing.
  */
 size_t tv_tree_attention_workspace_size(int32_t batch, int32_t num_nodes, int32_t heads,

@@ -1,104 +1,943 @@
-// Attention of tree nodes over a paged cache (tv_tree_attention): a workgroup per
-// tree, node and query head, 256 keys at a time with the running maximum and sum
-// of the softmax.
+// Attention of tree nodes over a paged cache for gfx950 (tv_tree_attention).
+//
+// All nodes of a tree and all query heads of a key head read the same cached keys
+// and values: these num_nodes * heads / kv_heads query rows are the columns of one
+// matrix product with each key. Per 32 keys a wavefront forms S^T = K Q^T, takes
+// 2^(s k - m k) with k = scale log2(e) in the frame of a running maximum m, and
+// adds V^T P^T to its accumulators (16x16x32 products; out = sum p v / sum p).
+// With keys as rows of S^T, a lane holds four consecutive keys of one query, which
+// is how the second product wants its operand: P never leaves its lane, the keys
+// of the two blocks taken in the order in which the lanes hold them. Values are
+// read transposed from LDS.
+//
+// The frame is a maximum seen so far; it moves only once some score exceeds it by
+// 8 in powers of two, so that most tiles rescale nothing (weights up to 2^8 in
+// their frame; sums in fp32). Weights are rounded to the type of the values, the
+// operand type of the product; sums of weights are those before that rounding.
+//
+// Keys and values come through LDS, in 16-key halves (a page holds whole halves)
+// by buffer loads that write LDS directly, chunks of 16 bytes of row r at position
+// c ^ f(r) so that the reads touch all banks. A workgroup of four wavefronts has RW
+// row groups of 16 MT rows and KW = 4 / RW groups of keys, which take the tiles in
+// turn and are merged at the end.
+//
+// Work. The tiles of all trees and key heads form one line that is cut into equal
+// parts, so ragged contexts keep every CU as busy as equal ones. A part is taken by
+// a team of workgroups, one for each tile of rows, on one XCD at the same time, so
+// that the keys leave HBM once. An item that is cut leaves its parts' (maximum, sum,
+// accumulators) in the workspace, and a second kernel merges them.
+//
+// A common prefix is an item of its own whose rows are those of all trees; its
+// (maximum, sum, accumulators) wait in the workspace for the trees' own parts.
 #include <hip/hip_runtime.h>
 #include <math.h>
+
+#include <mutex>
+#include <type_traits>
+#include <utility>
 
 #include "tv.h"
 #include "tv_launch.h"
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kWaves = 4;
+constexpr int kKeys = 32, kHalf = 16;     // keys of a tile and of a half
+constexpr int kXcds = 8, kMaxCus = 256;
+constexpr int kPerCu = 2;                 // workgroups on a CU
+constexpr int kMaxTeam = 32;              // workgroups of a team: the CUs of an XCD
+constexpr int kMinTiles = 8;              // of a part
 
-__device__ __forceinline__ float value(__bf16 x) { return static_cast<float>(x); }
-__device__ __forceinline__ float value(_Float16 x) { return static_cast<float>(x); }
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(8))) short s16x8;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((address_space(3))) uint8_t lds_byte;
+#define LDS(type) __attribute__((address_space(3))) type
+// read through the scalar cache: nothing of the launch writes it
+#define CONSTANT(type) const __attribute__((address_space(4))) type
 
-template <class T>
-__global__ void __launch_bounds__(kThreads) attention_kernel(tv::AttentionArgs a) {
-  __shared__ float qs[TV_MAX_HEAD_DIM];
-  __shared__ float ps[kThreads];
-  __shared__ const T* vs[kThreads];
-  __shared__ float red[kThreads / 64];
-  __shared__ uint8_t on_path[TV_MAX_NODES];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int h = blockIdx.x, i = blockIdx.y, b = blockIdx.z;
-  const int D = a.head_dim, n1 = a.num_nodes, kh = h / (a.heads / a.kv_heads);
-  const int ctx = a.ctx_len[b];
-  if (ctx < 0) return;
-  const int shift = 31 - __builtin_clz(a.page_size);
-  const bool shared = a.prefix_len > 0 && ctx >= a.prefix_len;
-  const size_t node = static_cast<size_t>(b) * n1 + i;
-  const T* q = static_cast<const T*>(a.q) + node * a.q_stride + h * D;
-  for (int d = tid; d < D; d += kThreads) qs[d] = value(q[d]);
-  for (int j = tid; j < n1; j += kThreads) on_path[j] = 0;
-  __syncthreads();
-  if (tid == 0) {
-    int x = i;
-    on_path[x] = 1;
-    while (x > 0) {
-      const int p = a.parents[static_cast<size_t>(b) * n1 + x];
-      if (p < 0 || p >= x) break;
-      x = p;
-      on_path[x] = 1;
+struct Bf16 {
+  static __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {   // to nearest even
+    return uint32_t{__builtin_bit_cast(uint16_t, static_cast<__bf16>(lo))} |
+           uint32_t{__builtin_bit_cast(uint16_t, static_cast<__bf16>(hi))} << 16;
+  }
+  static __device__ __forceinline__ float value(uint16_t x) { return __uint_as_float(uint32_t{x} << 16); }
+  static constexpr uint32_t kExponent = 0x7f80;
+};
+struct F16 {
+  static __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    return uint32_t{__builtin_bit_cast(uint16_t, static_cast<_Float16>(lo))} |
+           uint32_t{__builtin_bit_cast(uint16_t, static_cast<_Float16>(hi))} << 16;
+  }
+  static __device__ __forceinline__ float value(uint16_t x) {
+    return static_cast<float>(__builtin_bit_cast(_Float16, x));
+  }
+  static constexpr uint32_t kExponent = 0x7c00;
+};
+
+// One pass: the trees over their own positions, or all their rows over the prefix.
+struct Pass {
+  const uint16_t* q;
+  const uint16_t* k_new;
+  const uint16_t* v_new;
+  const uint16_t* k_cache;
+  const uint16_t* v_cache;
+  const int32_t* parents;
+  const int32_t* table;
+  const int32_t* ctx_len;       // NULL in the prefix pass
+  uint16_t* out;
+  int64_t q_stride, kv_stride, page_stride;
+  int num_pages, page_shift, table_width;
+  int batch, num_nodes, heads, kv_heads, head_dim;
+  int group;                    // query heads of a key head
+  int rows;                     // query rows of a tree and key head
+  int prefix_len;
+  bool prefix_pass;
+  int team, chunks, teams;      // row tiles of a team, teams' worth of row tiles, teams
+  float k;                      // scale log2(e)
+  float slack;                  // how far a score may exceed its frame
+  float* parts;                 // [team][2][member]: accumulators, then (maximum, sum) per row
+  i32x4* desc;                  // [team]: tree, key head, chunk, parts of the item cut before it
+  float* pre;                   // prefix accumulators [row][DP]
+  f32x2* pre_ml;                // their (maximum, sum)
+};
+
+template <int DP_, int MT_, int RW_>
+struct Shape {
+  static constexpr int DP = DP_, MT = MT_, RW = RW_, KW = kWaves / RW;
+  static constexpr int BM = 16 * MT * RW;         // rows of a workgroup
+  static constexpr int CH = DP / 8;               // 16-byte chunks of a row
+  static constexpr int DB = DP / 16;              // 16-wide blocks of the head
+  static constexpr int ROW = DP * 2;
+  static constexpr int HALF = kHalf * ROW;        // bytes
+  static constexpr int LOADS = HALF / 1024;       // load instructions of a half
+  static constexpr int MAT = 2 * HALF, STAGE = 2 * MAT;
+  // loads of a wavefront per tile, of keys (or values)
+  static constexpr int MINE = 2 * LOADS / RW;
+  // One wavefront per key group and a wide head leave room for one tile: its keys are
+  // refilled after the first product and its values after the second.
+  static constexpr bool SPLIT = RW == 1 && DP == 128;
+  static constexpr int S = SPLIT ? 1 : DP == 128 ? RW : RW == 1 ? 2 : 4;
+  static constexpr int RING = KW * S * STAGE;
+  // accumulators and (maximum, sum) of the other key groups
+  static constexpr int ACC = (KW - 1) * RW * MT * DB * 1024;
+  static constexpr int MERGE = ACC + (KW - 1) * RW * MT * 64 * 8;
+  static constexpr int MAIN = RING > MERGE ? RING : MERGE;
+  static constexpr int PARENTS = MAIN;            // int16 per node
+  static constexpr int WALK = PARENTS + 2 * TV_MAX_NODES;
+  static constexpr int FLAGS = WALK + 2 * kWaves * 16 * MT;
+  static constexpr int SCAN = FLAGS + 4 * kWaves;
+  static constexpr int BYTES = SCAN + 8 * (kWaves + 2) + 16;
+  // floats of a part in the workspace
+  static constexpr int PART_ACC = RW * MT * DB * 256;
+  static constexpr int PART = PART_ACC + BM * 2;
+  static_assert(BYTES <= 160 * 1024 / kPerCu, "two workgroups on a CU");
+  static_assert((S - 1) * 2 * MINE < 64, "the count of loads in flight");
+};
+
+constexpr int kPastRange = 0x40000000, kRange = 0x3fffffff;
+
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+// 64 lanes' 16 bytes from the buffer at byte offset voff into LDS at dst + 16 lane;
+// zeros for an offset past the range. (In assembly, so that the compiler does not
+// wait for it at the next LDS read: the waits are written out below.)
+__device__ __forceinline__ void load_to_lds(const i32x4& rs, int voff, int dst) {
+  asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :: "s"(dst), "v"(voff), "s"(rs) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+// All but the newest N loads have landed, and this wavefront's LDS reads are done.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(N) : "memory");
+}
+__device__ __forceinline__ void barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// the largest of three, NaN if one is
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+}
+
+template <class F, int... I>
+__device__ __forceinline__ void unrolled(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void unrolled(F&& f) {
+  unrolled(f, std::make_integer_sequence<int, N>{});
+}
+
+// The frame of a maximum, -m k (0 where there is none), rounded by itself: sums are
+// moved between frames by the differences of these.
+__device__ __forceinline__ float frame(float m, float k) {
+#pragma clang fp contract(off)
+  return m > -INFINITY ? -m * k : 0.0f;
+}
+// What takes a sum from the frame of m to that of top >= m. (0 where nothing was
+// seen; a sum that is NaN stays NaN.)
+__device__ __forceinline__ float to_frame(float m, float top, float k) {
+  return m > -INFINITY ? __builtin_amdgcn_exp2f(frame(top, k) - frame(m, k)) : 0.0f;
+}
+
+// Positions of tree b that this pass reads from pages, where they start, and whether
+// its table cannot hold its context.
+struct Reach {
+  int from, len, tiles;   // first position, positions, tiles with those of the nodes
+  bool bad, shared;
+};
+__device__ __forceinline__ Reach reach(const Pass& P, int ctx) {
+  Reach r{};
+  if (P.prefix_pass) {
+    r.len = P.prefix_len;
+    r.tiles = (r.len + kKeys - 1) / kKeys;
+    return r;
+  }
+  if (ctx < 0) return r;
+  r.shared = P.prefix_len > 0 && ctx >= P.prefix_len;
+  r.from = r.shared ? P.prefix_len : 0;
+  r.bad = ctx > static_cast<long long>(P.table_width) << P.page_shift ||
+          (ctx > r.from && P.num_pages == 0);
+  r.len = r.bad ? 0 : ctx - r.from;
+  r.tiles = (r.len + kKeys - 1) / kKeys + (P.num_nodes + kKeys - 1) / kKeys;
+  return r;
+}
+__device__ __forceinline__ int context(const Pass& P, int b) {
+  return P.prefix_pass ? 0 : ((CONSTANT(int)*)P.ctx_len)[b];
+}
+
+// A value that all lanes hold, known as such.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ long long uniform(long long x) {
+  const uint32_t lo = static_cast<uint32_t>(uniform(static_cast<int>(x)));
+  return static_cast<long long>(
+      static_cast<uint64_t>(static_cast<uint32_t>(uniform(static_cast<int>(x >> 32)))) << 32 | lo);
+}
+
+// The same value, of which the compiler knows nothing: what is computed from it
+// stays behind this point and out of the registers of the loop over the tiles.
+__device__ __forceinline__ int here(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// Where part `t` of `parts` begins on the line of `total` tiles.
+__device__ __forceinline__ long long cut(long long total, int t, int parts) {
+  const long long each = total / parts;
+  return each * t + (total - each * parts) * t / parts;
+}
+
+// Rows of one block of 16: adds what is kept elsewhere, and writes the result.
+template <class T, class SH>
+struct Finish {
+  // The prefix' part of row `row` (of all trees' query rows), into the running (m, l, acc).
+  static __device__ __forceinline__ void absorb(const Pass& P, size_t at, int g, int db0, int ndb,
+                                                float& m, float& l, f32x4* acc) {
+    const f32x2 ml = P.pre_ml[at];
+    const float top = fmaxf(m, ml[0]);
+    const float a = to_frame(m, top, P.k), b = to_frame(ml[0], top, P.k);
+    m = top;
+    l = l * a + ml[1] * b;
+    for (int i = 0; i < ndb; ++i) {
+      const f32x4 o = *reinterpret_cast<const f32x4*>(P.pre + at * SH::DP + 16 * (db0 + i) + 4 * g);
+      for (int r = 0; r < 4; ++r) acc[i][r] = acc[i][r] * a + o[r] * b;
     }
   }
-  __syncthreads();
-  bool bad = ctx > static_cast<int64_t>(a.table_width) * a.page_size;
-  const long long n = bad ? 0 : static_cast<long long>(ctx) + n1;
-  float m = -INFINITY, l = 0.0f, o = 0.0f;
-  for (long long t0 = 0; t0 < n; t0 += kThreads) {
-    const long long x = t0 + tid;
-    const T *k = nullptr, *v = nullptr;
-    if (x < ctx) {
-      const int at = static_cast<int>(x), j = at >> shift;
-      const int page = shared && at < a.prefix_len
-                           ? a.prefix_pages[j]
-                           : a.block_table[static_cast<size_t>(b) * a.table_width + j];
-      if (page < 0 || page >= a.num_pages) {
-        bad = true;
-      } else {
-        const size_t e = page * a.page_stride +
-                         (static_cast<size_t>(kh) * a.page_size + (at & (a.page_size - 1))) * D;
-        k = static_cast<const T*>(a.k_cache) + e;
-        v = static_cast<const T*>(a.v_cache) + e;
-      }
-    } else if (x < n && on_path[x - ctx]) {
-      const size_t e = (static_cast<size_t>(b) * n1 + (x - ctx)) * a.kv_stride + kh * D;
-      k = static_cast<const T*>(a.k_new) + e;
-      v = static_cast<const T*>(a.v_new) + e;
-    }
-    float s = -INFINITY;
-    if (k) {
-      s = 0.0f;
-      for (int d = 0; d < D; ++d) s = fmaf(qs[d], value(k[d]), s);
-      s *= a.scale;
-    }
-    float top = s;
-    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-    if (lane == 0) red[wave] = top;
-    __syncthreads();
-    top = m;
-    for (int w = 0; w < kThreads / 64; ++w) top = fmaxf(top, red[w]);
-    ps[tid] = k ? expf(s - top) : 0.0f;
-    vs[tid] = v;
-    __syncthreads();
-    if (top > -INFINITY) {
-      const float f = expf(m - top);
-      l *= f;
-      o *= f;
-      m = top;
-    }
-    for (int j = 0; j < kThreads; ++j)
-      if (vs[j]) {
-        l += ps[j];
-        if (tid < D) o = fmaf(ps[j], value(vs[j][tid]), o);
-      }
-    __syncthreads();
+};
+
+// Output index of row r of an item: (node of the pass, head).
+__device__ __forceinline__ size_t out_row(const Pass& P, int b, int kh, int r) {
+  const int node = r / P.group, g = r - node * P.group;
+  return (static_cast<size_t>(b) * P.num_nodes + node) * P.heads + kh * P.group + g;
+}
+
+template <class T, class SH>
+__device__ __forceinline__ void write_out(const Pass& P, size_t row, int d, const f32x4& o) {
+  if (d >= P.head_dim) return;
+  *reinterpret_cast<u32x2*>(P.out + row * P.head_dim + d) =
+      u32x2{T::pack(o[0], o[1]), T::pack(o[2], o[3])};
+}
+
+template <class T, class SH>
+__global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
+  constexpr int MT = SH::MT, RW = SH::RW, KW = SH::KW, DB = SH::DB, KK = SH::DP / 32;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[SH::BYTES];
+  lds_byte* const lds = (lds_byte*)smem;
+  const int lds0 = static_cast<int>(reinterpret_cast<uintptr_t>(lds));
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rg = wave % RW, kg = wave / RW;
+  const int n = lane & 15, g = lane >> 4;
+
+  // This workgroup's team and row tile. Workgroups are dealt to the XCDs in turn.
+  const int per_xcd = P.teams / kXcds;
+  const int in_xcd = blockIdx.x / kXcds;
+  const int of_xcd = uniform(in_xcd / P.team), member = in_xcd - of_xcd * P.team;
+  const int team = static_cast<int>(blockIdx.x % kXcds) * per_xcd + of_xcd;
+  if (of_xcd >= per_xcd) return;
+
+  // The line of tiles: how long, and where this team's part begins.
+  LDS(long long)* const scan = (LDS(long long)*)(lds + SH::SCAN);
+  LDS(int)* const found = (LDS(int)*)(scan + kWaves + 2);
+  const long long per_tile = static_cast<long long>(P.kv_heads) * P.chunks;
+  const int per = (P.batch + kThreads - 1) / kThreads;
+  const int b_lo = min(tid * per, P.batch), b_hi = min(b_lo + per, P.batch);
+  long long own = 0;
+  for (int b = b_lo; b < b_hi; ++b)
+    own += reach(P, P.prefix_pass ? 0 : P.ctx_len[b]).tiles * per_tile;
+  long long upto = own;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const long long o = __shfl_up(upto, off, 64);
+    if (lane >= off) upto += o;
   }
-  bad = __syncthreads_or(bad);
-  if (tid < D)
-    static_cast<T*>(a.out)[(node * a.heads + h) * D + tid] = static_cast<T>(bad ? NAN : o / l);
+  if (lane == 63) scan[wave] = upto;
+  barrier();
+  long long total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) upto += scan[w];
+    total += scan[w];
+  }
+  total = uniform(total);
+  const long long room = total / kMinTiles;
+  const int parts = uniform(static_cast<int>(max<long long>(1, min<long long>(P.teams, room))));
+  const bool idle = team >= parts || total == 0;
+  const long long begin = idle ? 0 : uniform(cut(total, team, parts));
+  const long long end = idle ? 0 : uniform(cut(total, team + 1, parts));
+  if (idle) {
+    if (member == 0 && tid == 0) P.desc[team] = i32x4{0, 0, 0, 0};
+    return;
+  }
+  if (upto - own <= begin && begin < upto) {
+    long long at = upto - own;
+    for (int b = b_lo; b < b_hi; ++b) {
+      const long long t = reach(P, P.prefix_pass ? 0 : P.ctx_len[b]).tiles * per_tile;
+      if (begin < at + t) {
+        scan[kWaves] = begin - at;
+        found[0] = b;
+        break;
+      }
+      at += t;
+    }
+  }
+  barrier();
+  int b = uniform(found[0]);
+  long long in_tree = uniform(scan[kWaves]);
+
+  // Loads: instruction i of a half fills 1024 bytes, this lane the chunk at position
+  // lane % CH of row i * 1024 / ROW + lane / CH. Swizzle: sixteen rows' reads of one
+  // chunk, and eight rows' reads of two neighbouring ones, touch all banks once.
+  constexpr int kRowsPer = 1024 / SH::ROW;
+  auto swizzle = [](int r) {
+    return SH::DP == 128 ? (r & 7) << 1 | (r >> 3 & 1) : (r & 6) | (r >> 3 & 1);
+  };
+  auto offset = [&](int ln, int i, int last, int stride) {
+    const int r = i * kRowsPer + ln / SH::CH;
+    const int c = ln % SH::CH ^ swizzle(r);
+    return 8 * c < P.head_dim ? min(r, last) * stride + 16 * c : kPastRange;
+  };
+  const int dbytes = P.head_dim * 2;
+  int kv_off[SH::LOADS];
+#pragma unroll
+  for (int i = 0; i < SH::LOADS; ++i) kv_off[i] = offset(lane, i, kHalf - 1, dbytes);
+  // Reads: keys, row n of a block and chunk 4 kk + g; values, four keys 4 g .. 4 g + 3
+  // by sixteen of the head, lane n's eight bytes at key n / 4, transposed by the read.
+  const int k_at = n * SH::ROW + (g ^ swizzle(n)) * 16;
+  const int vrow = 4 * g + (n >> 2);
+  const int v_at = vrow * SH::ROW + (((n & 3) >> 1) ^ swizzle(vrow)) * 16 + (n & 1) * 8;
+  LDS(int16_t)* const par = (LDS(int16_t)*)(lds + SH::PARENTS);
+  LDS(int)* const flags = (LDS(int)*)(lds + SH::FLAGS);
+  // the next node on the path of each of this wavefront's rows
+  LDS(int16_t)* const walk = (LDS(int16_t)*)(lds + SH::WALK) + wave * 16 * MT;
+
+  bool opened = false;
+  for (long long pos = begin; pos < end;) {
+    // the item at pos
+    const int ctx = context(P, b);
+    const Reach R = reach(P, ctx);
+    const long long in_all = R.tiles * per_tile;
+    if (in_tree >= in_all) {      // (also trees without tiles)
+      in_tree -= in_all;
+      if (++b >= P.batch) break;
+      continue;
+    }
+    const int item = uniform(static_cast<int>(in_tree / R.tiles));
+    const int t0 = static_cast<int>(in_tree - static_cast<long long>(item) * R.tiles);
+    const int kh = uniform(item / P.chunks), chunk = item - kh * P.chunks;
+    const int t1 = static_cast<int>(min<long long>(R.tiles, t0 + (end - pos)));
+    if (!opened) {
+      opened = true;
+      if (member == 0 && tid == 0) {
+        // the item this part cuts, if no earlier part cuts it too
+        const long long s = begin - t0, e = s + R.tiles;
+        int count = 0;
+        if (team > 0 && t0 > 0 && cut(total, team - 1, parts) <= s) {
+          count = 2;
+          while (team + count - 1 < parts && cut(total, team + count - 1, parts) < e) ++count;
+        }
+        P.desc[team] = i32x4{b, kh, chunk, count};
+      }
+    }
+    pos += t1 - t0;
+    in_tree += t1 - t0;
+    const int row_tile = chunk * P.team + member;
+    const int r0 = row_tile * SH::BM;
+    if (r0 >= P.rows) continue;   // (for the whole workgroup)
+    const int nct = (R.len + kKeys - 1) / kKeys;
+
+    // queries
+    const int rbase = r0 + rg * 16 * MT;
+    s16x8 q[MT][KK];
+    const int qn = here(n), qg = here(g);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      const int r = min(rbase + 16 * mt + qn, P.rows - 1);
+      const int node = r / P.group;
+      walk[16 * mt + qn] = static_cast<int16_t>(node);   // (the prefix pass walks no paths)
+      const uint16_t* src = P.q + (static_cast<int64_t>(b) * P.num_nodes + node) * P.q_stride +
+                            (kh * P.group + r - node * P.group) * P.head_dim;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        const int d = 32 * kk + 8 * qg;
+        q[mt][kk] = d < P.head_dim ? *reinterpret_cast<const s16x8*>(src + d) : s16x8{};
+      }
+    }
+    if (t1 > nct && !P.prefix_pass) {
+      for (int i = tid; i < P.num_nodes; i += kThreads) {
+        const int p = P.parents && i > 0
+                          ? P.parents[static_cast<size_t>(b) * P.num_nodes + i] : -1;
+        par[i] = static_cast<int16_t>(p >= 0 && p < i ? p : -1);
+      }
+    }
+    barrier();                    // the links are there (and the last item's merge is done)
+
+    // Loads of tile t: this wavefront's part of its keys (0) and values (1).
+    CONSTANT(int)* const pages =
+        (CONSTANT(int)*)(P.table + static_cast<size_t>(b) * P.table_width);
+    bool bad = R.bad;
+    auto first_key = [&](int t, int h) { return R.from + t * kKeys + h * kHalf; };
+    auto page_of = [&](int t, int h) {
+      return t < nct ? pages[min(first_key(t, h), R.from + R.len - 1) >> P.page_shift] : 0;
+    };
+    constexpr int kHalves = RW == 1 ? 2 : 1;        // halves this wavefront loads
+    const int h0 = RW == 4 ? rg >> 1 : RW == 2 ? rg : 0;
+    int page[kHalves];
+    auto fetch = [&](int t) {
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) page[h] = page_of(t, h0 + h);
+    };
+    const int ring = kg * SH::S * SH::STAGE;
+    const int in_page = (1 << P.page_shift) - 1;
+    auto issue = [&](int t, int slot, auto what) {
+      constexpr int w0 = what.value == 2 ? 0 : what.value, w1 = what.value == 2 ? 2 : w0 + 1;
+      constexpr int in = RW == 4 ? SH::LOADS / 2 : SH::LOADS;
+      const int odd = RW == 4 ? rg & 1 : 0;         // which loads of the half
+#pragma unroll
+      for (int hh = 0; hh < kHalves; ++hh) {
+        const int h = h0 + hh;
+        const int dst = lds0 + ring + slot * SH::STAGE + h * SH::HALF + odd * in * 1024;
+        int64_t base;
+        int last, stride = dbytes;
+        if (t < nct) {
+          const int key = min(first_key(t, h), R.from + R.len - 1);
+          last = R.from + R.len - key - 1;          // rows past the context: its last one again
+          int pg = page[hh];
+          if (pg < 0 || pg >= P.num_pages) {
+            bad = true;
+            pg = 0;
+          }
+          base = pg * P.page_stride +
+                 ((static_cast<int64_t>(kh) << P.page_shift) + (key & in_page)) * P.head_dim;
+        } else {                                    // nodes, the last ones first
+          const int from = min((R.tiles - 1 - t) * kKeys + h * kHalf, P.num_nodes - 1);
+          last = P.num_nodes - 1 - from;
+          stride = static_cast<int>(P.kv_stride) * 2;
+          base = (static_cast<int64_t>(b) * P.num_nodes + from) * P.kv_stride + kh * P.head_dim;
+        }
+#pragma unroll
+        for (int w = w0; w < w1; ++w) {
+          const uint64_t a = reinterpret_cast<uint64_t>(
+              (t < nct ? w ? P.v_cache : P.k_cache : w ? P.v_new : P.k_new) + base);
+          const i32x4 rs = {static_cast<int>(a), static_cast<int>(a >> 32) & 0xffff, kRange,
+                            0x00020000};
+          if (t < nct && last >= kHalf - 1) {
+#pragma unroll
+            for (int i = 0; i < in; ++i)
+              load_to_lds(rs, odd ? kv_off[SH::LOADS - in + i] : kv_off[i],
+                          dst + w * SH::MAT + i * 1024);
+          } else {
+            const int ln = here(lane);
+#pragma unroll 1
+            for (int i = 0; i < in; ++i)
+              load_to_lds(rs, offset(ln, odd * in + i, last, stride), dst + w * SH::MAT + i * 1024);
+          }
+        }
+      }
+    };
+    constexpr std::integral_constant<int, 0> kKeysOnly{};
+    constexpr std::integral_constant<int, 1> kValuesOnly{};
+    constexpr std::integral_constant<int, 2> kBoth{};
+
+    float m[MT], l[MT], c[MT];
+    f32x4 acc[MT][DB];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      m[mt] = -INFINITY;
+      l[mt] = c[mt] = 0.0f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) acc[mt][db] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    // Scores of a tile and their weights.
+    uint32_t seen[MT];            // visible keys of the lane's query, where a tile masks any
+    auto scores = [&](int t, int slot, f32x4 (&s)[MT][2]) {
+      const int at = ring + slot * SH::STAGE + k_at;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+        s[mt][0] = s[mt][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          const s16x8 a = *(const LDS(s16x8)*)(lds + (at ^ (64 * kk)) + kb * SH::HALF);
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) s[mt][kb] = T::mfma(a, q[mt][kk], s[mt][kb]);
+        }
+    };
+    auto masked = [&](int t) { return t >= nct || (t + 1) * kKeys > R.len; };
+    auto weights = [&](int t, f32x4 (&s)[MT][2], s16x8 (&p)[MT]) {
+      if (masked(t)) {
+        const int hn = here(n), hg = here(g);
+        if (t < nct) {
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) seen[mt] = (1u << (R.len - t * kKeys)) - 1;
+        } else {
+          // walk the path down to this tile, then through it
+          const int lo = (R.tiles - 1 - t) * kKeys;
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            int y = walk[16 * mt + hn];
+            while (y >= lo + kKeys) y = par[y];
+            uint32_t w = 0;
+            while (y >= lo) {
+              w |= 1u << (y - lo);
+              y = par[y];
+            }
+            walk[16 * mt + hn] = static_cast<int16_t>(y);
+            seen[mt] = w;
+          }
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              s[mt][kb][r] = seen[mt] >> (4 * hg) >> (16 * kb + r) & 1 ? s[mt][kb][r] : -INFINITY;
+      }
+      float top[MT];
+      bool moves = false;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        top[mt] = max3(s[mt][0][0], s[mt][0][1], s[mt][0][2]);
+        top[mt] = max3(top[mt], s[mt][0][3], s[mt][1][0]);
+        top[mt] = max3(top[mt], s[mt][1][1], s[mt][1][2]);
+        top[mt] = __builtin_elementwise_maximum(top[mt], s[mt][1][3]);
+        moves |= top[mt] > m[mt] + P.slack;
+      }
+      if (__builtin_amdgcn_ballot_w64(moves)) {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          float u = fmaxf(m[mt], top[mt]);
+          u = fmaxf(u, __shfl_xor(u, 16, 64));
+          u = fmaxf(u, __shfl_xor(u, 32, 64));
+          const float f = to_frame(m[mt], u, P.k);
+          m[mt] = u;
+          c[mt] = frame(u, P.k);
+          l[mt] *= f;
+#pragma unroll
+          for (int db = 0; db < DB; ++db) acc[mt][db] *= f;
+        }
+      }
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            s[mt][kb][r] = __builtin_amdgcn_exp2f(fmaf(s[mt][kb][r], P.k, c[mt]));
+            l[mt] += s[mt][kb][r];
+          }
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          w[i] = T::pack(s[mt][i >> 1][2 * (i & 1)], s[mt][i >> 1][2 * (i & 1) + 1]);
+        p[mt] = __builtin_bit_cast(s16x8, w);
+      }
+    };
+    auto add_values = [&](int t, int slot, const s16x8 (&p)[MT]) {
+      const int mat = ring + slot * SH::STAGE + SH::MAT;
+      const int at = mat + v_at;
+      auto operand = [&](int db) {
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (LDS(s16x4)*)(lds + (at ^ (32 * db))));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (LDS(s16x4)*)(lds + (at ^ (32 * db)) + SH::HALF));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      };
+      if (t < nct) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const s16x8 a = operand(db);
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) acc[mt][db] = T::mfma(a, p[mt], acc[mt][db]);
+        }
+        return;
+      }
+      // Nodes that a row does not see may hold anything: their weight 0 times NaN or
+      // infinity must not reach the row. Such values enter the product as 0 and are
+      // then added to the rows that see them.
+      bool any = false;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        u32x4 a = __builtin_bit_cast(u32x4, operand(db));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bool lo = (a[i] & T::kExponent) == T::kExponent;
+          const bool hi = (a[i] >> 16 & T::kExponent) == T::kExponent;
+          any |= lo | hi;
+          a[i] = (lo ? 0 : a[i] & 0xffffu) | (hi ? 0 : a[i] & 0xffff0000u);
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+          acc[mt][db] = T::mfma(__builtin_bit_cast(s16x8, a), p[mt], acc[mt][db]);
+      }
+      if (!__builtin_amdgcn_ballot_w64(any)) return;
+      const int hg = here(g);
+#pragma unroll 1
+      for (int key = 0; key < kKeys; ++key) {
+        const int from = mat + key * SH::ROW + (hg & 1) * 8, f = swizzle(key & (kHalf - 1));
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const s16x4 v = *(const LDS(s16x4)*)(lds + from + ((2 * db + (hg >> 1)) ^ f) * 16);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint16_t u = static_cast<uint16_t>(v[e]);
+            const float add = (u & T::kExponent) == T::kExponent ? T::value(u) : 0.0f;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+              if (seen[mt] >> key & 1) acc[mt][db][e] += add;
+          }
+        }
+      }
+    };
+
+    const int mine = max(0, (t1 - t0 - kg + KW - 1) / KW);   // tiles of this key group
+    const int tile0 = t0 + kg;
+    if constexpr (SH::SPLIT) {
+      f32x4 s[MT][2];
+      s16x8 p[MT];
+      for (int i = -1; i < mine; ++i) {            // (round -1 loads tile 0)
+        const int t = tile0 + i * KW;
+        const bool more = i + 1 < mine;
+        if (more) fetch(t + KW);
+        if (i >= 0) {
+          wait_loads<SH::MINE>();                  // the values may be in flight
+          scores(t, 0, s);
+          wait_loads<SH::MINE>();                  // the keys are read
+        }
+        if (more) issue(t + KW, 0, kKeysOnly);
+        if (i >= 0) {
+          weights(t, s, p);
+          if (more)
+            wait_loads<SH::MINE>();
+          else
+            wait_loads<0>();
+          add_values(t, 0, p);
+          wait_loads<SH::MINE>();
+        }
+        if (more) issue(t + KW, 0, kValuesOnly);
+      }
+    } else {
+      const int rounds = (t1 - t0 + KW - 1) / KW;  // of the whole workgroup
+      int slot = 1, next = 0;                      // of tile i (round 0: slot 0), i + S - 1
+      if (mine > 0) fetch(tile0);
+      for (int i = 1 - SH::S; i < rounds; ++i) {   // (the first rounds only load)
+        const int t = tile0 + i * KW;
+        if (i >= 0) {
+          // tile i is there, for all wavefronts that share it, and they have read tile i - 1
+          if (i + SH::S - 2 < mine)
+            wait_loads<(SH::S - 2) * 2 * SH::MINE>();
+          else
+            wait_loads<0>();
+          if constexpr (RW > 1) barrier();
+        }
+        if (i + SH::S - 1 < mine) {
+          issue(t + (SH::S - 1) * KW, next, kBoth);
+          if (i + SH::S < mine) fetch(t + SH::S * KW);
+        }
+        if (i >= 0 && i < mine) {
+          f32x4 s[MT][2];
+          s16x8 p[MT];
+          scores(t, slot, s);
+          weights(t, s, p);
+          add_values(t, slot, p);
+        }
+        slot = slot + 1 == SH::S ? 0 : slot + 1;
+        next = next + 1 == SH::S ? 0 : next + 1;
+      }
+      wait_loads<0>();
+    }
+
+    // The key groups' parts, merged by group 0.
+    const int el = here(lane), en = el & 15, eg = el >> 4;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      l[mt] += __shfl_xor(l[mt], 16, 64);
+      l[mt] += __shfl_xor(l[mt], 32, 64);
+    }
+    barrier();                    // all have read their last tile
+    if (el == 0) flags[wave] = bad;
+    if (kg > 0) {
+      const int w = (kg - 1) * RW + rg;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+          *(LDS(f32x4)*)(lds + ((w * MT + mt) * DB + db) * 1024 + el * 16) = acc[mt][db];
+        *(LDS(f32x2)*)(lds + SH::ACC + (w * MT + mt) * 512 + el * 8) = f32x2{m[mt], l[mt]};
+      }
+    }
+    barrier();
+    bool any_bad = false;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) any_bad |= flags[w] != 0;
+    if (kg == 0) {
+      const bool whole = t0 == 0 && t1 == R.tiles;
+      const size_t part = (static_cast<size_t>(team) * 2 + (t0 > 0 ? 0 : 1)) * P.team + member;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        f32x2 o[KW];
+        float top = m[mt];
+#pragma unroll
+        for (int j = 1; j < KW; ++j) {
+          o[j] = *(const LDS(f32x2)*)(lds + SH::ACC + (((j - 1) * RW + rg) * MT + mt) * 512 + el * 8);
+          top = fmaxf(top, o[j][0]);
+        }
+        const float f = to_frame(m[mt], top, P.k);
+        m[mt] = top;
+        l[mt] *= f;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) acc[mt][db] *= f;
+#pragma unroll
+        for (int j = 1; j < KW; ++j) {
+          const float fj = to_frame(o[j][0], top, P.k);
+          l[mt] += o[j][1] * fj;
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+            acc[mt][db] += fj * *(const LDS(f32x4)*)(
+                lds + ((((j - 1) * RW + rg) * MT + mt) * DB + db) * 1024 + el * 16);
+        }
+        if (any_bad) {
+          m[mt] = 0.0f;
+          l[mt] = NAN;
+        }
+        const int r = rbase + 16 * mt + en;
+        if (!whole) {
+          float* const to = P.parts + part * SH::PART;
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+            *reinterpret_cast<f32x4*>(to + ((rg * MT + mt) * DB + db) * 256 + el * 4) = acc[mt][db];
+          if (eg == 0)
+            *reinterpret_cast<f32x2*>(to + SH::PART_ACC + ((rg * MT + mt) * 16 + en) * 2) =
+                f32x2{m[mt], l[mt]};
+        } else if (r < P.rows) {
+          const size_t row = out_row(P, b, kh, r);
+          if (P.prefix_pass) {
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+              *reinterpret_cast<f32x4*>(P.pre + row * SH::DP + 16 * db + 4 * eg) = acc[mt][db];
+            if (eg == 0) P.pre_ml[row] = f32x2{m[mt], l[mt]};
+          } else {
+            if (R.shared) Finish<T, SH>::absorb(P, row, eg, 0, DB, m[mt], l[mt], acc[mt]);
+            const float inv = 1.0f / l[mt];
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+              write_out<T, SH>(P, row, 16 * db + 4 * eg, acc[mt][db] * inv);
+          }
+        }
+      }
+    }
+  }
+}
+
+// Merges the parts of the item that team blockIdx.x's part cuts first: workgroup y
+// one block of 16 rows of the item's, a wavefront a quarter of the head.
+template <class T, class SH>
+__global__ void __launch_bounds__(kThreads) merge_kernel(Pass P) {
+  constexpr int DBW = SH::DB / kWaves;     // blocks of the head per wavefront
+  const int team = blockIdx.x;
+  const i32x4 d = P.desc[team];
+  const int count = d[3];
+  if (count == 0) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
+  const int member = blockIdx.y / (SH::RW * SH::MT), block = blockIdx.y % (SH::RW * SH::MT);
+  const int r = (d[2] * P.team + member) * SH::BM + 16 * block + n;
+  if (r - n >= P.rows) return;
+  // part i: the end of the team before, then the starts of this one and those behind
+  auto part = [&](int i) {
+    const size_t at = i == 0 ? (static_cast<size_t>(team - 1) * 2 + 1)
+                             : static_cast<size_t>(team + i - 1) * 2;
+    return P.parts + (at * P.team + member) * SH::PART;
+  };
+  float m = -INFINITY, l = 0.0f;
+  for (int i = 0; i < count; ++i)
+    m = fmaxf(m, part(i)[SH::PART_ACC + (block * 16 + n) * 2]);
+  f32x4 acc[DBW];
+  for (int k = 0; k < DBW; ++k) acc[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int i = 0; i < count; ++i) {
+    const float* const from = part(i);
+    const f32x2 ml = *reinterpret_cast<const f32x2*>(from + SH::PART_ACC + (block * 16 + n) * 2);
+    const float f = to_frame(ml[0], m, P.k);
+    l += ml[1] * f;
+#pragma unroll
+    for (int k = 0; k < DBW; ++k)
+      acc[k] += f * *reinterpret_cast<const f32x4*>(
+                        from + (block * SH::DB + wave * DBW + k) * 256 + lane * 4);
+  }
+  if (r >= P.rows) return;
+  const int b = d[0];
+  const size_t row = out_row(P, b, d[1], r);
+  const int db0 = wave * DBW;
+  if (P.prefix_pass) {
+    for (int k = 0; k < DBW; ++k)
+      *reinterpret_cast<f32x4*>(P.pre + row * SH::DP + 16 * (db0 + k) + 4 * g) = acc[k];
+    if (g == 0 && wave == 0) P.pre_ml[row] = f32x2{m, l};
+    return;
+  }
+  if (P.prefix_len > 0 && P.ctx_len[b] >= P.prefix_len)
+    Finish<T, SH>::absorb(P, row, g, db0, DBW, m, l, acc);
+  const float inv = 1.0f / l;
+  for (int k = 0; k < DBW; ++k) write_out<T, SH>(P, row, 16 * (db0 + k) + 4 * g, acc[k] * inv);
+}
+
+// Rows per workgroup for `rows` query rows: 16, 32 or 48 of one wavefront's width, or
+// two or four of 48, whichever pads less.
+int block_rows(int64_t rows) {
+  if (rows <= 16) return 16;
+  if (rows <= 32) return 32;
+  if (rows <= 48) return 48;
+  const int64_t two = (rows + 95) / 96 * 96, four = (rows + 191) / 192 * 192;
+  return four <= two ? 192 : 96;
+}
+
+struct Plan {
+  int rows_per_wg, team, chunks, teams;
+  size_t parts_bytes;
+};
+Plan plan(int64_t rows, int padded, int cus) {
+  Plan p{};
+  p.rows_per_wg = block_rows(rows);
+  const int64_t tiles = (rows + p.rows_per_wg - 1) / p.rows_per_wg;
+  p.chunks = static_cast<int>((tiles + kMaxTeam - 1) / kMaxTeam);
+  p.team = static_cast<int>((tiles + p.chunks - 1) / p.chunks);
+  const int per_xcd = cus / kXcds * kPerCu;
+  p.teams = per_xcd / p.team * kXcds;
+  p.parts_bytes = static_cast<size_t>(p.teams) * 2 * p.team *
+                  (static_cast<size_t>(p.rows_per_wg) * (padded + 2)) * sizeof(float);
+  return p;
+}
+
+struct Layout {
+  size_t desc, parts, pre, pre_ml, bytes;
+};
+Layout layout(int64_t batch, int num_nodes, int heads, int kv_heads, int head_dim, int prefix_len) {
+  const int padded = head_dim <= 64 ? 64 : 128;
+  const int64_t rows = static_cast<int64_t>(num_nodes) * (heads / kv_heads);
+  Layout L{};
+  L.desc = 0;
+  L.parts = tv::align256(kMaxCus * kPerCu * sizeof(i32x4));
+  size_t parts = plan(rows, padded, kMaxCus).parts_bytes;
+  if (prefix_len > 0) {
+    const size_t p = plan(rows * batch, padded, kMaxCus).parts_bytes;
+    parts = parts > p ? parts : p;
+  }
+  L.pre = tv::align256(L.parts + parts);
+  const size_t all = prefix_len > 0 ? static_cast<size_t>(batch) * num_nodes * heads : 0;
+  L.pre_ml = tv::align256(L.pre + all * padded * sizeof(float));
+  L.bytes = tv::align256(L.pre_ml + all * sizeof(f32x2));
+  return L;
+}
+
+// CUs of the current device, in whole XCDs and at most kMaxCus; 0 on failure.
+int device_cus() {
+  constexpr int kMaxDevices = 64;
+  static int cus[kMaxDevices];
+  static std::mutex mu;
+  int dev = 0, n = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0) return 0;
+  std::lock_guard<std::mutex> lock(mu);
+  if (dev < kMaxDevices && cus[dev]) return cus[dev];
+  if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return 0;
+  n = n > kMaxCus ? kMaxCus : n / kXcds * kXcds;
+  // (fewer: the teams of an XCD still need room for the largest one)
+  if (n < kMaxTeam / kPerCu * kXcds) n = kMaxTeam / kPerCu * kXcds;
+  if (dev < kMaxDevices) cus[dev] = n;
+  return n;
+}
+
+template <class T, class SH>
+hipError_t run(const Pass& P, hipStream_t stream) {
+  const unsigned wgs = static_cast<unsigned>(P.teams * P.team);
+  // whole rounds over the XCDs: every XCD has teams / 8 teams
+  hipLaunchKernelGGL((attention_kernel<T, SH>), dim3(wgs), dim3(kThreads), 0, stream, P);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((merge_kernel<T, SH>),
+                     dim3(static_cast<unsigned>(P.teams), static_cast<unsigned>(P.team * SH::RW * SH::MT)),
+                     dim3(kThreads), 0, stream, P);
+  return hipGetLastError();
+}
+
+template <class T, int DP>
+hipError_t run_rows(const Pass& P, int rows_per_wg, hipStream_t stream) {
+  switch (rows_per_wg) {
+    case 16: return run<T, Shape<DP, 1, 1>>(P, stream);
+    case 32: return run<T, Shape<DP, 2, 1>>(P, stream);
+    case 48: return run<T, Shape<DP, 3, 1>>(P, stream);
+    case 96: return run<T, Shape<DP, 3, 2>>(P, stream);
+    default: return run<T, Shape<DP, 3, 4>>(P, stream);
+  }
+}
+
+hipError_t run_pass(Pass P, int dtype, int cus, hipStream_t stream) {
+  const int padded = P.head_dim <= 64 ? 64 : 128;
+  const Plan p = plan(P.rows, padded, cus);
+  P.team = p.team;
+  P.chunks = p.chunks;
+  P.teams = p.teams;
+  if (dtype == TV_DTYPE_BF16)
+    return padded == 64 ? run_rows<Bf16, 64>(P, p.rows_per_wg, stream)
+                        : run_rows<Bf16, 128>(P, p.rows_per_wg, stream);
+  return padded == 64 ? run_rows<F16, 64>(P, p.rows_per_wg, stream)
+                      : run_rows<F16, 128>(P, p.rows_per_wg, stream);
 }
 
 }  // namespace
@@ -107,28 +946,59 @@ namespace tv {
 
 size_t attention_workspace(int32_t batch, int32_t num_nodes, int32_t heads, int32_t kv_heads,
                            int32_t head_dim, int32_t prefix_len) {
-  return 256;
+  return layout(batch, num_nodes, heads, kv_heads, head_dim, prefix_len).bytes;
 }
 
 int launch_attention(const AttentionArgs& a, void* workspace, hipStream_t stream) {
-  for (int b0 = 0; b0 < a.batch; b0 += 32768) {
-    AttentionArgs c = a;
-    c.batch = a.batch - b0 < 32768 ? a.batch - b0 : 32768;
-    const size_t rows = static_cast<size_t>(b0) * a.num_nodes;
-    c.parents = a.parents ? a.parents + rows : nullptr;
-    c.q = static_cast<const uint16_t*>(a.q) + rows * a.q_stride;
-    c.k_new = static_cast<const uint16_t*>(a.k_new) + rows * a.kv_stride;
-    c.v_new = static_cast<const uint16_t*>(a.v_new) + rows * a.kv_stride;
-    c.block_table = a.block_table + static_cast<size_t>(b0) * a.table_width;
-    c.ctx_len = a.ctx_len + b0;
-    c.out = static_cast<uint16_t*>(a.out) + rows * a.heads * a.head_dim;
-    const dim3 grid(a.heads, a.num_nodes, c.batch);
-    if (a.dtype == TV_DTYPE_BF16)
-      hipLaunchKernelGGL((attention_kernel<__bf16>), grid, dim3(kThreads), 0, stream, c);
-    else
-      hipLaunchKernelGGL((attention_kernel<_Float16>), grid, dim3(kThreads), 0, stream, c);
+  const int cus = device_cus();
+  if (!cus) return TV_ERR_HIP;
+  const Layout L = layout(a.batch, a.num_nodes, a.heads, a.kv_heads, a.head_dim, a.prefix_len);
+  uint8_t* const ws = static_cast<uint8_t*>(workspace);
+  Pass P{};
+  P.q = static_cast<const uint16_t*>(a.q);
+  P.k_new = static_cast<const uint16_t*>(a.k_new);
+  P.v_new = static_cast<const uint16_t*>(a.v_new);
+  P.k_cache = static_cast<const uint16_t*>(a.k_cache);
+  P.v_cache = static_cast<const uint16_t*>(a.v_cache);
+  P.parents = a.num_nodes > 1 ? a.parents : nullptr;
+  P.table = a.block_table;
+  P.ctx_len = a.ctx_len;
+  P.out = static_cast<uint16_t*>(a.out);
+  P.q_stride = a.q_stride;
+  P.kv_stride = a.kv_stride;
+  P.page_stride = a.page_stride;
+  P.num_pages = a.num_pages;
+  P.page_shift = 31 - __builtin_clz(static_cast<unsigned>(a.page_size));
+  P.table_width = a.table_width;
+  P.batch = a.batch;
+  P.num_nodes = a.num_nodes;
+  P.heads = a.heads;
+  P.kv_heads = a.kv_heads;
+  P.head_dim = a.head_dim;
+  P.group = a.heads / a.kv_heads;
+  P.rows = a.num_nodes * P.group;
+  // (without pages a tree that has a context has bad ones, the prefix among them)
+  P.prefix_len = a.num_pages > 0 ? a.prefix_len : 0;
+  P.k = static_cast<float>(static_cast<double>(a.scale) * 1.4426950408889634);
+  const double slack = 8.0 / static_cast<double>(P.k);
+  P.slack = slack < 3.0e38 ? static_cast<float>(slack) : 3.0e38f;
+  P.desc = reinterpret_cast<i32x4*>(ws + L.desc);
+  P.parts = reinterpret_cast<float*>(ws + L.parts);
+  P.pre = reinterpret_cast<float*>(ws + L.pre);
+  P.pre_ml = reinterpret_cast<f32x2*>(ws + L.pre_ml);
+  if (P.prefix_len > 0) {
+    Pass X = P;
+    X.prefix_pass = true;
+    X.table = a.prefix_pages;
+    X.table_width = 0;
+    X.ctx_len = nullptr;
+    X.parents = nullptr;
+    X.batch = 1;
+    X.num_nodes = a.batch * a.num_nodes;
+    X.rows = a.batch * P.rows;
+    if (run_pass(X, a.dtype, cus, stream) != hipSuccess) return TV_ERR_HIP;
   }
-  return hipGetLastError() == hipSuccess ? TV_OK : TV_ERR_HIP;
+  return run_pass(P, a.dtype, cus, stream) == hipSuccess ? TV_OK : TV_ERR_HIP;
 }
 
 }  // namespace tv

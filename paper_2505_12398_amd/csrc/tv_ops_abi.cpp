@@ -18,7 +18,7 @@ bool page_size_ok(int32_t page_size) {
          (page_size & (page_size - 1)) == 0;
 }
 
-constexpr int64_t kMaxBytes = int64_t{1} << 30;   // of a tree's nodes, and of a page
+constexpr int64_t kMaxBytes = int64_t{1} << 29;   // of a tree's nodes, and of a page
 
 // TV_OK if an attention call of these sizes is taken
 int attention_sizes(int32_t batch, int32_t num_nodes, int32_t heads, int32_t kv_heads,
@@ -27,7 +27,8 @@ int attention_sizes(int32_t batch, int32_t num_nodes, int32_t heads, int32_t kv_
     return TV_ERR_INVALID_ARG;
   if (heads % kv_heads) return TV_ERR_INVALID_ARG;
   if (batch > TV_MAX_BATCH || num_nodes > TV_MAX_NODES || head_dim > TV_MAX_HEAD_DIM ||
-      head_dim % 8 || static_cast<int64_t>(heads) * head_dim > TV_MAX_HIDDEN)
+      head_dim % 8 || static_cast<int64_t>(heads) * head_dim > TV_MAX_HIDDEN ||
+      static_cast<int64_t>(batch) * num_nodes * heads > INT32_MAX)
     return TV_ERR_UNSUPPORTED;
   return TV_OK;
 }
