@@ -144,7 +144,7 @@ struct Shape {
   static constexpr int BYTES = SCAN + 8 * (kWaves + 2) + 16;
   // floats of a part in the workspace
   static constexpr int PART_ACC = RW * MT * DB * 256;
-  static constexpr int PART = PART_ACC + BM * 2;
+  static constexpr int PART = PART_ACC + BM * 2 + 4;   // the last: values that are not finite
   static_assert(BYTES <= 160 * 1024 / kPerCu, "two workgroups on a CU");
   static_assert((S - 1) * 2 * MINE < 64, "the count of loads in flight");
 };
@@ -243,24 +243,6 @@ __device__ __forceinline__ long long cut(long long total, int t, int parts) {
   return each * t + (total - each * parts) * t / parts;
 }
 
-// Rows of one block of 16: adds what is kept elsewhere, and writes the result.
-template <class T, class SH>
-struct Finish {
-  // The prefix' part of row `row` (of all trees' query rows), into the running (m, l, acc).
-  static __device__ __forceinline__ void absorb(const Pass& P, size_t at, int g, int db0, int ndb,
-                                                float& m, float& l, f32x4* acc) {
-    const f32x2 ml = P.pre_ml[at];
-    const float top = fmaxf(m, ml[0]);
-    const float a = to_frame(m, top, P.k), b = to_frame(ml[0], top, P.k);
-    m = top;
-    l = l * a + ml[1] * b;
-    for (int i = 0; i < ndb; ++i) {
-      const f32x4 o = *reinterpret_cast<const f32x4*>(P.pre + at * SH::DP + 16 * (db0 + i) + 4 * g);
-      for (int r = 0; r < 4; ++r) acc[i][r] = acc[i][r] * a + o[r] * b;
-    }
-  }
-};
-
 // Output index of row r of an item: (node of the pass, head).
 __device__ __forceinline__ size_t out_row(const Pass& P, int b, int kh, int r) {
   const int node = r / P.group, g = r - node * P.group;
@@ -272,6 +254,31 @@ __device__ __forceinline__ void write_out(const Pass& P, size_t row, int d, cons
   if (d >= P.head_dim) return;
   *reinterpret_cast<u32x2*>(P.out + row * P.head_dim + d) =
       u32x2{T::pack(o[0], o[1]), T::pack(o[2], o[3])};
+}
+
+// Adds to elements d .. d + 3 of an output what of the values of its row's path is not
+// finite (written by this lane before, from sums without them).
+template <class T, class SH>
+__device__ void add_odd(const Pass& P, int b, int kh, int r, size_t row, int d) {
+  if (d >= P.head_dim) return;
+  float add[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  const int64_t tree = static_cast<int64_t>(b) * P.num_nodes;
+  for (int x = r / P.group; x >= 0;) {
+    const u32x2 v = *reinterpret_cast<const u32x2*>(P.v_new + (tree + x) * P.kv_stride +
+                                                    kh * P.head_dim + d);
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t u = v[e >> 1] >> (16 * (e & 1)) & 0xffffu;
+      if ((u & T::kExponent) == T::kExponent) add[e] += T::value(static_cast<uint16_t>(u));
+    }
+    const int p = P.parents && x > 0 ? P.parents[tree + x] : -1;
+    x = p < x ? p : -1;
+  }
+  u32x2* const at = reinterpret_cast<u32x2*>(P.out + row * P.head_dim + d);
+  const u32x2 o = *at;
+  float s[4];
+  for (int e = 0; e < 4; ++e)
+    s[e] = T::value(static_cast<uint16_t>(o[e >> 1] >> (16 * (e & 1)))) + add[e];
+  *at = u32x2{T::pack(s[0], s[1]), T::pack(s[2], s[3])};
 }
 
 template <class T, class SH>
@@ -431,7 +438,8 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
     // Loads of tile t: this wavefront's part of its keys (0) and values (1).
     CONSTANT(int)* const pages =
         (CONSTANT(int)*)(P.table + static_cast<size_t>(b) * P.table_width);
-    bool bad = R.bad;
+    bool bad = R.bad;             // a page that is none
+    bool odd = false;             // a node's value that is not finite
     auto first_key = [&](int t, int h) { return R.from + t * kKeys + h * kHalf; };
     auto page_of = [&](int t, int h) {
       return t < nct ? pages[min(first_key(t, h), R.from + R.len - 1) >> P.page_shift] : 0;
@@ -496,17 +504,16 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
     constexpr std::integral_constant<int, 2> kBoth{};
 
     float m[MT], l[MT], c[MT];
-    f32x4 acc[MT][DB];
+    f32x4 acc[DB][MT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       m[mt] = -INFINITY;
       l[mt] = c[mt] = 0.0f;
 #pragma unroll
-      for (int db = 0; db < DB; ++db) acc[mt][db] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int db = 0; db < DB; ++db) acc[db][mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
     // Scores of a tile and their weights.
-    uint32_t seen[MT];            // visible keys of the lane's query, where a tile masks any
     auto scores = [&](int t, int slot, f32x4 (&s)[MT][2]) {
       const int at = ring + slot * SH::STAGE + k_at;
 #pragma unroll
@@ -525,32 +532,29 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
     auto weights = [&](int t, f32x4 (&s)[MT][2], s16x8 (&p)[MT]) {
       if (masked(t)) {
         const int hn = here(n), hg = here(g);
-        if (t < nct) {
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) seen[mt] = (1u << (R.len - t * kKeys)) - 1;
-        } else {
-          // walk the path down to this tile, then through it
-          const int lo = (R.tiles - 1 - t) * kKeys;
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
+        for (int mt = 0; mt < MT; ++mt) {
+          uint32_t w = 0;
+          if (t < nct) {
+            w = (1u << (R.len - t * kKeys)) - 1;
+          } else {
+            // walk the path down to this tile, then through it
+            const int lo = (R.tiles - 1 - t) * kKeys;
             int y = walk[16 * mt + hn];
             while (y >= lo + kKeys) y = par[y];
-            uint32_t w = 0;
             while (y >= lo) {
               w |= 1u << (y - lo);
               y = par[y];
             }
             walk[16 * mt + hn] = static_cast<int16_t>(y);
-            seen[mt] = w;
           }
-        }
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+          w >>= 4 * hg;
 #pragma unroll
           for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-              s[mt][kb][r] = seen[mt] >> (4 * hg) >> (16 * kb + r) & 1 ? s[mt][kb][r] : -INFINITY;
+              s[mt][kb][r] = w >> (16 * kb + r) & 1 ? s[mt][kb][r] : -INFINITY;
+        }
       }
       float top[MT];
       bool moves = false;
@@ -563,7 +567,7 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
         moves |= top[mt] > m[mt] + P.slack;
       }
       if (__builtin_amdgcn_ballot_w64(moves)) {
-#pragma unroll
+    #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
           float u = fmaxf(m[mt], top[mt]);
           u = fmaxf(u, __shfl_xor(u, 16, 64));
@@ -573,9 +577,9 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
           c[mt] = frame(u, P.k);
           l[mt] *= f;
 #pragma unroll
-          for (int db = 0; db < DB; ++db) acc[mt][db] *= f;
+          for (int db = 0; db < DB; ++db) acc[db][mt] *= f;
         }
-      }
+          }
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
@@ -594,58 +598,35 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
     };
     auto add_values = [&](int t, int slot, const s16x8 (&p)[MT]) {
       const int mat = ring + slot * SH::STAGE + SH::MAT;
+      // Nodes that a row does not see may hold anything: their weight 0 times NaN or
+      // infinity must not reach the row. Such values enter the product as 0 and are
+      // added to the rows that see them once these are written.
+      if (t >= nct) {
+        const int hl = here(lane);
+        bool some = false;
+#pragma unroll 1
+        for (int i = hl; i < SH::MAT / 4; i += 64) {
+          LDS(uint32_t)* const at = (LDS(uint32_t)*)(lds + mat + 4 * i);
+          const uint32_t w = *at;
+          const bool lo = (w & T::kExponent) == T::kExponent;
+          const bool hi = (w >> 16 & T::kExponent) == T::kExponent;
+          if (lo || hi) {
+            *at = (lo ? 0 : w & 0xffffu) | (hi ? 0 : w & 0xffff0000u);
+            some = true;
+          }
+        }
+        odd |= __builtin_amdgcn_ballot_w64(some) != 0;
+      }
       const int at = mat + v_at;
-      auto operand = [&](int db) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
             (LDS(s16x4)*)(lds + (at ^ (32 * db))));
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
             (LDS(s16x4)*)(lds + (at ^ (32 * db)) + SH::HALF));
-        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      };
-      if (t < nct) {
+        const s16x8 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          const s16x8 a = operand(db);
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt) acc[mt][db] = T::mfma(a, p[mt], acc[mt][db]);
-        }
-        return;
-      }
-      // Nodes that a row does not see may hold anything: their weight 0 times NaN or
-      // infinity must not reach the row. Such values enter the product as 0 and are
-      // then added to the rows that see them.
-      bool any = false;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        u32x4 a = __builtin_bit_cast(u32x4, operand(db));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const bool lo = (a[i] & T::kExponent) == T::kExponent;
-          const bool hi = (a[i] >> 16 & T::kExponent) == T::kExponent;
-          any |= lo | hi;
-          a[i] = (lo ? 0 : a[i] & 0xffffu) | (hi ? 0 : a[i] & 0xffff0000u);
-        }
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-          acc[mt][db] = T::mfma(__builtin_bit_cast(s16x8, a), p[mt], acc[mt][db]);
-      }
-      if (!__builtin_amdgcn_ballot_w64(any)) return;
-      const int hg = here(g);
-#pragma unroll 1
-      for (int key = 0; key < kKeys; ++key) {
-        const int from = mat + key * SH::ROW + (hg & 1) * 8, f = swizzle(key & (kHalf - 1));
-#pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          const s16x4 v = *(const LDS(s16x4)*)(lds + from + ((2 * db + (hg >> 1)) ^ f) * 16);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint16_t u = static_cast<uint16_t>(v[e]);
-            const float add = (u & T::kExponent) == T::kExponent ? T::value(u) : 0.0f;
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-              if (seen[mt] >> key & 1) acc[mt][db][e] += add;
-          }
-        }
+        for (int mt = 0; mt < MT; ++mt) acc[db][mt] = T::mfma(a, p[mt], acc[db][mt]);
       }
     };
 
@@ -714,21 +695,21 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
       l[mt] += __shfl_xor(l[mt], 32, 64);
     }
     barrier();                    // all have read their last tile
-    if (el == 0) flags[wave] = bad;
+    if (el == 0) flags[wave] = bad | odd << 1;
     if (kg > 0) {
       const int w = (kg - 1) * RW + rg;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
         for (int db = 0; db < DB; ++db)
-          *(LDS(f32x4)*)(lds + ((w * MT + mt) * DB + db) * 1024 + el * 16) = acc[mt][db];
+          *(LDS(f32x4)*)(lds + ((w * MT + mt) * DB + db) * 1024 + el * 16) = acc[db][mt];
         *(LDS(f32x2)*)(lds + SH::ACC + (w * MT + mt) * 512 + el * 8) = f32x2{m[mt], l[mt]};
       }
     }
     barrier();
-    bool any_bad = false;
+    int any = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) any_bad |= flags[w] != 0;
+    for (int w = 0; w < kWaves; ++w) any |= flags[w];
     if (kg == 0) {
       const bool whole = t0 == 0 && t1 == R.tiles;
       const size_t part = (static_cast<size_t>(team) * 2 + (t0 > 0 ? 0 : 1)) * P.team + member;
@@ -745,17 +726,19 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
         m[mt] = top;
         l[mt] *= f;
 #pragma unroll
-        for (int db = 0; db < DB; ++db) acc[mt][db] *= f;
+        for (int db = 0; db < DB; ++db) acc[db][mt] *= f;
 #pragma unroll
         for (int j = 1; j < KW; ++j) {
           const float fj = to_frame(o[j][0], top, P.k);
           l[mt] += o[j][1] * fj;
 #pragma unroll
-          for (int db = 0; db < DB; ++db)
-            acc[mt][db] += fj * *(const LDS(f32x4)*)(
+          for (int db = 0; db < DB; ++db) {
+            acc[db][mt] += fj * *(const LDS(f32x4)*)(
                 lds + ((((j - 1) * RW + rg) * MT + mt) * DB + db) * 1024 + el * 16);
+            if (db % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+          }
         }
-        if (any_bad) {
+        if (any & 1) {
           m[mt] = 0.0f;
           l[mt] = NAN;
         }
@@ -764,23 +747,39 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
           float* const to = P.parts + part * SH::PART;
 #pragma unroll
           for (int db = 0; db < DB; ++db)
-            *reinterpret_cast<f32x4*>(to + ((rg * MT + mt) * DB + db) * 256 + el * 4) = acc[mt][db];
+            *reinterpret_cast<f32x4*>(to + ((rg * MT + mt) * DB + db) * 256 + el * 4) = acc[db][mt];
           if (eg == 0)
             *reinterpret_cast<f32x2*>(to + SH::PART_ACC + ((rg * MT + mt) * 16 + en) * 2) =
                 f32x2{m[mt], l[mt]};
+          if (mt == 0 && rg == 0 && el == 0) to[SH::PART - 1] = any & 2 ? 1.0f : 0.0f;
         } else if (r < P.rows) {
           const size_t row = out_row(P, b, kh, r);
           if (P.prefix_pass) {
 #pragma unroll
             for (int db = 0; db < DB; ++db)
-              *reinterpret_cast<f32x4*>(P.pre + row * SH::DP + 16 * db + 4 * eg) = acc[mt][db];
+              *reinterpret_cast<f32x4*>(P.pre + row * SH::DP + 16 * db + 4 * eg) = acc[db][mt];
             if (eg == 0) P.pre_ml[row] = f32x2{m[mt], l[mt]};
           } else {
-            if (R.shared) Finish<T, SH>::absorb(P, row, eg, 0, DB, m[mt], l[mt], acc[mt]);
-            const float inv = 1.0f / l[mt];
+            float a = 1.0f, c2 = 0.0f;
+            f32x2 ml = {0.0f, 0.0f};
+            if (R.shared) {
+              ml = P.pre_ml[row];
+              const float both = fmaxf(m[mt], ml[0]);
+              a = to_frame(m[mt], both, P.k);
+              c2 = to_frame(ml[0], both, P.k);
+            }
+            const float inv = 1.0f / (l[mt] * a + ml[1] * c2);
 #pragma unroll
-            for (int db = 0; db < DB; ++db)
-              write_out<T, SH>(P, row, 16 * db + 4 * eg, acc[mt][db] * inv);
+            for (int db = 0; db < DB; ++db) {
+              f32x4 o = acc[db][mt] * a;
+              if (R.shared)
+                o += c2 * *reinterpret_cast<const f32x4*>(P.pre + row * SH::DP + 16 * db + 4 * eg);
+              write_out<T, SH>(P, row, 16 * db + 4 * eg, o * inv);
+            }
+            if (any & 2) {
+#pragma unroll 1
+              for (int db = 0; db < DB; ++db) add_odd<T, SH>(P, b, kh, r, row, 16 * db + 4 * eg);
+            }
           }
         }
       }
@@ -832,10 +831,21 @@ __global__ void __launch_bounds__(kThreads) merge_kernel(Pass P) {
     if (g == 0 && wave == 0) P.pre_ml[row] = f32x2{m, l};
     return;
   }
-  if (P.prefix_len > 0 && P.ctx_len[b] >= P.prefix_len)
-    Finish<T, SH>::absorb(P, row, g, db0, DBW, m, l, acc);
-  const float inv = 1.0f / l;
-  for (int k = 0; k < DBW; ++k) write_out<T, SH>(P, row, 16 * (db0 + k) + 4 * g, acc[k] * inv);
+  f32x2 ml = {-INFINITY, 0.0f};
+  const bool shared = P.prefix_len > 0 && P.ctx_len[b] >= P.prefix_len;
+  if (shared) ml = P.pre_ml[row];
+  const float both = fmaxf(m, ml[0]);
+  const float own = to_frame(m, both, P.k), pre = to_frame(ml[0], both, P.k);
+  const float inv = 1.0f / (l * own + ml[1] * pre);
+  bool odd = false;
+  for (int i = 0; i < count; ++i) odd |= part(i)[SH::PART - 1] != 0.0f;
+  for (int k = 0; k < DBW; ++k) {
+    const int at = 16 * (db0 + k) + 4 * g;
+    f32x4 o = acc[k] * own;
+    if (shared) o += pre * *reinterpret_cast<const f32x4*>(P.pre + row * SH::DP + at);
+    write_out<T, SH>(P, row, at, o * inv);
+    if (odd) add_odd<T, SH>(P, b, d[1], r, row, at);
+  }
 }
 
 // Rows per workgroup for `rows` query rows: 16, 32 or 48 of one wavefront's width, or
@@ -861,7 +871,7 @@ Plan plan(int64_t rows, int padded, int cus) {
   const int per_xcd = cus / kXcds * kPerCu;
   p.teams = per_xcd / p.team * kXcds;
   p.parts_bytes = static_cast<size_t>(p.teams) * 2 * p.team *
-                  (static_cast<size_t>(p.rows_per_wg) * (padded + 2)) * sizeof(float);
+                  (static_cast<size_t>(p.rows_per_wg) * (padded + 2) + 4) * sizeof(float);
   return p;
 }
 
