@@ -55,6 +55,8 @@ typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((ext_vector_type(8))) short s16x8;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((address_space(3))) uint8_t lds_byte;
@@ -68,8 +70,7 @@ struct Bf16 {
                                                    __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   }
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {   // to nearest even
-    return uint32_t{__builtin_bit_cast(uint16_t, static_cast<__bf16>(lo))} |
-           uint32_t{__builtin_bit_cast(uint16_t, static_cast<__bf16>(hi))} << 16;
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
   }
   static __device__ __forceinline__ float value(uint16_t x) { return __uint_as_float(uint32_t{x} << 16); }
   static constexpr uint32_t kExponent = 0x7f80;
@@ -80,8 +81,7 @@ struct F16 {
                                                   __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
   }
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
-    return uint32_t{__builtin_bit_cast(uint16_t, static_cast<_Float16>(lo))} |
-           uint32_t{__builtin_bit_cast(uint16_t, static_cast<_Float16>(hi))} << 16;
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, f16x2));
   }
   static __device__ __forceinline__ float value(uint16_t x) {
     return static_cast<float>(__builtin_bit_cast(_Float16, x));
@@ -149,16 +149,32 @@ struct Shape {
   static_assert((S - 1) * 2 * MINE < 64, "the count of loads in flight");
 };
 
+constexpr int kMfma = 0x008, kDsRead = 0x100;   // kinds of instructions to the scheduler
 constexpr int kPastRange = 0x40000000, kRange = 0x3fffffff;
 
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-// 64 lanes' 16 bytes from the buffer at byte offset voff into LDS at dst + 16 lane;
-// zeros for an offset past the range. (In assembly, so that the compiler does not
-// wait for it at the next LDS read: the waits are written out below.)
-__device__ __forceinline__ void load_to_lds(const i32x4& rs, int voff, int dst) {
-  asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-               :: "s"(dst), "v"(voff), "s"(rs) : "memory", "m0");
+// N loads of 64 lanes' 16 bytes from the buffer at byte offsets voff into LDS, load i
+// at dst + 1024 i + 16 lane; zeros for an offset past the range. (In assembly, so that
+// the compiler does not wait for them at the next LDS read: the waits are written out
+// below. The hazard recogniser does not look into it: the five wait states between a
+// scalar that the vector unit wrote and a load, and the one behind m0, are here.)
+template <int N>
+__device__ __forceinline__ void load_to_lds(const i32x4& rs, const int (&voff)[N], int dst) {
+  if constexpr (N == 1)
+    asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :: "s"(dst), "v"(voff[0]), "s"(rs) : "memory", "m0");
+  else if constexpr (N == 2)
+    asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %3, 0 offen lds\n\t"
+                 "s_add_u32 m0, %0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds"
+                 :: "s"(dst), "v"(voff[0]), "v"(voff[1]), "s"(rs) : "memory", "m0", "scc");
+  else
+    asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %5, 0 offen lds\n\t"
+                 "s_add_u32 m0, %0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %5, 0 offen lds\n\t"
+                 "s_add_u32 m0, %0, 0x800\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %5, 0 offen lds\n\t"
+                 "s_add_u32 m0, %0, 0xc00\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %5, 0 offen lds"
+                 :: "s"(dst), "v"(voff[0]), "v"(voff[1]), "v"(voff[2]), "v"(voff[3]), "s"(rs)
+                 : "memory", "m0", "scc");
 }
 #pragma clang diagnostic pop
 // All but the newest N loads have landed, and this wavefront's LDS reads are done.
@@ -361,9 +377,12 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
     return 8 * c < P.head_dim ? min(r, last) * stride + 16 * c : kPastRange;
   };
   const int dbytes = P.head_dim * 2;
-  int kv_off[SH::LOADS];
+  // this wavefront's halves of a tile, and its loads of a half
+  constexpr int kHalves = RW == 1 ? 2 : 1, kIn = RW == 4 ? SH::LOADS / 2 : SH::LOADS;
+  const int h0 = RW == 4 ? rg >> 1 : RW == 2 ? rg : 0, in0 = RW == 4 ? (rg & 1) * kIn : 0;
+  int kv_off[kIn];
 #pragma unroll
-  for (int i = 0; i < SH::LOADS; ++i) kv_off[i] = offset(lane, i, kHalf - 1, dbytes);
+  for (int i = 0; i < kIn; ++i) kv_off[i] = offset(lane, in0 + i, kHalf - 1, dbytes);
   // Reads: keys, row n of a block and chunk 4 kk + g; values, four keys 4 g .. 4 g + 3
   // by sixteen of the head, lane n's eight bytes at key n / 4, transposed by the read.
   const int k_at = n * SH::ROW + (g ^ swizzle(n)) * 16;
@@ -440,63 +459,74 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
         (CONSTANT(int)*)(P.table + static_cast<size_t>(b) * P.table_width);
     bool bad = R.bad;             // a page that is none
     bool odd = false;             // a node's value that is not finite
-    auto first_key = [&](int t, int h) { return R.from + t * kKeys + h * kHalf; };
-    auto page_of = [&](int t, int h) {
-      return t < nct ? pages[min(first_key(t, h), R.from + R.len - 1) >> P.page_shift] : 0;
+    const int ring = kg * SH::S * SH::STAGE;
+    const int in_page = (1 << P.page_shift) - 1, nfull = R.len / kKeys;
+    const int64_t of_head = (static_cast<int64_t>(kh) << P.page_shift) * P.head_dim;
+    const uint64_t k_base = reinterpret_cast<uint64_t>(P.k_cache + of_head);
+    const uint64_t v_base = reinterpret_cast<uint64_t>(P.v_cache + of_head);
+    const int64_t page_bytes = 2 * P.page_stride;
+    auto resource = [](uint64_t a) {
+      return i32x4{static_cast<int>(a), static_cast<int>(a >> 32) & 0xffff, kRange, 0x00020000};
     };
-    constexpr int kHalves = RW == 1 ? 2 : 1;        // halves this wavefront loads
-    const int h0 = RW == 4 ? rg >> 1 : RW == 2 ? rg : 0;
-    int page[kHalves];
+    auto first_key = [&](int t, int h) { return R.from + t * kKeys + h * kHalf; };
+    int page[kHalves];            // of the tile to load next
     auto fetch = [&](int t) {
 #pragma unroll
-      for (int h = 0; h < kHalves; ++h) page[h] = page_of(t, h0 + h);
+      for (int hh = 0; hh < kHalves; ++hh)
+        if (t < nct)
+          page[hh] = pages[min(first_key(t, h0 + hh), R.from + R.len - 1) >> P.page_shift];
     };
-    const int ring = kg * SH::S * SH::STAGE;
-    const int in_page = (1 << P.page_shift) - 1;
     auto issue = [&](int t, int slot, auto what) {
       constexpr int w0 = what.value == 2 ? 0 : what.value, w1 = what.value == 2 ? 2 : w0 + 1;
-      constexpr int in = RW == 4 ? SH::LOADS / 2 : SH::LOADS;
-      const int odd = RW == 4 ? rg & 1 : 0;         // which loads of the half
+      const int to = lds0 + ring + slot * SH::STAGE + h0 * SH::HALF + in0 * 1024;
+      if (t < nfull) {
 #pragma unroll
-      for (int hh = 0; hh < kHalves; ++hh) {
-        const int h = h0 + hh;
-        const int dst = lds0 + ring + slot * SH::STAGE + h * SH::HALF + odd * in * 1024;
-        int64_t base;
-        int last, stride = dbytes;
-        if (t < nct) {
-          const int key = min(first_key(t, h), R.from + R.len - 1);
-          last = R.from + R.len - key - 1;          // rows past the context: its last one again
+        for (int hh = 0; hh < kHalves; ++hh) {
           int pg = page[hh];
-          if (pg < 0 || pg >= P.num_pages) {
+          if (static_cast<unsigned>(pg) >= static_cast<unsigned>(P.num_pages)) {
             bad = true;
             pg = 0;
           }
-          base = pg * P.page_stride +
-                 ((static_cast<int64_t>(kh) << P.page_shift) + (key & in_page)) * P.head_dim;
+          const int64_t at = pg * page_bytes + (first_key(t, h0 + hh) & in_page) * dbytes;
+#pragma unroll
+          for (int w = w0; w < w1; ++w)
+            load_to_lds<kIn>(resource((w ? v_base : k_base) + at), kv_off,
+                             to + hh * SH::HALF + w * SH::MAT);
+        }
+        return;
+      }
+      const int ln = here(lane);
+#pragma unroll
+      for (int hh = 0; hh < kHalves; ++hh) {
+        uint64_t k_at, v_at;
+        int last, stride = dbytes;
+        if (t < nct) {
+          const int key = min(first_key(t, h0 + hh), R.from + R.len - 1);
+          last = R.from + R.len - key - 1;          // rows past the context: its last one again
+          int pg = page[hh];
+          if (static_cast<unsigned>(pg) >= static_cast<unsigned>(P.num_pages)) {
+            bad = true;
+            pg = 0;
+          }
+          const int64_t at = pg * page_bytes + (key & in_page) * dbytes;
+          k_at = k_base + at;
+          v_at = v_base + at;
         } else {                                    // nodes, the last ones first
-          const int from = min((R.tiles - 1 - t) * kKeys + h * kHalf, P.num_nodes - 1);
+          const int from = min((R.tiles - 1 - t) * kKeys + (h0 + hh) * kHalf, P.num_nodes - 1);
           last = P.num_nodes - 1 - from;
           stride = static_cast<int>(P.kv_stride) * 2;
-          base = (static_cast<int64_t>(b) * P.num_nodes + from) * P.kv_stride + kh * P.head_dim;
+          const int64_t at =
+              (static_cast<int64_t>(b) * P.num_nodes + from) * P.kv_stride + kh * P.head_dim;
+          k_at = reinterpret_cast<uint64_t>(P.k_new + at);
+          v_at = reinterpret_cast<uint64_t>(P.v_new + at);
         }
 #pragma unroll
-        for (int w = w0; w < w1; ++w) {
-          const uint64_t a = reinterpret_cast<uint64_t>(
-              (t < nct ? w ? P.v_cache : P.k_cache : w ? P.v_new : P.k_new) + base);
-          const i32x4 rs = {static_cast<int>(a), static_cast<int>(a >> 32) & 0xffff, kRange,
-                            0x00020000};
-          if (t < nct && last >= kHalf - 1) {
-#pragma unroll
-            for (int i = 0; i < in; ++i)
-              load_to_lds(rs, odd ? kv_off[SH::LOADS - in + i] : kv_off[i],
-                          dst + w * SH::MAT + i * 1024);
-          } else {
-            const int ln = here(lane);
+        for (int w = w0; w < w1; ++w)
 #pragma unroll 1
-            for (int i = 0; i < in; ++i)
-              load_to_lds(rs, offset(ln, odd * in + i, last, stride), dst + w * SH::MAT + i * 1024);
+          for (int i = 0; i < kIn; ++i) {
+            const int voff[1] = {offset(ln, in0 + i, last, stride)};
+            load_to_lds<1>(resource(w ? v_at : k_at), voff, to + hh * SH::HALF + w * SH::MAT + i * 1024);
           }
-        }
       }
     };
     constexpr std::integral_constant<int, 0> kKeysOnly{};
@@ -527,6 +557,13 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt) s[mt][kb] = T::mfma(a, q[mt][kk], s[mt][kb]);
         }
+      // three reads ahead of the products
+      __builtin_amdgcn_sched_group_barrier(kDsRead, 3, 0);
+      unrolled<2 * KK - 3>([](auto) {
+        __builtin_amdgcn_sched_group_barrier(kMfma, MT, 0);
+        __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+      });
+      __builtin_amdgcn_sched_group_barrier(kMfma, 3 * MT, 0);
     };
     auto masked = [&](int t) { return t >= nct || (t + 1) * kKeys > R.len; };
     auto weights = [&](int t, f32x4 (&s)[MT][2], s16x8 (&p)[MT]) {
@@ -628,6 +665,12 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) acc[db][mt] = T::mfma(a, p[mt], acc[db][mt]);
       }
+      __builtin_amdgcn_sched_group_barrier(kDsRead, 4, 1);
+      unrolled<DB - 2>([](auto) {
+        __builtin_amdgcn_sched_group_barrier(kMfma, MT, 1);
+        __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 1);
+      });
+      __builtin_amdgcn_sched_group_barrier(kMfma, 2 * MT, 1);
     };
 
     const int mine = max(0, (t1 - t0 - kg + KW - 1) / KW);   // tiles of this key group
