@@ -149,7 +149,6 @@ struct Shape {
   static_assert((S - 1) * 2 * MINE < 64, "the count of loads in flight");
 };
 
-constexpr int kMfma = 0x008, kDsRead = 0x100;   // kinds of instructions to the scheduler
 constexpr int kPastRange = 0x40000000, kRange = 0x3fffffff;
 
 #pragma clang diagnostic push
@@ -452,6 +451,12 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
         par[i] = static_cast<int16_t>(p >= 0 && p < i ? p : -1);
       }
     }
+    // The queries are there: left to the compiler, their wait would be at the first
+    // product of every tile, and one for all loads in flight.
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(q[mt][kk]));
     barrier();                    // the links are there (and the last item's merge is done)
 
     // Loads of tile t: this wavefront's part of its keys (0) and values (1).
@@ -549,21 +554,22 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
         s[mt][0] = s[mt][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      // operand i: chunk group i / 2 of block i % 2, read three ahead of its products
+      constexpr int kAhead = 3, kOps = 2 * KK;
+      s16x8 a[kAhead + 1];
+      auto read = [&](auto i) {
+        a[i.value % (kAhead + 1)] =
+            *(const LDS(s16x8)*)(lds + (at ^ (64 * (i.value / 2))) + i.value % 2 * SH::HALF);
+      };
+      unrolled<kAhead>(read);
+      unrolled<kOps>([&](auto ic) {
+        constexpr int i = ic.value, kb = i % 2, kk = i / 2;
+        if constexpr (i + kAhead < kOps) read(std::integral_constant<int, i + kAhead>{});
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk)
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-          const s16x8 a = *(const LDS(s16x8)*)(lds + (at ^ (64 * kk)) + kb * SH::HALF);
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt) s[mt][kb] = T::mfma(a, q[mt][kk], s[mt][kb]);
-        }
-      // three reads ahead of the products
-      __builtin_amdgcn_sched_group_barrier(kDsRead, 3, 0);
-      unrolled<2 * KK - 3>([](auto) {
-        __builtin_amdgcn_sched_group_barrier(kMfma, MT, 0);
-        __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+        for (int mt = 0; mt < MT; ++mt)
+          s[mt][kb] = T::mfma(a[i % (kAhead + 1)], q[mt][kk], s[mt][kb]);
+        __builtin_amdgcn_sched_barrier(0);
       });
-      __builtin_amdgcn_sched_group_barrier(kMfma, 3 * MT, 0);
     };
     auto masked = [&](int t) { return t >= nct || (t + 1) * kKeys > R.len; };
     auto weights = [&](int t, f32x4 (&s)[MT][2], s16x8 (&p)[MT]) {
@@ -655,22 +661,24 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
         odd |= __builtin_amdgcn_ballot_w64(some) != 0;
       }
       const int at = mat + v_at;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
+      constexpr int kAhead = 2;
+      s16x8 a[kAhead + 1];
+      auto read = [&](auto db) {
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (LDS(s16x4)*)(lds + (at ^ (32 * db))));
+            (LDS(s16x4)*)(lds + (at ^ (32 * db.value))));
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (LDS(s16x4)*)(lds + (at ^ (32 * db)) + SH::HALF));
-        const s16x8 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            (LDS(s16x4)*)(lds + (at ^ (32 * db.value)) + SH::HALF));
+        a[db.value % (kAhead + 1)] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      };
+      unrolled<kAhead>(read);
+      unrolled<DB>([&](auto dbc) {
+        constexpr int db = dbc.value;
+        if constexpr (db + kAhead < DB) read(std::integral_constant<int, db + kAhead>{});
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) acc[db][mt] = T::mfma(a, p[mt], acc[db][mt]);
-      }
-      __builtin_amdgcn_sched_group_barrier(kDsRead, 4, 1);
-      unrolled<DB - 2>([](auto) {
-        __builtin_amdgcn_sched_group_barrier(kMfma, MT, 1);
-        __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 1);
+        for (int mt = 0; mt < MT; ++mt)
+          acc[db][mt] = T::mfma(a[db % (kAhead + 1)], p[mt], acc[db][mt]);
+        __builtin_amdgcn_sched_barrier(0);
       });
-      __builtin_amdgcn_sched_group_barrier(kMfma, 2 * MT, 1);
     };
 
     const int mine = max(0, (t1 - t0 - kg + KW - 1) / KW);   // tiles of this key group
@@ -678,10 +686,10 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
     if constexpr (SH::SPLIT) {
       f32x4 s[MT][2];
       s16x8 p[MT];
+      if (mine > 0) fetch(tile0);
       for (int i = -1; i < mine; ++i) {            // (round -1 loads tile 0)
         const int t = tile0 + i * KW;
         const bool more = i + 1 < mine;
-        if (more) fetch(t + KW);
         if (i >= 0) {
           wait_loads<SH::MINE>();                  // the values may be in flight
           scores(t, 0, s);
@@ -698,6 +706,7 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
           wait_loads<SH::MINE>();
         }
         if (more) issue(t + KW, 0, kValuesOnly);
+        if (i + 2 < mine) fetch(t + 2 * KW);
       }
     } else {
       const int rounds = (t1 - t0 + KW - 1) / KW;  // of the whole workgroup
@@ -715,12 +724,14 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
         }
         if (i + SH::S - 1 < mine) {
           issue(t + (SH::S - 1) * KW, next, kBoth);
-          if (i + SH::S < mine) fetch(t + SH::S * KW);
+          if (i < 0 && i + SH::S < mine) fetch(t + SH::S * KW);
         }
         if (i >= 0 && i < mine) {
           f32x4 s[MT][2];
           s16x8 p[MT];
           scores(t, slot, s);
+          // (a page's number comes with the LDS reads' counter: not before those of the keys)
+          if (i + SH::S < mine) fetch(t + SH::S * KW);
           weights(t, s, p);
           add_values(t, slot, p);
         }
