@@ -47,6 +47,7 @@ constexpr int kXcds = 8, kMaxCus = 256;
 constexpr int kPerCu = 2;                 // workgroups on a CU
 constexpr int kMaxTeam = 32;              // workgroups of a team: the CUs of an XCD
 constexpr int kMinTiles = 8;              // of a part
+constexpr int kWordNodes = 256;
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
@@ -128,17 +129,22 @@ struct Shape {
   static constexpr int MAT = 2 * HALF, STAGE = 2 * MAT;
   // loads of a wavefront per tile, of keys (or values)
   static constexpr int MINE = 2 * LOADS / RW;
-  // One wavefront per key group and a wide head leave room for one tile: its keys are
-  // refilled after the first product and its values after the second.
-  static constexpr bool SPLIT = RW == 1 && DP == 128;
-  static constexpr int S = SPLIT ? 1 : DP == 128 ? RW : RW == 1 ? 2 : 4;
+  // tiles in LDS per key group
+  static constexpr int S = DP == 128 ? RW : RW == 1 ? 2 : 4;
+  // Loads younger than those a round waits for, in units of MINE (see the tiles' loop)
+  static constexpr int YOUNGER = 2 * (S - 1) + (RW == 1 ? 1 : 0);
   static constexpr int RING = KW * S * STAGE;
   // accumulators and (maximum, sum) of the other key groups
   static constexpr int ACC = (KW - 1) * RW * MT * DB * 1024;
   static constexpr int MERGE = ACC + (KW - 1) * RW * MT * 64 * 8;
   static constexpr int MAIN = RING > MERGE ? RING : MERGE;
+  // Trees of up to kWordNodes nodes: a word per node of the row tile and 32 nodes says
+  // which of these are on its path, and the links are needed only to find them.
   static constexpr int PARENTS = MAIN;            // int16 per node
-  static constexpr int WALK = PARENTS + 2 * TV_MAX_NODES;
+  static constexpr int WORDS = PARENTS + 2 * kWordNodes;
+  static constexpr int WORDS_END = WORDS + BM * (kWordNodes / 8);
+  static constexpr int PARENTS_END = PARENTS + 2 * TV_MAX_NODES;
+  static constexpr int WALK = WORDS_END > PARENTS_END ? WORDS_END : PARENTS_END;
   static constexpr int FLAGS = WALK + 2 * kWaves * 16 * MT;
   static constexpr int SCAN = FLAGS + 4 * kWaves;
   static constexpr int BYTES = SCAN + 8 * (kWaves + 2) + 16;
@@ -146,7 +152,7 @@ struct Shape {
   static constexpr int PART_ACC = RW * MT * DB * 256;
   static constexpr int PART = PART_ACC + BM * 2 + 4;   // the last: values that are not finite
   static_assert(BYTES <= 160 * 1024 / kPerCu, "two workgroups on a CU");
-  static_assert((S - 1) * 2 * MINE < 64, "the count of loads in flight");
+  static_assert(YOUNGER * MINE < 64, "the count of loads in flight");
 };
 
 constexpr int kPastRange = 0x40000000, kRange = 0x3fffffff;
@@ -181,6 +187,7 @@ template <int N>
 __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(N) : "memory");
 }
+__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
@@ -388,6 +395,7 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
   const int vrow = 4 * g + (n >> 2);
   const int v_at = vrow * SH::ROW + (((n & 3) >> 1) ^ swizzle(vrow)) * 16 + (n & 1) * 8;
   LDS(int16_t)* const par = (LDS(int16_t)*)(lds + SH::PARENTS);
+  LDS(uint32_t)* const word = (LDS(uint32_t)*)(lds + SH::WORDS);
   LDS(int)* const flags = (LDS(int)*)(lds + SH::FLAGS);
   // the next node on the path of each of this wavefront's rows
   LDS(int16_t)* const walk = (LDS(int16_t)*)(lds + SH::WALK) + wave * 16 * MT;
@@ -427,6 +435,7 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
     if (r0 >= P.rows) continue;   // (for the whole workgroup)
     const int nct = (R.len + kKeys - 1) / kKeys;
 
+    barrier();                    // the last item's merge is done
     // queries
     const int rbase = r0 + rg * 16 * MT;
     s16x8 q[MT][KK];
@@ -444,20 +453,40 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
         q[mt][kk] = d < P.head_dim ? *reinterpret_cast<const s16x8*>(src + d) : s16x8{};
       }
     }
-    if (t1 > nct && !P.prefix_pass) {
-      for (int i = tid; i < P.num_nodes; i += kThreads) {
-        const int p = P.parents && i > 0
-                          ? P.parents[static_cast<size_t>(b) * P.num_nodes + i] : -1;
-        par[i] = static_cast<int16_t>(p >= 0 && p < i ? p : -1);
+    // What the first tile needs besides: its queries, and which nodes the rows see.
+    const bool words = P.num_nodes <= kWordNodes;
+    const int node0 = r0 / P.group;                        // the row tile's first node
+    auto prepare = [&] {
+      const bool nodes = t1 > nct && !P.prefix_pass;
+      if (nodes) {
+        for (int i = tid; i < P.num_nodes; i += kThreads) {
+          const int p = P.parents && i > 0
+                            ? P.parents[static_cast<size_t>(b) * P.num_nodes + i] : -1;
+          par[i] = static_cast<int16_t>(p >= 0 && p < i ? p : -1);
+        }
       }
-    }
-    // The queries are there: left to the compiler, their wait would be at the first
-    // product of every tile, and one for all loads in flight.
+      // (left to the compiler, the queries' wait would be at the first product of every
+      // tile, and one for all loads in flight)
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+      for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(q[mt][kk]));
-    barrier();                    // the links are there (and the last item's merge is done)
+        for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(q[mt][kk]));
+      if (!nodes) return;
+      barrier();
+      if (words) {
+        const int last = (min(r0 + SH::BM, P.rows) - 1) / P.group;
+        for (int i = tid; i <= last - node0; i += kThreads) {
+          int y = node0 + i;
+#pragma unroll 1
+          for (int w = (P.num_nodes - 1) / kKeys; w >= 0; --w) {
+            uint32_t on = 0;
+            for (; y >= w * kKeys; y = par[y]) on |= 1u << (y - w * kKeys);
+            word[i * (kWordNodes / kKeys) + w] = on;
+          }
+        }
+        barrier();
+      }
+    };
 
     // Loads of tile t: this wavefront's part of its keys (0) and values (1).
     CONSTANT(int)* const pages =
@@ -536,7 +565,6 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
     };
     constexpr std::integral_constant<int, 0> kKeysOnly{};
     constexpr std::integral_constant<int, 1> kValuesOnly{};
-    constexpr std::integral_constant<int, 2> kBoth{};
 
     float m[MT], l[MT], c[MT];
     f32x4 acc[DB][MT];
@@ -581,15 +609,15 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
           if (t < nct) {
             w = (1u << (R.len - t * kKeys)) - 1;
           } else {
-            // walk the path down to this tile, then through it
-            const int lo = (R.tiles - 1 - t) * kKeys;
+            const int tile = R.tiles - 1 - t, lo = tile * kKeys;
             int y = walk[16 * mt + hn];
-            while (y >= lo + kKeys) y = par[y];
-            while (y >= lo) {
-              w |= 1u << (y - lo);
-              y = par[y];
+            if (words) {
+              w = word[(y - node0) * (kWordNodes / kKeys) + tile];
+            } else {              // walk the path down to this tile, then through it
+              while (y >= lo + kKeys) y = par[y];
+              for (; y >= lo; y = par[y]) w |= 1u << (y - lo);
+              walk[16 * mt + hn] = static_cast<int16_t>(y);
             }
-            walk[16 * mt + hn] = static_cast<int16_t>(y);
           }
           w >>= 4 * hg;
 #pragma unroll
@@ -645,17 +673,24 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
       // infinity must not reach the row. Such values enter the product as 0 and are
       // added to the rows that see them once these are written.
       if (t >= nct) {
+        // (a half word's exponent of ones, plus one, carries into its sign's place)
+        constexpr uint32_t kExp = T::kExponent * 0x10001u, kOne = (0x8000u - T::kExponent) * 0x10001u;
         const int hl = here(lane);
-        bool some = false;
+        uint32_t ones = 0;
+#pragma unroll 2
+        for (int i = 0; i < SH::MAT / 1024; ++i) {
+          const u32x4 w = *(const LDS(u32x4)*)(lds + mat + 1024 * i + 16 * hl);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) ones |= (w[j] & kExp) + kOne;
+        }
+        const bool some = ones & 0x80008000u;
+        if (__builtin_amdgcn_ballot_w64(some)) {
 #pragma unroll 1
-        for (int i = hl; i < SH::MAT / 4; i += 64) {
-          LDS(uint32_t)* const at = (LDS(uint32_t)*)(lds + mat + 4 * i);
-          const uint32_t w = *at;
-          const bool lo = (w & T::kExponent) == T::kExponent;
-          const bool hi = (w >> 16 & T::kExponent) == T::kExponent;
-          if (lo || hi) {
-            *at = (lo ? 0 : w & 0xffffu) | (hi ? 0 : w & 0xffff0000u);
-            some = true;
+          for (int i = hl; i < SH::MAT / 4; i += 64) {
+            LDS(uint32_t)* const at = (LDS(uint32_t)*)(lds + mat + 4 * i);
+            const uint32_t w = *at;
+            *at = ((w & T::kExponent) == T::kExponent ? 0 : w & 0xffffu) |
+                  ((w >> 16 & T::kExponent) == T::kExponent ? 0 : w & 0xffff0000u);
           }
         }
         odd |= __builtin_amdgcn_ballot_w64(some) != 0;
@@ -683,62 +718,67 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
 
     const int mine = max(0, (t1 - t0 - kg + KW - 1) / KW);   // tiles of this key group
     const int tile0 = t0 + kg;
-    if constexpr (SH::SPLIT) {
+    // Round i multiplies tile i. Its keys' place is free after the first product and its
+    // values' after the second, once all wavefronts that share them are there, and is
+    // refilled at once with those of tile i + S: loads are issued in the order K_0, V_0,
+    // K_1, ..., V_{i-1+S} at the top of round i and K_{i+S} in its middle (a wavefront
+    // that shares with none issues before it waits, the others after the barrier). All
+    // but the YOUNGER newest have landed when tile i's are there; near the end, where
+    // fewer were issued, all have.
+    const int rounds = (t1 - t0 + KW - 1) / KW;              // of the whole workgroup
+    constexpr int kSteady = SH::YOUNGER * SH::MINE;
+#pragma unroll 1
+    for (int j = 0; j < SH::S && j < mine; ++j) {
+      fetch(tile0 + j * KW);
+      issue(tile0 + j * KW, j, kKeysOnly);
+      if (j < SH::S - 1) issue(tile0 + j * KW, j, kValuesOnly);
+    }
+    prepare();
+    int slot = 0, before = SH::S - 1;                        // of tiles i and i - 1
+#pragma unroll 1
+    for (int i = 0; i < rounds; ++i) {
+      const int t = tile0 + i * KW;
+      auto load_v = [&] {
+        if (i + SH::S - 1 >= mine) return;
+        issue(t + (SH::S - 1) * KW, before, kValuesOnly);
+        if (i + SH::S < mine) fetch(t + SH::S * KW);
+      };
+      auto load_k = [&] {
+        if (i + SH::S < mine) issue(t + SH::S * KW, slot, kKeysOnly);
+      };
       f32x4 s[MT][2];
       s16x8 p[MT];
-      if (mine > 0) fetch(tile0);
-      for (int i = -1; i < mine; ++i) {            // (round -1 loads tile 0)
-        const int t = tile0 + i * KW;
-        const bool more = i + 1 < mine;
-        if (i >= 0) {
-          wait_loads<SH::MINE>();                  // the values may be in flight
-          scores(t, 0, s);
-          wait_loads<SH::MINE>();                  // the keys are read
-        }
-        if (more) issue(t + KW, 0, kKeysOnly);
-        if (i >= 0) {
-          weights(t, s, p);
-          if (more)
-            wait_loads<SH::MINE>();
-          else
-            wait_loads<0>();
-          add_values(t, 0, p);
-          wait_loads<SH::MINE>();
-        }
-        if (more) issue(t + KW, 0, kValuesOnly);
-        if (i + 2 < mine) fetch(t + 2 * KW);
+      if constexpr (RW == 1) {
+        wait_reads();
+        load_v();
       }
-    } else {
-      const int rounds = (t1 - t0 + KW - 1) / KW;  // of the whole workgroup
-      int slot = 1, next = 0;                      // of tile i (round 0: slot 0), i + S - 1
-      if (mine > 0) fetch(tile0);
-      for (int i = 1 - SH::S; i < rounds; ++i) {   // (the first rounds only load)
-        const int t = tile0 + i * KW;
-        if (i >= 0) {
-          // tile i is there, for all wavefronts that share it, and they have read tile i - 1
-          if (i + SH::S - 2 < mine)
-            wait_loads<(SH::S - 2) * 2 * SH::MINE>();
-          else
-            wait_loads<0>();
-          if constexpr (RW > 1) barrier();
-        }
-        if (i + SH::S - 1 < mine) {
-          issue(t + (SH::S - 1) * KW, next, kBoth);
-          if (i < 0 && i + SH::S < mine) fetch(t + SH::S * KW);
-        }
-        if (i >= 0 && i < mine) {
-          f32x4 s[MT][2];
-          s16x8 p[MT];
-          scores(t, slot, s);
-          // (a page's number comes with the LDS reads' counter: not before those of the keys)
-          if (i + SH::S < mine) fetch(t + SH::S * KW);
-          weights(t, s, p);
-          add_values(t, slot, p);
-        }
-        slot = slot + 1 == SH::S ? 0 : slot + 1;
-        next = next + 1 == SH::S ? 0 : next + 1;
+      if (i + SH::S - 1 < mine)
+        wait_loads<kSteady>();
+      else
+        wait_loads<0>();
+      if constexpr (RW > 1) {
+        barrier();
+        load_v();
       }
-      wait_loads<0>();
+      scores(t, slot, s);         // (of a tile that is none, behind this group's last: unused)
+      if constexpr (RW == 1) {
+        wait_reads();
+        load_k();
+      }
+      if (i + SH::S - (RW > 1 ? 1 : 0) < mine)
+        wait_loads<kSteady>();
+      else
+        wait_loads<0>();
+      if constexpr (RW > 1) {
+        barrier();
+        load_k();
+      }
+      if (i < mine) {
+        weights(t, s, p);
+        add_values(t, slot, p);
+      }
+      before = slot;
+      slot = slot + 1 == SH::S ? 0 : slot + 1;
     }
 
     // The key groups' parts, merged by group 0.
