@@ -41,10 +41,10 @@
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4;
+constexpr int kMergeWaves = 4;
 constexpr int kKeys = 32, kHalf = 16;     // keys of a tile and of a half
 constexpr int kXcds = 8, kMaxCus = 256;
-constexpr int kPerCu = 2;                 // workgroups on a CU
+constexpr int kWavesPerCu = 8;            // resident wavefronts, two on a SIMD
 constexpr int kMaxTeam = 32;              // workgroups of a team: the CUs of an XCD
 constexpr int kMinTiles = 8;              // of a part
 constexpr int kWordNodes = 256;
@@ -117,9 +117,10 @@ struct Pass {
   f32x2* pre_ml;                // their (maximum, sum)
 };
 
-template <int DP_, int MT_, int RW_>
+template <int DP_, int MT_, int RW_, int KW_>
 struct Shape {
-  static constexpr int DP = DP_, MT = MT_, RW = RW_, KW = kWaves / RW;
+  static constexpr int DP = DP_, MT = MT_, RW = RW_, KW = KW_;
+  static constexpr int WAVES = RW * KW, THREADS = 64 * WAVES, PER_CU = kWavesPerCu / WAVES;
   static constexpr int BM = 16 * MT * RW;         // rows of a workgroup
   static constexpr int CH = DP / 8;               // 16-byte chunks of a row
   static constexpr int DB = DP / 16;              // 16-wide blocks of the head
@@ -145,13 +146,13 @@ struct Shape {
   static constexpr int WORDS_END = WORDS + BM * (kWordNodes / 8);
   static constexpr int PARENTS_END = PARENTS + 2 * TV_MAX_NODES;
   static constexpr int WALK = WORDS_END > PARENTS_END ? WORDS_END : PARENTS_END;
-  static constexpr int FLAGS = WALK + 2 * kWaves * 16 * MT;
-  static constexpr int SCAN = FLAGS + 4 * kWaves;
-  static constexpr int BYTES = SCAN + 8 * (kWaves + 2) + 16;
+  static constexpr int FLAGS = WALK + 2 * WAVES * 16 * MT;
+  static constexpr int SCAN = FLAGS + 4 * WAVES;
+  static constexpr int BYTES = SCAN + 8 * (WAVES + 2) + 16;
   // floats of a part in the workspace
   static constexpr int PART_ACC = RW * MT * DB * 256;
   static constexpr int PART = PART_ACC + BM * 2 + 4;   // the last: values that are not finite
-  static_assert(BYTES <= 160 * 1024 / kPerCu, "two workgroups on a CU");
+  static_assert(BYTES <= 160 * 1024 / PER_CU, "that many workgroups on a CU");
   static_assert(YOUNGER * MINE < 64, "the count of loads in flight");
 };
 
@@ -304,7 +305,7 @@ __device__ void add_odd(const Pass& P, int b, int kh, int r, size_t row, int d) 
 }
 
 template <class T, class SH>
-__global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
+__global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
   constexpr int MT = SH::MT, RW = SH::RW, KW = SH::KW, DB = SH::DB, KK = SH::DP / 32;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[SH::BYTES];
   lds_byte* const lds = (lds_byte*)smem;
@@ -323,9 +324,9 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
 
   // The line of tiles: how long, and where this team's part begins.
   LDS(long long)* const scan = (LDS(long long)*)(lds + SH::SCAN);
-  LDS(int)* const found = (LDS(int)*)(scan + kWaves + 2);
+  LDS(int)* const found = (LDS(int)*)(scan + SH::WAVES + 2);
   const long long per_tile = static_cast<long long>(P.kv_heads) * P.chunks;
-  const int per = (P.batch + kThreads - 1) / kThreads;
+  const int per = (P.batch + SH::THREADS - 1) / SH::THREADS;
   const int b_lo = min(tid * per, P.batch), b_hi = min(b_lo + per, P.batch);
   long long own = 0;
   for (int b = b_lo; b < b_hi; ++b)
@@ -340,7 +341,7 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
   barrier();
   long long total = 0;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
+  for (int w = 0; w < SH::WAVES; ++w) {
     if (w < wave) upto += scan[w];
     total += scan[w];
   }
@@ -359,7 +360,7 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
     for (int b = b_lo; b < b_hi; ++b) {
       const long long t = reach(P, P.prefix_pass ? 0 : P.ctx_len[b]).tiles * per_tile;
       if (begin < at + t) {
-        scan[kWaves] = begin - at;
+        scan[SH::WAVES] = begin - at;
         found[0] = b;
         break;
       }
@@ -368,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
   }
   barrier();
   int b = uniform(found[0]);
-  long long in_tree = uniform(scan[kWaves]);
+  long long in_tree = uniform(scan[SH::WAVES]);
 
   // Loads: instruction i of a half fills 1024 bytes, this lane the chunk at position
   // lane % CH of row i * 1024 / ROW + lane / CH. Swizzle: sixteen rows' reads of one
@@ -401,6 +402,7 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
   LDS(int16_t)* const walk = (LDS(int16_t)*)(lds + SH::WALK) + wave * 16 * MT;
 
   bool opened = false;
+  int word_tree = -1, word_chunk = -1;   // whose words are there
   for (long long pos = begin; pos < end;) {
     // the item at pos
     const int ctx = context(P, b);
@@ -457,9 +459,9 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
     const bool words = P.num_nodes <= kWordNodes;
     const int node0 = r0 / P.group;                        // the row tile's first node
     auto prepare = [&] {
-      const bool nodes = t1 > nct && !P.prefix_pass;
+      const bool nodes = t1 > nct && !P.prefix_pass && !(words && b == word_tree && chunk == word_chunk);
       if (nodes) {
-        for (int i = tid; i < P.num_nodes; i += kThreads) {
+        for (int i = tid; i < P.num_nodes; i += SH::THREADS) {
           const int p = P.parents && i > 0
                             ? P.parents[static_cast<size_t>(b) * P.num_nodes + i] : -1;
           par[i] = static_cast<int16_t>(p >= 0 && p < i ? p : -1);
@@ -474,8 +476,10 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
       if (!nodes) return;
       barrier();
       if (words) {
+        word_tree = b;
+        word_chunk = chunk;
         const int last = (min(r0 + SH::BM, P.rows) - 1) / P.group;
-        for (int i = tid; i <= last - node0; i += kThreads) {
+        for (int i = tid; i <= last - node0; i += SH::THREADS) {
           int y = node0 + i;
 #pragma unroll 1
           for (int w = (P.num_nodes - 1) / kKeys; w >= 0; --w) {
@@ -803,7 +807,7 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
     barrier();
     int any = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) any |= flags[w];
+    for (int w = 0; w < SH::WAVES; ++w) any |= flags[w];
     if (kg == 0) {
       const bool whole = t0 == 0 && t1 == R.tiles;
       const size_t part = (static_cast<size_t>(team) * 2 + (t0 > 0 ? 0 : 1)) * P.team + member;
@@ -884,8 +888,8 @@ __global__ void __launch_bounds__(kThreads, kPerCu) attention_kernel(Pass P) {
 // Merges the parts of the item that team blockIdx.x's part cuts first: workgroup y
 // one block of 16 rows of the item's, a wavefront a quarter of the head.
 template <class T, class SH>
-__global__ void __launch_bounds__(kThreads) merge_kernel(Pass P) {
-  constexpr int DBW = SH::DB / kWaves;     // blocks of the head per wavefront
+__global__ void __launch_bounds__(64 * kMergeWaves) merge_kernel(Pass P) {
+  constexpr int DBW = SH::DB / kMergeWaves;     // blocks of the head per wavefront
   const int team = blockIdx.x;
   const i32x4 d = P.desc[team];
   const int count = d[3];
@@ -962,7 +966,7 @@ Plan plan(int64_t rows, int padded, int cus) {
   const int64_t tiles = (rows + p.rows_per_wg - 1) / p.rows_per_wg;
   p.chunks = static_cast<int>((tiles + kMaxTeam - 1) / kMaxTeam);
   p.team = static_cast<int>((tiles + p.chunks - 1) / p.chunks);
-  const int per_xcd = cus / kXcds * kPerCu;
+  const int per_xcd = cus / kXcds * (p.rows_per_wg == 96 ? 4 : 2);   // workgroups resident
   p.teams = per_xcd / p.team * kXcds;
   p.parts_bytes = static_cast<size_t>(p.teams) * 2 * p.team *
                   (static_cast<size_t>(p.rows_per_wg) * (padded + 2) + 4) * sizeof(float);
@@ -977,7 +981,7 @@ Layout layout(int64_t batch, int num_nodes, int heads, int kv_heads, int head_di
   const int64_t rows = static_cast<int64_t>(num_nodes) * (heads / kv_heads);
   Layout L{};
   L.desc = 0;
-  L.parts = tv::align256(kMaxCus * kPerCu * sizeof(i32x4));
+  L.parts = tv::align256(kMaxCus * kWavesPerCu * sizeof(i32x4));
   size_t parts = plan(rows, padded, kMaxCus).parts_bytes;
   if (prefix_len > 0) {
     const size_t p = plan(rows * batch, padded, kMaxCus).parts_bytes;
@@ -1002,7 +1006,7 @@ int device_cus() {
   if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return 0;
   n = n > kMaxCus ? kMaxCus : n / kXcds * kXcds;
   // (fewer: the teams of an XCD still need room for the largest one)
-  if (n < kMaxTeam / kPerCu * kXcds) n = kMaxTeam / kPerCu * kXcds;
+  if (n < kMaxTeam / 2 * kXcds) n = kMaxTeam / 2 * kXcds;
   if (dev < kMaxDevices) cus[dev] = n;
   return n;
 }
@@ -1011,23 +1015,23 @@ template <class T, class SH>
 hipError_t run(const Pass& P, hipStream_t stream) {
   const unsigned wgs = static_cast<unsigned>(P.teams * P.team);
   // whole rounds over the XCDs: every XCD has teams / 8 teams
-  hipLaunchKernelGGL((attention_kernel<T, SH>), dim3(wgs), dim3(kThreads), 0, stream, P);
+  hipLaunchKernelGGL((attention_kernel<T, SH>), dim3(wgs), dim3(SH::THREADS), 0, stream, P);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((merge_kernel<T, SH>),
                      dim3(static_cast<unsigned>(P.teams), static_cast<unsigned>(P.team * SH::RW * SH::MT)),
-                     dim3(kThreads), 0, stream, P);
+                     dim3(64 * kMergeWaves), 0, stream, P);
   return hipGetLastError();
 }
 
 template <class T, int DP>
 hipError_t run_rows(const Pass& P, int rows_per_wg, hipStream_t stream) {
   switch (rows_per_wg) {
-    case 16: return run<T, Shape<DP, 1, 1>>(P, stream);
-    case 32: return run<T, Shape<DP, 2, 1>>(P, stream);
-    case 48: return run<T, Shape<DP, 3, 1>>(P, stream);
-    case 96: return run<T, Shape<DP, 3, 2>>(P, stream);
-    default: return run<T, Shape<DP, 3, 4>>(P, stream);
+    case 16: return run<T, Shape<DP, 1, 1, 4>>(P, stream);
+    case 32: return run<T, Shape<DP, 2, 1, 4>>(P, stream);
+    case 48: return run<T, Shape<DP, 3, 1, 4>>(P, stream);
+    case 96: return run<T, Shape<DP, 3, 2, 1>>(P, stream);
+    default: return run<T, Shape<DP, 3, 4, 1>>(P, stream);
   }
 }
 
