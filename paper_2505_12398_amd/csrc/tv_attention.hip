@@ -586,8 +586,8 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
         s[mt][0] = s[mt][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      // operand i: chunk group i / 2 of block i % 2, read three ahead of its products
-      constexpr int kAhead = 3, kOps = 2 * KK;
+      // operand i: chunk group i / 2 of block i % 2; all reads before the first product
+      constexpr int kOps = 2 * KK, kAhead = kOps - 1;
       s16x8 a[kAhead + 1];
       auto read = [&](auto i) {
         a[i.value % (kAhead + 1)] =
@@ -671,7 +671,16 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
         p[mt] = __builtin_bit_cast(s16x8, w);
       }
     };
-    auto add_values = [&](int t, int slot, const s16x8 (&p)[MT]) {
+    // Values: the first kAhead operands are read before the weights are formed.
+    constexpr int kAhead = DB / 2;
+    auto read_values = [&](int slot, auto dbc, s16x8 (&a)[kAhead + 1]) {
+      constexpr int db = dbc.value;
+      const int at = (ring + slot * SH::STAGE + SH::MAT + v_at) ^ (32 * db);
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS(s16x4)*)(lds + at));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS(s16x4)*)(lds + at + SH::HALF));
+      a[db % (kAhead + 1)] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    auto first_values = [&](int t, int slot, s16x8 (&a)[kAhead + 1]) {
       const int mat = ring + slot * SH::STAGE + SH::MAT;
       // Nodes that a row does not see may hold anything: their weight 0 times NaN or
       // infinity must not reach the row. Such values enter the product as 0 and are
@@ -699,20 +708,12 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
         }
         odd |= __builtin_amdgcn_ballot_w64(some) != 0;
       }
-      const int at = mat + v_at;
-      constexpr int kAhead = 2;
-      s16x8 a[kAhead + 1];
-      auto read = [&](auto db) {
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (LDS(s16x4)*)(lds + (at ^ (32 * db.value))));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (LDS(s16x4)*)(lds + (at ^ (32 * db.value)) + SH::HALF));
-        a[db.value % (kAhead + 1)] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      };
-      unrolled<kAhead>(read);
+      unrolled<kAhead>([&](auto db) { read_values(slot, db, a); });
+    };
+    auto add_values = [&](int slot, const s16x8 (&p)[MT], s16x8 (&a)[kAhead + 1]) {
       unrolled<DB>([&](auto dbc) {
         constexpr int db = dbc.value;
-        if constexpr (db + kAhead < DB) read(std::integral_constant<int, db + kAhead>{});
+        if constexpr (db + kAhead < DB) read_values(slot, std::integral_constant<int, db + kAhead>{}, a);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
           acc[db][mt] = T::mfma(a[db % (kAhead + 1)], p[mt], acc[db][mt]);
@@ -778,8 +779,10 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
         load_k();
       }
       if (i < mine) {
+        s16x8 v[kAhead + 1];
+        first_values(t, slot, v);
         weights(t, s, p);
-        add_values(t, slot, p);
+        add_values(slot, p, v);
       }
       before = slot;
       slot = slot + 1 == SH::S ? 0 : slot + 1;
