@@ -396,7 +396,7 @@ int tv_commit_paths(int32_t batch, int32_t num_nodes, const int32_t* parents,
  * kv_heads; heads * head_dim at most TV_MAX_HIDDEN; page_size a power of two
  * from TV_MIN_PAGE to TV_MAX_PAGE; scale positive and finite; q, k_new, v_new,
  * caches and out 16-byte aligned, strides multiples of 8; the nodes of a tree,
- * and a page, at most 2^29 bytes; batch * num_nodes * heads at most 2^31 - 1.
+ * and the distance of two pages, at most 2^29 bytes; batch * num_nodes * heads at most 2^31 - 1.
  * out dtype [batch][num_nodes][heads][head_dim]. workspace:
  * tv_tree_attention_workspace_size() bytes (0 for invalid sizes), 256-byte
  * aligned. Nothing is allocated. Returns a tv_status_t; argument errors

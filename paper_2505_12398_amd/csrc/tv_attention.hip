@@ -502,73 +502,71 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
     const int64_t of_head = (static_cast<int64_t>(kh) << P.page_shift) * P.head_dim;
     const uint64_t k_base = reinterpret_cast<uint64_t>(P.k_cache + of_head);
     const uint64_t v_base = reinterpret_cast<uint64_t>(P.v_cache + of_head);
-    const int64_t page_bytes = 2 * P.page_stride;
-    auto resource = [](uint64_t a) {
-      return i32x4{static_cast<int>(a), static_cast<int>(a >> 32) & 0xffff, kRange, 0x00020000};
-    };
+    const uint32_t page_bytes = static_cast<uint32_t>(2 * P.page_stride);
+    const int mine = max(0, (t1 - t0 - kg + KW - 1) / KW);   // tiles of this key group
+    const int tile0 = t0 + kg, tile_end = tile0 + mine * KW, last_key = R.from + R.len - 1;
     auto first_key = [&](int t, int h) { return R.from + t * kKeys + h * kHalf; };
-    int page[kHalves];            // of the tile to load next
+    int page[kHalves] = {};       // of the tile to load next
     auto fetch = [&](int t) {
+      if (t < min(nct, tile_end)) {
 #pragma unroll
-      for (int hh = 0; hh < kHalves; ++hh)
-        if (t < nct)
-          page[hh] = pages[min(first_key(t, h0 + hh), R.from + R.len - 1) >> P.page_shift];
+        for (int hh = 0; hh < kHalves; ++hh)
+          page[hh] = pages[min(first_key(t, h0 + hh), last_key) >> P.page_shift];
+      }
     };
-    auto issue = [&](int t, int slot, auto what) {
-      constexpr int w0 = what.value == 2 ? 0 : what.value, w1 = what.value == 2 ? 2 : w0 + 1;
-      const int to = lds0 + ring + slot * SH::STAGE + h0 * SH::HALF + in0 * 1024;
-      if (t < nfull) {
+    // Where the tile to load lies: each half's keys, how much further the values are, its
+    // last row and the rows' distance. A tile behind the last has no range: its loads
+    // write zeros and read nothing, so that every round has the same loads in flight.
+    uint64_t at_k[kHalves] = {};
+    uint64_t to_v = 0;
+    int last[kHalves] = {}, stride = dbytes, range = 0;
+    bool plain = true;            // two full halves of a page
+    auto place = [&](int t) {
+      plain = t < nfull || t >= tile_end;
+      range = t < tile_end ? kRange : 0;
+      if (t < nct && t < tile_end) {
+        to_v = v_base - k_base;
+        stride = dbytes;
 #pragma unroll
         for (int hh = 0; hh < kHalves; ++hh) {
-          int pg = page[hh];
-          if (static_cast<unsigned>(pg) >= static_cast<unsigned>(P.num_pages)) {
-            bad = true;
-            pg = 0;
-          }
-          const int64_t at = pg * page_bytes + (first_key(t, h0 + hh) & in_page) * dbytes;
-#pragma unroll
-          for (int w = w0; w < w1; ++w)
-            load_to_lds<kIn>(resource((w ? v_base : k_base) + at), kv_off,
-                             to + hh * SH::HALF + w * SH::MAT);
+          const int key = min(first_key(t, h0 + hh), last_key);
+          last[hh] = last_key - key;                // rows past the context: its last one again
+          const bool is = static_cast<unsigned>(page[hh]) < static_cast<unsigned>(P.num_pages);
+          bad |= !is;
+          at_k[hh] = k_base + static_cast<uint64_t>(is ? page[hh] : 0) * page_bytes +
+                     static_cast<uint32_t>((key & in_page) * dbytes);
         }
-        return;
-      }
-      const int ln = here(lane);
+      } else if (t < tile_end) {                    // nodes, the last ones first
+        to_v = reinterpret_cast<uint64_t>(P.v_new) - reinterpret_cast<uint64_t>(P.k_new);
+        stride = static_cast<int>(P.kv_stride) * 2;
 #pragma unroll
-      for (int hh = 0; hh < kHalves; ++hh) {
-        uint64_t k_at, v_at;
-        int last, stride = dbytes;
-        if (t < nct) {
-          const int key = min(first_key(t, h0 + hh), R.from + R.len - 1);
-          last = R.from + R.len - key - 1;          // rows past the context: its last one again
-          int pg = page[hh];
-          if (static_cast<unsigned>(pg) >= static_cast<unsigned>(P.num_pages)) {
-            bad = true;
-            pg = 0;
-          }
-          const int64_t at = pg * page_bytes + (key & in_page) * dbytes;
-          k_at = k_base + at;
-          v_at = v_base + at;
-        } else {                                    // nodes, the last ones first
+        for (int hh = 0; hh < kHalves; ++hh) {
           const int from = min((R.tiles - 1 - t) * kKeys + (h0 + hh) * kHalf, P.num_nodes - 1);
-          last = P.num_nodes - 1 - from;
-          stride = static_cast<int>(P.kv_stride) * 2;
-          const int64_t at =
-              (static_cast<int64_t>(b) * P.num_nodes + from) * P.kv_stride + kh * P.head_dim;
-          k_at = reinterpret_cast<uint64_t>(P.k_new + at);
-          v_at = reinterpret_cast<uint64_t>(P.v_new + at);
+          last[hh] = P.num_nodes - 1 - from;
+          at_k[hh] = reinterpret_cast<uint64_t>(
+              P.k_new + (static_cast<int64_t>(b) * P.num_nodes + from) * P.kv_stride +
+              kh * P.head_dim);
         }
-#pragma unroll
-        for (int w = w0; w < w1; ++w)
-#pragma unroll 1
-          for (int i = 0; i < kIn; ++i) {
-            const int voff[1] = {offset(ln, in0 + i, last, stride)};
-            load_to_lds<1>(resource(w ? v_at : k_at), voff, to + hh * SH::HALF + w * SH::MAT + i * 1024);
-          }
       }
     };
-    constexpr std::integral_constant<int, 0> kKeysOnly{};
-    constexpr std::integral_constant<int, 1> kValuesOnly{};
+    auto issue = [&](int stage, bool values) {      // of the tile at that place
+      const int to = lds0 + stage + h0 * SH::HALF + in0 * 1024 + (values ? SH::MAT : 0);
+#pragma unroll
+      for (int hh = 0; hh < kHalves; ++hh) {
+        const uint64_t a = at_k[hh] + (values ? to_v : 0);
+        const i32x4 rs = {static_cast<int>(a), static_cast<int>(a >> 32) & 0xffff, range, 0x00020000};
+        if (plain) {
+          load_to_lds<kIn>(rs, kv_off, to + hh * SH::HALF);
+        } else {
+          const int ln = here(lane);
+#pragma unroll 1
+          for (int i = 0; i < kIn; ++i) {
+            const int voff[1] = {offset(ln, in0 + i, last[hh], stride)};
+            load_to_lds<1>(rs, voff, to + hh * SH::HALF + i * 1024);
+          }
+        }
+      }
+    };
 
     float m[MT], l[MT], c[MT];
     f32x4 acc[DB][MT];
@@ -581,8 +579,8 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
     }
 
     // Scores of a tile and their weights.
-    auto scores = [&](int t, int slot, f32x4 (&s)[MT][2]) {
-      const int at = ring + slot * SH::STAGE + k_at;
+    auto scores = [&](int stage, f32x4 (&s)[MT][2]) {
+      const int at = stage + k_at;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
         s[mt][0] = s[mt][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -603,34 +601,34 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
         __builtin_amdgcn_sched_barrier(0);
       });
     };
-    auto masked = [&](int t) { return t >= nct || (t + 1) * kKeys > R.len; };
-    auto weights = [&](int t, f32x4 (&s)[MT][2], s16x8 (&p)[MT]) {
-      if (masked(t)) {
-        const int hn = here(n), hg = here(g);
+    // A tile with keys that some rows do not see.
+    auto mask = [&](int t, f32x4 (&s)[MT][2]) {
+      const int hn = here(n), hg = here(g);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          uint32_t w = 0;
-          if (t < nct) {
-            w = (1u << (R.len - t * kKeys)) - 1;
-          } else {
-            const int tile = R.tiles - 1 - t, lo = tile * kKeys;
-            int y = walk[16 * mt + hn];
-            if (words) {
-              w = word[(y - node0) * (kWordNodes / kKeys) + tile];
-            } else {              // walk the path down to this tile, then through it
-              while (y >= lo + kKeys) y = par[y];
-              for (; y >= lo; y = par[y]) w |= 1u << (y - lo);
-              walk[16 * mt + hn] = static_cast<int16_t>(y);
-            }
+      for (int mt = 0; mt < MT; ++mt) {
+        uint32_t w = 0;
+        if (t < nct) {
+          w = (1u << (R.len - t * kKeys)) - 1;
+        } else {
+          const int tile = R.tiles - 1 - t, lo = tile * kKeys;
+          int y = walk[16 * mt + hn];
+          if (words) {
+            w = word[(y - node0) * (kWordNodes / kKeys) + tile];
+          } else {                // walk the path down to this tile, then through it
+            while (y >= lo + kKeys) y = par[y];
+            for (; y >= lo; y = par[y]) w |= 1u << (y - lo);
+            walk[16 * mt + hn] = static_cast<int16_t>(y);
           }
-          w >>= 4 * hg;
-#pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              s[mt][kb][r] = w >> (16 * kb + r) & 1 ? s[mt][kb][r] : -INFINITY;
         }
+        w >>= 4 * hg;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            s[mt][kb][r] = w >> (16 * kb + r) & 1 ? s[mt][kb][r] : -INFINITY;
       }
+    };
+    auto weights = [&](f32x4 (&s)[MT][2], s16x8 (&p)[MT]) {
       float top[MT];
       bool moves = false;
 #pragma unroll
@@ -673,47 +671,44 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
     };
     // Values: the first kAhead operands are read before the weights are formed.
     constexpr int kAhead = DB / 2;
-    auto read_values = [&](int slot, auto dbc, s16x8 (&a)[kAhead + 1]) {
+    auto read_values = [&](int stage, auto dbc, s16x8 (&a)[kAhead + 1]) {
       constexpr int db = dbc.value;
-      const int at = (ring + slot * SH::STAGE + SH::MAT + v_at) ^ (32 * db);
+      const int at = (stage + SH::MAT + v_at) ^ (32 * db);
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS(s16x4)*)(lds + at));
       const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS(s16x4)*)(lds + at + SH::HALF));
       a[db % (kAhead + 1)] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    auto first_values = [&](int t, int slot, s16x8 (&a)[kAhead + 1]) {
-      const int mat = ring + slot * SH::STAGE + SH::MAT;
-      // Nodes that a row does not see may hold anything: their weight 0 times NaN or
-      // infinity must not reach the row. Such values enter the product as 0 and are
-      // added to the rows that see them once these are written.
-      if (t >= nct) {
-        // (a half word's exponent of ones, plus one, carries into its sign's place)
-        constexpr uint32_t kExp = T::kExponent * 0x10001u, kOne = (0x8000u - T::kExponent) * 0x10001u;
-        const int hl = here(lane);
-        uint32_t ones = 0;
+    // Nodes that a row does not see may hold anything: their weight 0 times NaN or
+    // infinity must not reach the row. Such values enter the product as 0 and are
+    // added to the rows that see them once these are written.
+    auto clean = [&](int stage) {
+      const int mat = stage + SH::MAT;
+      // (a half word's exponent of ones, plus one, carries into its sign's place)
+      constexpr uint32_t kExp = T::kExponent * 0x10001u, kOne = (0x8000u - T::kExponent) * 0x10001u;
+      const int hl = here(lane);
+      uint32_t ones = 0;
 #pragma unroll 2
-        for (int i = 0; i < SH::MAT / 1024; ++i) {
-          const u32x4 w = *(const LDS(u32x4)*)(lds + mat + 1024 * i + 16 * hl);
+      for (int i = 0; i < SH::MAT / 1024; ++i) {
+        const u32x4 w = *(const LDS(u32x4)*)(lds + mat + 1024 * i + 16 * hl);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) ones |= (w[j] & kExp) + kOne;
-        }
-        const bool some = ones & 0x80008000u;
-        if (__builtin_amdgcn_ballot_w64(some)) {
-#pragma unroll 1
-          for (int i = hl; i < SH::MAT / 4; i += 64) {
-            LDS(uint32_t)* const at = (LDS(uint32_t)*)(lds + mat + 4 * i);
-            const uint32_t w = *at;
-            *at = ((w & T::kExponent) == T::kExponent ? 0 : w & 0xffffu) |
-                  ((w >> 16 & T::kExponent) == T::kExponent ? 0 : w & 0xffff0000u);
-          }
-        }
-        odd |= __builtin_amdgcn_ballot_w64(some) != 0;
+        for (int j = 0; j < 4; ++j) ones |= (w[j] & kExp) + kOne;
       }
-      unrolled<kAhead>([&](auto db) { read_values(slot, db, a); });
+      const bool some = ones & 0x80008000u;
+      if (__builtin_amdgcn_ballot_w64(some)) {
+#pragma unroll 1
+        for (int i = hl; i < SH::MAT / 4; i += 64) {
+          LDS(uint32_t)* const at = (LDS(uint32_t)*)(lds + mat + 4 * i);
+          const uint32_t w = *at;
+          *at = ((w & T::kExponent) == T::kExponent ? 0 : w & 0xffffu) |
+                ((w >> 16 & T::kExponent) == T::kExponent ? 0 : w & 0xffff0000u);
+        }
+      }
+      odd |= __builtin_amdgcn_ballot_w64(some) != 0;
     };
-    auto add_values = [&](int slot, const s16x8 (&p)[MT], s16x8 (&a)[kAhead + 1]) {
+    auto add_values = [&](int stage, const s16x8 (&p)[MT], s16x8 (&a)[kAhead + 1]) {
       unrolled<DB>([&](auto dbc) {
         constexpr int db = dbc.value;
-        if constexpr (db + kAhead < DB) read_values(slot, std::integral_constant<int, db + kAhead>{}, a);
+        if constexpr (db + kAhead < DB) read_values(stage, std::integral_constant<int, db + kAhead>{}, a);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
           acc[db][mt] = T::mfma(a[db % (kAhead + 1)], p[mt], acc[db][mt]);
@@ -721,72 +716,64 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
       });
     };
 
-    const int mine = max(0, (t1 - t0 - kg + KW - 1) / KW);   // tiles of this key group
-    const int tile0 = t0 + kg;
     // Round i multiplies tile i. Its keys' place is free after the first product and its
     // values' after the second, once all wavefronts that share them are there, and is
     // refilled at once with those of tile i + S: loads are issued in the order K_0, V_0,
     // K_1, ..., V_{i-1+S} at the top of round i and K_{i+S} in its middle (a wavefront
     // that shares with none issues before it waits, the others after the barrier). All
-    // but the YOUNGER newest have landed when tile i's are there; near the end, where
-    // fewer were issued, all have.
+    // but the YOUNGER newest have landed when tile i's are there.
     const int rounds = (t1 - t0 + KW - 1) / KW;              // of the whole workgroup
     constexpr int kSteady = SH::YOUNGER * SH::MINE;
 #pragma unroll 1
-    for (int j = 0; j < SH::S && j < mine; ++j) {
+    for (int j = 0; j < SH::S; ++j) {
       fetch(tile0 + j * KW);
-      issue(tile0 + j * KW, j, kKeysOnly);
-      if (j < SH::S - 1) issue(tile0 + j * KW, j, kValuesOnly);
+      place(tile0 + j * KW);
+      issue(ring + j * SH::STAGE, false);
+      if (j < SH::S - 1) issue(ring + j * SH::STAGE, true);
     }
     prepare();
-    int slot = 0, before = SH::S - 1;                        // of tiles i and i - 1
+    constexpr int kLast = (SH::S - 1) * SH::STAGE;
+    int stage = ring, before = ring + kLast;                 // places of tiles i and i - 1
+    int t = tile0;
 #pragma unroll 1
-    for (int i = 0; i < rounds; ++i) {
-      const int t = tile0 + i * KW;
-      auto load_v = [&] {
-        if (i + SH::S - 1 >= mine) return;
-        issue(t + (SH::S - 1) * KW, before, kValuesOnly);
-        if (i + SH::S < mine) fetch(t + SH::S * KW);
-      };
-      auto load_k = [&] {
-        if (i + SH::S < mine) issue(t + SH::S * KW, slot, kKeysOnly);
-      };
+    for (int i = 0; i < rounds; ++i, t += KW) {
       f32x4 s[MT][2];
       s16x8 p[MT];
       if constexpr (RW == 1) {
         wait_reads();
-        load_v();
-      }
-      if (i + SH::S - 1 < mine)
+        issue(before, true);
         wait_loads<kSteady>();
-      else
-        wait_loads<0>();
-      if constexpr (RW > 1) {
+      } else {
+        wait_loads<kSteady>();
         barrier();
-        load_v();
+        issue(before, true);
       }
-      scores(t, slot, s);         // (of a tile that is none, behind this group's last: unused)
+      fetch(t + SH::S * KW);
+      scores(stage, s);           // (of a tile that is none, behind this group's last: unused)
+      place(t + SH::S * KW);
       if constexpr (RW == 1) {
         wait_reads();
-        load_k();
-      }
-      if (i + SH::S - (RW > 1 ? 1 : 0) < mine)
+        issue(stage, false);
         wait_loads<kSteady>();
-      else
-        wait_loads<0>();
-      if constexpr (RW > 1) {
+      } else {
+        wait_loads<kSteady>();
         barrier();
-        load_k();
+        issue(stage, false);
       }
-      if (i < mine) {
+      if (KW == 1 || i < mine) {
+        if (t >= nfull) {
+          mask(t, s);
+          if (t >= nct) clean(stage);
+        }
         s16x8 v[kAhead + 1];
-        first_values(t, slot, v);
-        weights(t, s, p);
-        add_values(slot, p, v);
+        unrolled<kAhead>([&](auto db) { read_values(stage, db, v); });
+        weights(s, p);
+        add_values(stage, p, v);
       }
-      before = slot;
-      slot = slot + 1 == SH::S ? 0 : slot + 1;
+      before = stage;
+      stage = stage == ring + kLast ? ring : stage + SH::STAGE;
     }
+    wait_loads<0>();              // (zeros for tiles that are none)
 
     // The key groups' parts, merged by group 0.
     const int el = here(lane), en = el & 15, eg = el >> 4;

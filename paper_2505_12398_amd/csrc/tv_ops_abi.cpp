@@ -49,7 +49,7 @@ int validate(const tv::AttentionArgs& a, void* workspace, size_t workspace_bytes
   if (a.num_pages > 0 && a.page_stride < kv_row * a.page_size) return TV_ERR_INVALID_ARG;
   if (a.q_stride % 8 || a.kv_stride % 8 || a.page_stride % 8) return TV_ERR_UNSUPPORTED;
   if (a.q_stride > kMaxBytes / 2 / a.num_nodes || a.kv_stride > kMaxBytes / 2 / a.num_nodes ||
-      kv_row * a.page_size > kMaxBytes / 2)
+      a.page_stride > kMaxBytes / 2)
     return TV_ERR_UNSUPPORTED;
   if (a.batch == 0) return TV_OK;
   if (!a.q || !a.k_new || !a.v_new || !a.ctx_len || !a.out || (a.num_nodes > 1 && !a.parents))
