@@ -375,32 +375,48 @@ def tv_cache_commit(layers, batch, num_nodes, kv_heads, head_bytes, k_new, v_new
         int(max_new), _ptr(slots), _ptr(path_nodes), int(path_width), _ptr(stream)))
 
 
-def _check(dev, **tensors):
-    """Each (tensor, shape, dtype) contiguous on ``dev`` with that shape and type (None passes)."""
-    for name, (t, shape, dtype) in tensors.items():
-        if t is None:
-            continue
-        if t.dtype != dtype:
-            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-        if tuple(t.shape) != tuple(shape):
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-        if t.device != dev or not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous on {dev}")
+def _check(name, t, shape, dtype, dev):
+    """``t`` contiguous on ``dev`` with that shape and type (None passes); its address."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.device != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous on {dev}")
+    return t.data_ptr()
 
 
-def _on(dev):
-    """The device as the current one while a call is enqueued on it."""
-    import contextlib
+class _On:
+    """The device of a call as the current one, and the stream to enqueue on (the given one or
+    that device's current stream)."""
 
-    import torch
-    return torch.cuda.device(dev) if dev.type == "cuda" else contextlib.nullcontext()
+    __slots__ = ("index", "before", "stream")
 
+    def __init__(self, dev, stream):
+        self.index = None
+        self.stream = stream
+        if dev.type == "cuda":
+            import torch
+            index = torch.cuda.current_device() if dev.index is None else dev.index
+            if index != torch.cuda.current_device():
+                self.index = index
+            if stream is None:
+                self.stream = torch._C._cuda_getCurrentRawStream(index)
 
-def _stream_of(dev, stream):
-    import torch
-    if stream is None and dev.type == "cuda":
-        return torch.cuda.current_stream(dev).cuda_stream
-    return stream
+    def __enter__(self):
+        if self.index is not None:
+            import torch
+            self.before = torch.cuda.current_device()
+            torch.cuda.set_device(self.index)
+        return self.stream
+
+    def __exit__(self, *_):
+        if self.index is not None:
+            import torch
+            torch.cuda.set_device(self.before)
+        return False
 
 
 def _workspace(need, workspace, dev):
@@ -412,28 +428,32 @@ def _workspace(need, workspace, dev):
     return workspace, workspace.numel() * workspace.element_size()
 
 
-def _rows(name, t, dev, dtype):
+def _rows(name, t, dev, dtype, shape):
     """Stride between the nodes of a [B, N+1, heads, head_dim] tensor whose nodes follow each
     other evenly, each node's heads together (a slice of a projection's output)."""
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    B, n1, H, D = t.shape
-    stride = t.stride(1) if n1 > 1 else t.stride(0) if B > 1 else H * D
-    if t.device != dev or t.stride(3) != 1 and D > 1 or t.stride(2) != D and H > 1 or \
-            t.stride(0) != n1 * stride and B > 1:
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    B, n1, H, D = shape
+    sb, sn, sh, sd = t.stride()
+    stride = sn if n1 > 1 else sb if B > 1 else H * D
+    if t.device != dev or sd != 1 and D > 1 or sh != D and H > 1 or sb != n1 * stride and B > 1:
         raise ValueError(f"{name}: nodes must lie evenly spaced on {dev}, their heads contiguous")
     return stride
 
 
-def _pages(name, t, dev, dtype):
+def _pages(name, t, dev, dtype, shape):
     """Stride between the pages of a [pages, kv_heads, page_size, head_dim] cache."""
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    P, KH, ps, D = t.shape
-    if t.device != dev or (t.stride(3) != 1 and D > 1) or t.stride(2) != D or \
-            (t.stride(1) != ps * D and KH > 1):
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    P, KH, ps, D = shape
+    sp, sh, sr, sd = t.stride()
+    if t.device != dev or (sd != 1 and D > 1) or sr != D or (sh != ps * D and KH > 1):
         raise ValueError(f"{name}: pages must be contiguous on {dev}")
-    return t.stride(0) if P > 1 else KH * ps * D
+    return sp if P > 1 else KH * ps * D
 
 
 def tree_attention(q, k_new, v_new, parents, k_cache, v_cache, block_table, ctx_len, scale,
@@ -449,38 +469,36 @@ def tree_attention(q, k_new, v_new, parents, k_cache, v_cache, block_table, ctx_
     if q.dim() != 4 or k_new.dim() != 4 or k_cache.dim() != 4:
         raise ValueError("q, k_new, v_new and the caches have four dimensions")
     B, n1, H, D = q.shape
-    KH, ps = k_cache.shape[1], k_cache.shape[2]
-    dev = q.device
-    if q.dtype not in (torch.bfloat16, torch.float16):
-        raise TypeError(f"q must be bfloat16 or float16, got {q.dtype}")
-    for name, t, shape in (("k_new", k_new, (B, n1, KH, D)), ("v_new", v_new, (B, n1, KH, D)),
-                           ("k_cache", k_cache, (k_cache.shape[0], KH, ps, D)),
-                           ("v_cache", v_cache, tuple(k_cache.shape))):
-        if tuple(t.shape) != shape:
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
-    q_stride = _rows("q", q, dev, q.dtype)
-    kv_stride = _rows("k_new", k_new, dev, q.dtype)
-    if _rows("v_new", v_new, dev, q.dtype) != kv_stride:
+    P, KH, ps, _ = k_cache.shape
+    dev, dt, i32 = q.device, q.dtype, torch.int32
+    if dt != torch.bfloat16 and dt != torch.float16:
+        raise TypeError(f"q must be bfloat16 or float16, got {dt}")
+    q_stride = _rows("q", q, dev, dt, (B, n1, H, D))
+    kv_stride = _rows("k_new", k_new, dev, dt, (B, n1, KH, D))
+    if _rows("v_new", v_new, dev, dt, (B, n1, KH, D)) != kv_stride:
         raise ValueError("k_new and v_new must have the same strides")
-    page_stride = _pages("k_cache", k_cache, dev, q.dtype)
-    if _pages("v_cache", v_cache, dev, q.dtype) != page_stride:
+    page_stride = _pages("k_cache", k_cache, dev, dt, (P, KH, ps, D))
+    if _pages("v_cache", v_cache, dev, dt, (P, KH, ps, D)) != page_stride:
         raise ValueError("k_cache and v_cache must have the same strides")
     if prefix_len and prefix_pages is None:
         prefix_pages = block_table[0, :prefix_len // ps]
     if out is None:
-        out = torch.empty((B, n1, H, D), dtype=q.dtype, device=dev)
-    _check(dev, parents=(parents, (B, n1), torch.int32),
-           block_table=(block_table, (B, block_table.shape[-1]), torch.int32),
-           ctx_len=(ctx_len, (B,), torch.int32), out=(out, (B, n1, H, D), q.dtype),
-           prefix_pages=(prefix_pages, (prefix_len // ps,), torch.int32))
-    with _on(dev):
-        need = tv_tree_attention_workspace_size(B, n1, H, KH, D, prefix_len)
-        workspace, nbytes = _workspace(need, workspace, dev)
-        st = tv_tree_attention(
-            B, n1, H, KH, D, TV_DTYPE_BF16 if q.dtype == torch.bfloat16 else TV_DTYPE_F16, parents,
-            q, q_stride, k_new, v_new, kv_stride, k_cache, v_cache, page_stride,
-            k_cache.shape[0], ps, block_table, block_table.shape[1], ctx_len, prefix_pages,
-            prefix_len, scale, out, workspace, nbytes, _stream_of(dev, stream))
+        out = torch.empty((B, n1, H, D), dtype=dt, device=dev)
+    width = block_table.shape[-1]
+    parents = _check("parents", parents, (B, n1), i32, dev)
+    table = _check("block_table", block_table, (B, width), i32, dev)
+    ctx = _check("ctx_len", ctx_len, (B,), i32, dev)
+    to = _check("out", out, (B, n1, H, D), dt, dev)
+    prefix = _check("prefix_pages", prefix_pages, (prefix_len // ps,), i32, dev)
+    lib = load_library()
+    with _On(dev, stream) as at:
+        ws, nbytes = _workspace(
+            lib.tv_tree_attention_workspace_size(B, n1, H, KH, D, prefix_len), workspace, dev)
+        st = lib.tv_tree_attention(
+            B, n1, H, KH, D, TV_DTYPE_BF16 if dt == torch.bfloat16 else TV_DTYPE_F16, parents,
+            q.data_ptr(), q_stride, k_new.data_ptr(), v_new.data_ptr(), kv_stride,
+            k_cache.data_ptr(), v_cache.data_ptr(), page_stride, P, ps, table, width, ctx, prefix,
+            prefix_len, scale, to, ws.data_ptr(), nbytes, at)
     if st != TV_OK:
         raise TvError(st, "tv_tree_attention")
     return out
@@ -498,35 +516,39 @@ def process_logits(logits, temperature, parents=None, tokens=None, history=None,
     other nodes are left as they were. Raises on a non-OK return."""
     import torch
     B, n1, V = logits.shape
-    dev = logits.device
+    dev, i32, f32 = logits.device, torch.int32, torch.float32
     first, count = (0, n1) if nodes is None else nodes
     dtype = _dtype_code(logits)
     if out is None:
         out = torch.empty_like(logits)
-    i32, f32 = torch.int32, torch.float32
     H = history.shape[-1] if history is not None else 0
     nb = bias_tokens.shape[-1] if bias_tokens is not None else 0
     nm = masks.shape[0] if masks is not None else 0
-    _check(dev, logits=(logits, (B, n1, V), logits.dtype), out=(out, (B, n1, V), logits.dtype),
-           parents=(parents, (B, n1), i32), tokens=(tokens, (B, n1), i32),
-           history=(history, (B, H), i32), history_len=(history_len, (B,), i32),
-           prompt_len=(prompt_len, (B,), i32), repetition=(repetition, (B,), f32),
-           presence=(presence, (B,), f32), frequency=(frequency, (B,), f32),
-           bias_tokens=(bias_tokens, (B, nb), i32), bias_values=(bias_values, (B, nb), f32),
-           masks=(masks, (nm, (V + 31) // 32), i32), mask_index=(mask_index, (B, n1), i32))
-    row_max = row_sum = None
-    with _on(dev):
-        need = 0
+    per_row, per_tree = (B, n1), (B,)
+    z = _check("logits", logits, (B, n1, V), logits.dtype, dev)
+    to = _check("out", out, (B, n1, V), logits.dtype, dev)
+    ins = (_check("parents", parents, per_row, i32, dev),
+           _check("tokens", tokens, per_row, i32, dev),
+           _check("history", history, (B, H), i32, dev), H,
+           _check("history_len", history_len, per_tree, i32, dev),
+           _check("prompt_len", prompt_len, per_tree, i32, dev),
+           _check("repetition", repetition, per_tree, f32, dev),
+           _check("presence", presence, per_tree, f32, dev),
+           _check("frequency", frequency, per_tree, f32, dev),
+           _check("bias_tokens", bias_tokens, (B, nb), i32, dev),
+           _check("bias_values", bias_values, (B, nb), f32, dev), nb,
+           _check("masks", masks, (nm, (V + 31) // 32), i32, dev), nm,
+           _check("mask_index", mask_index, per_row, i32, dev))
+    row_max = row_sum = ws = None
+    nbytes = 0
+    lib = load_library()
+    with _On(dev, stream) as at:
         if want_stats:
-            row_max = torch.empty((B, n1), dtype=torch.float32, device=dev)
-            row_sum = torch.empty((B, n1), dtype=torch.float64, device=dev)
-            need = tv_process_logits_workspace_size(B, n1, V)
-        workspace, nbytes = _workspace(need, workspace, dev)
-        st = tv_process_logits(
-            B, n1, V, first, count, logits, dtype, temperature, parents, tokens, history, H,
-            history_len, prompt_len, repetition, presence, frequency, bias_tokens, bias_values, nb,
-            masks, nm, mask_index, out, row_max, row_sum, workspace, nbytes,
-            _stream_of(dev, stream))
+            row_max = torch.empty(per_row, dtype=f32, device=dev)
+            row_sum = torch.empty(per_row, dtype=torch.float64, device=dev)
+            ws, nbytes = _workspace(lib.tv_process_logits_workspace_size(B, n1, V), workspace, dev)
+        st = lib.tv_process_logits(B, n1, V, first, count, z, dtype, temperature, *ins, to,
+                                   _ptr(row_max), _ptr(row_sum), _ptr(ws), nbytes, at)
     if st != TV_OK:
         raise TvError(st, "tv_process_logits")
     return out, row_max, row_sum
@@ -548,24 +570,29 @@ def cache_extend(new_len, seq_len, block_table, free_pages, free_count, page_siz
     may hold ``seq_len`` and ``free_count`` themselves). Raises on a non-OK
     return."""
     import torch
-    B, dev = new_len.shape[0], block_table.device
-    i32 = torch.int32
+    B, dev, i32 = new_len.shape[0], block_table.device, torch.int32
     if out is None:
         if B == 0:
             return CacheGrowth(new_len.new_empty((0, max_new)), seq_len.clone(),
                                free_count.clone(), new_len.new_empty(0))
-        out = CacheGrowth(*(torch.empty(s, dtype=i32, device=dev)
-                            for s in ((B, max_new), (B,), (1,), (B,))))
-    _check(dev, new_len=(new_len, (B,), i32), seq_len=(seq_len, (B,), i32),
-           block_table=(block_table, (B, block_table.shape[-1]), i32),
-           free_pages=(free_pages, (free_pages.shape[0],), i32), free_count=(free_count, (1,), i32),
-           slots=(out.slots, (B, max_new), i32), out_seq_len=(out.seq_len, (B,), i32),
-           out_free_count=(out.free_count, (1,), i32), status=(out.status, (B,), i32))
-    with _on(dev):
-        st = tv_cache_extend(B, new_len, max_new, seq_len, out.seq_len, block_table,
-                             block_table.shape[1], page_size, prefix_len, free_pages,
-                             free_pages.shape[0], free_count, out.free_count, out.slots,
-                             out.status, _stream_of(dev, stream))
+        out = CacheGrowth(torch.empty((B, max_new), dtype=i32, device=dev),
+                          torch.empty(B, dtype=i32, device=dev),
+                          torch.empty(1, dtype=i32, device=dev),
+                          torch.empty(B, dtype=i32, device=dev))
+    width, pages, per = block_table.shape[-1], free_pages.shape[0], (B,)
+    new = _check("new_len", new_len, per, i32, dev)
+    seq = _check("seq_len", seq_len, per, i32, dev)
+    table = _check("block_table", block_table, (B, width), i32, dev)
+    free = _check("free_pages", free_pages, (pages,), i32, dev)
+    count = _check("free_count", free_count, (1,), i32, dev)
+    slots = _check("slots", out.slots, (B, max_new), i32, dev)
+    out_seq = _check("out.seq_len", out.seq_len, per, i32, dev)
+    out_count = _check("out.free_count", out.free_count, (1,), i32, dev)
+    status = _check("status", out.status, per, i32, dev)
+    with _On(dev, stream) as at:
+        st = load_library().tv_cache_extend(B, new, max_new, seq, out_seq, table, width, page_size,
+                                            prefix_len, free, pages, count, out_count, slots,
+                                            status, at)
     if st != TV_OK:
         raise TvError(st, "tv_cache_extend")
     return out
@@ -582,33 +609,35 @@ def cache_commit(k_new, v_new, k_cache, v_cache, new_len, slots, path_nodes=None
     if k_new.dim() != 5 or k_cache.dim() != 5:
         raise ValueError("k_new, v_new and the caches have five dimensions")
     L, B, n1, KH, D = k_new.shape
-    P, ps = k_cache.shape[1], k_cache.shape[3]
+    _, P, _, ps, _ = k_cache.shape
     dev, dt, i32 = k_cache.device, k_cache.dtype, torch.int32
-    if tuple(k_cache.shape) != (L, P, KH, ps, D):
-        raise ValueError(f"k_cache has shape {tuple(k_cache.shape)}, expected {(L, P, KH, ps, D)}")
-    strides = {}
-    for name, t, like in (("k_new", k_new, k_new), ("v_new", v_new, k_new),
-                          ("k_cache", k_cache, k_cache), ("v_cache", v_cache, k_cache)):
-        if t.shape != like.shape:
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(like.shape)}")
-        if L == 0:
-            return
-        one = _rows(name, t[0], dev, dt) if like is k_new else _pages(name, t[0], dev, dt)
-        strides[name] = (t.stride(0) if L > 1 else 0, one)
-    if strides["k_new"] != strides["v_new"] or strides["k_cache"] != strides["v_cache"]:
+    for name, t, lead in (("k_cache", k_cache, L), ("v_cache", v_cache, L), ("v_new", v_new, L)):
+        if t.dim() != 5 or t.shape[0] != lead:
+            raise ValueError(f"{name} must have five dimensions and {lead} layers")
+    if L == 0:
+        return
+    nodes, pages = (B, n1, KH, D), (P, KH, ps, D)
+    node = _rows("k_new", k_new[0], dev, dt, nodes)
+    page = _pages("k_cache", k_cache[0], dev, dt, pages)
+    same = _rows("v_new", v_new[0], dev, dt, nodes) == node and \
+        _pages("v_cache", v_cache[0], dev, dt, pages) == page
+    new_layer, layer = (k_new.stride(0), k_cache.stride(0)) if L > 1 else (0, 0)
+    if not same or L > 1 and (v_new.stride(0) != new_layer or v_cache.stride(0) != layer):
         raise ValueError("keys and values must have the same strides")
-    most = slots.shape[-1]
-    width = path_nodes.shape[-1] if path_nodes is not None else 0
-    if path_nodes is not None and path_nodes.dim() == 2 and path_nodes.stride(0) != width:
-        path_nodes = path_nodes.contiguous()
-    _check(dev, new_len=(new_len, (B,), i32), slots=(slots, (B, most), i32),
-           path_nodes=(path_nodes, (B, width), i32))
+    most, width, path = slots.shape[-1], 0, None
+    if path_nodes is not None:
+        width = path_nodes.shape[-1]
+        if path_nodes.dim() == 2 and path_nodes.stride(0) != width:
+            path_nodes = path_nodes.contiguous()
+        path = _check("path_nodes", path_nodes, (B, width), i32, dev)
+    new = _check("new_len", new_len, (B,), i32, dev)
+    at_slots = _check("slots", slots, (B, most), i32, dev)
     e = k_new.element_size()
-    with _on(dev):
-        st = tv_cache_commit(L, B, n1, KH, D * e, k_new, v_new, strides["k_new"][0] * e,
-                             strides["k_new"][1] * e, k_cache, v_cache, strides["k_cache"][0] * e,
-                             strides["k_cache"][1] * e, P, ps, new_len, most, slots, path_nodes,
-                             width, _stream_of(dev, stream))
+    with _On(dev, stream) as at:
+        st = load_library().tv_cache_commit(
+            L, B, n1, KH, D * e, k_new.data_ptr(), v_new.data_ptr(), new_layer * e, node * e,
+            k_cache.data_ptr(), v_cache.data_ptr(), layer * e, page * e, P, ps, new, most,
+            at_slots, path, width, at)
     if st != TV_OK:
         raise TvError(st, "tv_cache_commit")
 
