@@ -15,6 +15,8 @@
 #include <hip/hip_runtime.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "tv.h"
 #include "tv_launch.h"
 
@@ -28,6 +30,8 @@ static_assert(kOwn == 32, "a thread's tokens are the bits of a word");
 constexpr uint32_t kTold = 0x80000000u;            // in the prompt; below it the count
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 // vectors of rows that need not start on 16 bytes
 typedef u32x4 __attribute__((aligned(2))) u32x4_any2;
 typedef u32x4 __attribute__((aligned(4))) u32x4_any4;
@@ -36,8 +40,10 @@ typedef u32x4 __attribute__((aligned(4))) u32x4_any4;
 template <class T> struct Raw;
 template <> struct Raw<uint16_t> {
   u32x4 w;
+  template <bool kOnce>
   __device__ __forceinline__ void load(const uint16_t* p) {
-    w = *reinterpret_cast<const u32x4_any2*>(p);
+    const auto* q = reinterpret_cast<const u32x4_any2*>(p);
+    w = kOnce ? __builtin_nontemporal_load(q) : *q;
   }
   __device__ __forceinline__ float at(int i) const {
     const uint32_t u = w[i >> 1];
@@ -46,9 +52,12 @@ template <> struct Raw<uint16_t> {
 };
 template <> struct Raw<float> {
   u32x4 w[2];
+  template <bool kOnce>
   __device__ __forceinline__ void load(const float* p) {
-    w[0] = *reinterpret_cast<const u32x4_any4*>(p);
-    w[1] = *reinterpret_cast<const u32x4_any4*>(p + 4);
+    const auto* q = reinterpret_cast<const u32x4_any4*>(p);
+    const auto* r = reinterpret_cast<const u32x4_any4*>(p + 4);
+    w[0] = kOnce ? __builtin_nontemporal_load(q) : *q;
+    w[1] = kOnce ? __builtin_nontemporal_load(r) : *r;
   }
   __device__ __forceinline__ float at(int i) const { return __uint_as_float(w[i >> 2][i & 3]); }
 };
@@ -61,21 +70,52 @@ template <> __device__ __forceinline__ uint16_t stored<uint16_t>(float x) {
 }
 template <> __device__ __forceinline__ float stored<float>(float x) { return x; }
 
+template <bool kOnce>
 __device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
   u32x4 w;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    w[i] = uint32_t{stored<uint16_t>(v[2 * i])} | uint32_t{stored<uint16_t>(v[2 * i + 1])} << 16;
-  *reinterpret_cast<u32x4_any2*>(p) = w;
+    w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2 * i], v[2 * i + 1]}, bf16x2));
+  if (kOnce)
+    __builtin_nontemporal_store(w, reinterpret_cast<u32x4_any2*>(p));
+  else
+    *reinterpret_cast<u32x4_any2*>(p) = w;
 }
+template <bool kOnce>
 __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     u32x4 w;
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[4 * h + i]);
-    *reinterpret_cast<u32x4_any4*>(p + 4 * h) = w;
+    if (kOnce)
+      __builtin_nontemporal_store(w, reinterpret_cast<u32x4_any4*>(p + 4 * h));
+    else
+      *reinterpret_cast<u32x4_any4*>(p + 4 * h) = w;
   }
+}
+
+// Reductions over a wavefront, in vector instructions alone: neighbours, pairs, the
+// quads and halves of a row of 16, rows, halves.
+template <class F>
+__device__ __forceinline__ float over_wave(float x, F&& join) {
+  auto other = [&](auto ctrl) {
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), ctrl.value, 0xf, 0xf, true));
+  };
+  x = join(x, other(std::integral_constant<int, 0xB1>{}));    // lanes 1 0 3 2
+  x = join(x, other(std::integral_constant<int, 0x4E>{}));    // lanes 2 3 0 1
+  x = join(x, other(std::integral_constant<int, 0x141>{}));   // half rows mirrored
+  x = join(x, other(std::integral_constant<int, 0x140>{}));   // rows mirrored
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = join(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return join(__uint_as_float(h[0]), __uint_as_float(h[1]));
+}
+
+// x where bit e of `bits` is set, else y
+__device__ __forceinline__ float where_bit(uint32_t bits, int e, float x, float y) {
+  const uint32_t m = static_cast<uint32_t>(static_cast<int32_t>(bits << (31 - e)) >> 31);
+  return __uint_as_float((__float_as_uint(x) & m) | (__float_as_uint(y) & ~m));
 }
 
 struct Penalties {
@@ -106,8 +146,9 @@ struct Params {
   float k32;                 // log2(e) / T rounded to fp32
 };
 
-template <class T>
-__global__ void __launch_bounds__(kThreads) logits_kernel(Params P) {
+// kMasks: nodes have masks. kOnce: past the caches, for more than these hold.
+template <class T, bool kMasks, bool kOnce>
+__global__ void __launch_bounds__(kThreads, 4) logits_kernel(Params P) {
   const tv::LogitsArgs& a = P.a;
   __shared__ uint32_t words[kChunk];
   __shared__ int32_t toks[TV_MAX_NODES];   // place in this chunk, or -1
@@ -126,6 +167,32 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(Params P) {
   };
   // token e of this thread (e < 32): its place in the chunk
   auto place = [&](int e) { return ((e >> 3) * kThreads + tid) * 8 + (e & 7); };
+
+  const T* const in = static_cast<const T*>(a.logits);
+  T* const to = static_cast<T*>(a.out);
+  const int mask_words = (V + 31) / 32;
+  const int r0 = a.first_node + slab * P.rows;
+  const int r1 = min(r0 + P.rows, a.first_node + a.num_rows);
+  const T ninf = stored<T>(-INFINITY);
+  auto row_of = [&](int i) { return static_cast<size_t>(b) * n1 + i; };
+  auto load = [&](int i, Raw<T> (&raw)[kGroups]) {
+    const T* p = in + row_of(i) * V + base;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const int at = (g * kThreads + tid) * 8;
+      if (at + 8 <= width) {
+        raw[g].template load<kOnce>(p + at);
+      } else {
+        // a row's last few tokens
+        T x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = at + e < width ? p[at + e] : ninf;
+        __builtin_memcpy(&raw[g], x, sizeof x);
+      }
+    }
+  };
+  Raw<T> next[kGroups];
+  load(r0, next);             // (under way while the counts are formed)
 
   // biases: of several entries for a token the last one
   float off[kOwn];
@@ -199,37 +266,13 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(Params P) {
     off[e] = taken(static_cast<int>(w & ~kTold), off[e], pen);
   }
 
-  const T* const in = static_cast<const T*>(a.logits);
-  T* const to = static_cast<T*>(a.out);
-  const int mask_words = (V + 31) / 32;
-  const int r0 = a.first_node + slab * P.rows;
-  const int r1 = min(r0 + P.rows, a.first_node + a.num_rows);
-  const T ninf = stored<T>(-INFINITY);
-  auto row_of = [&](int i) { return static_cast<size_t>(b) * n1 + i; };
-  auto load = [&](int i, Raw<T> (&raw)[kGroups]) {
-    const T* p = in + row_of(i) * V + base;
-#pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-      const int at = (g * kThreads + tid) * 8;
-      if (at + 8 <= width) {
-        raw[g].load(p + at);
-      } else {
-        // a row's last few tokens
-        T x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = at + e < width ? p[at + e] : ninf;
-        __builtin_memcpy(&raw[g], x, sizeof x);
-      }
-    }
-  };
-  Raw<T> next[kGroups];
-  load(r0, next);
   for (int i = r0; i < r1; ++i) {
     Raw<T> raw[kGroups];
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) raw[g] = next[g];
     if (i + 1 < r1) load(i + 1, next);
     const size_t row = row_of(i);
+    asm volatile("" : "+v"(seen));     // 32 lane masks would not fit the scalar registers
     // this thread's tokens that are on the path
     uint32_t mine = 0;
     int first = 0;
@@ -242,7 +285,7 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(Params P) {
     }
     // this thread's allowed tokens
     uint32_t allowed = ~0u;
-    if (a.mask_index) {
+    if constexpr (kMasks) {
       const int m = a.mask_index[row];
       if (m >= a.num_masks) {
         allowed = 0;
@@ -262,8 +305,8 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(Params P) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float z = raw[g].at(e);
-        const float x = (seen >> (8 * g + e) & 1 ? repeated(z, pen) : z) - off[8 * g + e];
-        v[g][e] = allowed >> (8 * g + e) & 1 ? x : -INFINITY;
+        const float x = where_bit(seen, 8 * g + e, repeated(z, pen), z) - off[8 * g + e];
+        v[g][e] = kMasks ? where_bit(allowed, 8 * g + e, x, -INFINITY) : x;
       }
     for (uint32_t left = mine & allowed; left; left &= left - 1) {
       const int e = __builtin_ctz(left), t = place(e);
@@ -286,7 +329,7 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(Params P) {
     for (int g = 0; g < kGroups; ++g) {
       const int at = (g * kThreads + tid) * 8;
       if (at + 8 <= width) {
-        store8(q + at, v[g]);
+        store8<kOnce>(q + at, v[g]);
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -299,13 +342,10 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(Params P) {
     for (int g = 0; g < kGroups; ++g)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        v[g][e] = value(stored<T>(v[g][e]));
-        const int at = (g * kThreads + tid) * 8 + e;
-        if (at >= width) v[g][e] = -INFINITY;
+        v[g][e] = value(stored<T>(v[g][e]));   // (-inf past the vocabulary, as loaded)
         mx = fmaxf(mx, v[g][e]);
       }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+    mx = over_wave(mx, [](float x, float y) { return fmaxf(x, y); });
     // a row with no finite value keeps the frame 0, so its terms are 0 as well
     const float c = mx > -INFINITY ? -mx * P.k32 : 0.0f;
     float s = 0.0f;
@@ -313,8 +353,7 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(Params P) {
     for (int g = 0; g < kGroups; ++g)
 #pragma unroll
       for (int e = 0; e < 8; ++e) s += __builtin_amdgcn_exp2f(fmaf(v[g][e], P.k32, c));
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    s = over_wave(s, [](float x, float y) { return x + y; });
     if (lane == 0) {
       const size_t part = (row * P.chunks + chunk) * kWaves + wave;
       P.part_max[part] = mx;
@@ -357,6 +396,22 @@ __global__ void __launch_bounds__(kThreads) logits_merge_kernel(Params P) {
   }
 }
 
+constexpr size_t kLastLevelCache = size_t{256} << 20;
+
+template <class T>
+hipError_t run(const Params& P, unsigned grid, size_t bytes, hipStream_t stream) {
+  const bool once = bytes > kLastLevelCache, masks = P.a.mask_index != nullptr;
+  if (masks && once)
+    hipLaunchKernelGGL((logits_kernel<T, true, true>), dim3(grid), dim3(kThreads), 0, stream, P);
+  else if (masks)
+    hipLaunchKernelGGL((logits_kernel<T, true, false>), dim3(grid), dim3(kThreads), 0, stream, P);
+  else if (once)
+    hipLaunchKernelGGL((logits_kernel<T, false, true>), dim3(grid), dim3(kThreads), 0, stream, P);
+  else
+    hipLaunchKernelGGL((logits_kernel<T, false, false>), dim3(grid), dim3(kThreads), 0, stream, P);
+  return hipGetLastError();
+}
+
 // Workgroups that fill the device a few times over.
 constexpr int kEnough = 2048;
 
@@ -380,12 +435,12 @@ int launch_logits(const LogitsArgs& a, void* workspace, hipStream_t stream) {
   P.rows = (a.num_rows + P.slabs - 1) / P.slabs;
   P.slabs = (a.num_rows + P.rows - 1) / P.rows;
   if (per * P.slabs > INT32_MAX) return TV_ERR_UNSUPPORTED;
-  const dim3 grid(static_cast<unsigned>(per * P.slabs));
-  if (a.dtype == TV_DTYPE_BF16)
-    hipLaunchKernelGGL((logits_kernel<uint16_t>), grid, dim3(kThreads), 0, stream, P);
-  else
-    hipLaunchKernelGGL((logits_kernel<float>), grid, dim3(kThreads), 0, stream, P);
-  if (hipGetLastError() != hipSuccess) return TV_ERR_HIP;
+  const size_t bytes = static_cast<size_t>(a.batch) * a.num_rows * a.vocab *
+                       (a.dtype == TV_DTYPE_BF16 ? 4 : 8);     // read and written
+  const hipError_t e = a.dtype == TV_DTYPE_BF16
+                           ? run<uint16_t>(P, static_cast<unsigned>(per * P.slabs), bytes, stream)
+                           : run<float>(P, static_cast<unsigned>(per * P.slabs), bytes, stream);
+  if (e != hipSuccess) return TV_ERR_HIP;
   if (!a.row_max) return TV_OK;
   const int64_t rows = static_cast<int64_t>(a.batch) * a.num_rows;
   hipLaunchKernelGGL(logits_merge_kernel, dim3(static_cast<unsigned>((rows + kWaves - 1) / kWaves)),
