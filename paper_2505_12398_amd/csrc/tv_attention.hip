@@ -260,10 +260,11 @@ __device__ __forceinline__ int here(int x) {
   return x;
 }
 
-// Where part `t` of `parts` begins on the line of `total` tiles.
+// Where part `t` of `parts` begins on the line of `total` tiles. (In double precision,
+// a tenth of the instructions of a 64-bit division: every workgroup computes the same
+// cuts, which grow with t and end at the total.)
 __device__ __forceinline__ long long cut(long long total, int t, int parts) {
-  const long long each = total / parts;
-  return each * t + (total - each * parts) * t / parts;
+  return static_cast<long long>(static_cast<double>(total) * t / parts);
 }
 
 // Output index of row r of an item: (node of the pass, head).
@@ -282,7 +283,7 @@ __device__ __forceinline__ void write_out(const Pass& P, size_t row, int d, cons
 // Adds to elements d .. d + 3 of an output what of the values of its row's path is not
 // finite (written by this lane before, from sums without them).
 template <class T, class SH>
-__device__ void add_odd(const Pass& P, int b, int kh, int r, size_t row, int d) {
+__device__ __forceinline__ void add_odd(const Pass& P, int b, int kh, int r, size_t row, int d) {
   if (d >= P.head_dim) return;
   float add[4] = {0.0f, 0.0f, 0.0f, 0.0f};
   const int64_t tree = static_cast<int64_t>(b) * P.num_nodes;
@@ -413,7 +414,9 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
       if (++b >= P.batch) break;
       continue;
     }
-    const int item = uniform(static_cast<int>(in_tree / R.tiles));
+    int item = uniform(static_cast<int>(static_cast<double>(in_tree) / R.tiles));
+    if (static_cast<long long>(item) * R.tiles > in_tree) --item;   // (rounded up)
+    item = uniform(item);
     const int t0 = static_cast<int>(in_tree - static_cast<long long>(item) * R.tiles);
     const int kh = uniform(item / P.chunks), chunk = item - kh * P.chunks;
     const int t1 = static_cast<int>(min<long long>(R.tiles, t0 + (end - pos)));
@@ -864,11 +867,14 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
                 o += c2 * *reinterpret_cast<const f32x4*>(P.pre + row * SH::DP + 16 * db + 4 * eg);
               write_out<T, SH>(P, row, 16 * db + 4 * eg, o * inv);
             }
-            if (any & 2) {
-#pragma unroll 1
-              for (int db = 0; db < DB; ++db) add_odd<T, SH>(P, b, kh, r, row, 16 * db + 4 * eg);
-            }
           }
+        }
+      }
+      if (whole && any & 2 && !P.prefix_pass) {
+#pragma unroll 1
+        for (int i = 0; i < MT * DB; ++i) {
+          const int r = rbase + 16 * (i / DB) + en;
+          if (r < P.rows) add_odd<T, SH>(P, b, kh, r, out_row(P, b, kh, r), 16 * (i % DB) + 4 * eg);
         }
       }
     }
