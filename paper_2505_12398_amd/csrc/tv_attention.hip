@@ -316,11 +316,12 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
   const int rg = wave % RW, kg = wave / RW;
   const int n = lane & 15, g = lane >> 4;
 
-  // This workgroup's team and row tile. Workgroups are dealt to the XCDs in turn.
+  // This workgroup's team and row tile. Workgroups are dealt to the XCDs in turn, and
+  // so are the teams (a team on one XCD), so that little work uses all of them.
   const int per_xcd = P.teams / kXcds;
   const int in_xcd = blockIdx.x / kXcds;
   const int of_xcd = uniform(in_xcd / P.team), member = in_xcd - of_xcd * P.team;
-  const int team = static_cast<int>(blockIdx.x % kXcds) * per_xcd + of_xcd;
+  const int team = of_xcd * kXcds + static_cast<int>(blockIdx.x % kXcds);
   if (of_xcd >= per_xcd) return;
 
   // The line of tiles: how long, and where this team's part begins.
