@@ -499,7 +499,7 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
     // Loads of tile t: this wavefront's part of its keys (0) and values (1).
     CONSTANT(int)* const pages =
         (CONSTANT(int)*)(P.table + static_cast<size_t>(b) * P.table_width);
-    bool bad = R.bad;             // a page that is none
+    uint32_t worst = 0;           // the largest page number seen
     bool odd = false;             // a node's value that is not finite
     const int ring = kg * SH::S * SH::STAGE;
     const int in_page = (1 << P.page_shift) - 1, nfull = R.len / kKeys;
@@ -525,6 +525,12 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
     uint64_t to_v = 0;
     int last[kHalves] = {}, stride = dbytes, range = 0;
     bool plain = true;            // two full halves of a page
+    auto key_at = [&](int page, int key) {          // (a page that is none: any other, to report)
+      const uint32_t pg = static_cast<uint32_t>(page);
+      worst = max(worst, pg);
+      return k_base + static_cast<uint64_t>(min(pg, static_cast<uint32_t>(P.num_pages - 1))) *
+                          page_bytes + static_cast<uint32_t>((key & in_page) * dbytes);
+    };
     auto place = [&](int t) {
       plain = t < nfull || t >= tile_end;
       range = t < tile_end ? kRange : 0;
@@ -535,10 +541,7 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
         for (int hh = 0; hh < kHalves; ++hh) {
           const int key = min(first_key(t, h0 + hh), last_key);
           last[hh] = last_key - key;                // rows past the context: its last one again
-          const bool is = static_cast<unsigned>(page[hh]) < static_cast<unsigned>(P.num_pages);
-          bad |= !is;
-          at_k[hh] = k_base + static_cast<uint64_t>(is ? page[hh] : 0) * page_bytes +
-                     static_cast<uint32_t>((key & in_page) * dbytes);
+          at_k[hh] = key_at(page[hh], key);
         }
       } else if (t < tile_end) {                    // nodes, the last ones first
         to_v = reinterpret_cast<uint64_t>(P.v_new) - reinterpret_cast<uint64_t>(P.k_new);
@@ -738,36 +741,65 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
     prepare();
     constexpr int kLast = (SH::S - 1) * SH::STAGE;
     int stage = ring, before = ring + kLast;                 // places of tiles i and i - 1
-    int t = tile0;
-#pragma unroll 1
-    for (int i = 0; i < rounds; ++i, t += KW) {
+    // hot: the tile itself and those it loads are full and lie in pages. Such rounds run
+    // without branches: a wavefront's own instructions, at five cycles or more each, are
+    // what a round without them takes (general rounds alone: 1.3 times the time).
+    auto round = [&](auto hot_c, int i, int t) {
+      constexpr bool kHot = hot_c.value;
       f32x4 s[MT][2];
       s16x8 p[MT];
+      auto load = [&](int stage, bool values) {
+        if constexpr (!kHot) {
+          issue(stage, values);
+        } else {
+          const int to = lds0 + stage + h0 * SH::HALF + in0 * 1024 + (values ? SH::MAT : 0);
+#pragma unroll
+          for (int hh = 0; hh < kHalves; ++hh) {
+            const uint64_t a = at_k[hh] + (values ? v_base - k_base : 0);
+            load_to_lds<kIn>(i32x4{static_cast<int>(a), static_cast<int>(a >> 32) & 0xffff, kRange,
+                                   0x00020000}, kv_off, to + hh * SH::HALF);
+          }
+        }
+      };
       if constexpr (RW == 1) {
         wait_reads();
-        issue(before, true);
+        load(before, true);
         wait_loads<kSteady>();
       } else {
         wait_loads<kSteady>();
         barrier();
-        issue(before, true);
+        load(before, true);
       }
-      fetch(t + SH::S * KW);
+      if constexpr (kHot) {
+#pragma unroll
+        for (int hh = 0; hh < kHalves; ++hh)
+          page[hh] = pages[first_key(t + SH::S * KW, h0 + hh) >> P.page_shift];
+      } else {
+        fetch(t + SH::S * KW);
+      }
       scores(stage, s);           // (of a tile that is none, behind this group's last: unused)
-      place(t + SH::S * KW);
+      if constexpr (kHot) {
+#pragma unroll
+        for (int hh = 0; hh < kHalves; ++hh)
+          at_k[hh] = key_at(page[hh], first_key(t + SH::S * KW, h0 + hh));
+      } else {
+        place(t + SH::S * KW);
+      }
       if constexpr (RW == 1) {
         wait_reads();
-        issue(stage, false);
+        load(stage, false);
         wait_loads<kSteady>();
       } else {
         wait_loads<kSteady>();
         barrier();
-        issue(stage, false);
+        load(stage, false);
       }
-      if (KW == 1 || i < mine) {
-        if (t >= nfull) {
-          mask(t, s);
-          if (t >= nct) clean(stage);
+      if (kHot || KW == 1 || i < mine) {
+        if constexpr (!kHot) {
+          if (t >= nfull) {
+            mask(t, s);
+            if (t >= nct) clean(stage);
+          }
         }
         s16x8 v[kAhead + 1];
         unrolled<kAhead>([&](auto db) { read_values(stage, db, v); });
@@ -776,7 +808,14 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
       }
       before = stage;
       stage = stage == ring + kLast ? ring : stage + SH::STAGE;
-    }
+    };
+    int i = 0, t = tile0;
+#pragma unroll 1
+    for (const int lim = min(nfull, tile_end) - SH::S * KW; t < lim; ++i, t += KW)
+      round(std::true_type{}, i, t);
+    // (what the first of these loads is placed by the last round above, or before them)
+#pragma unroll 1
+    for (; i < rounds; ++i, t += KW) round(std::false_type{}, i, t);
     wait_loads<0>();              // (zeros for tiles that are none)
 
     // The key groups' parts, merged by group 0.
@@ -787,7 +826,7 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
       l[mt] += __shfl_xor(l[mt], 32, 64);
     }
     barrier();                    // all have read their last tile
-    if (el == 0) flags[wave] = bad | odd << 1;
+    if (el == 0) flags[wave] = (R.bad || (P.num_pages > 0 && worst >= static_cast<uint32_t>(P.num_pages))) | odd << 1;
     if (kg > 0) {
       const int w = (kg - 1) * RW + rg;
 #pragma unroll
