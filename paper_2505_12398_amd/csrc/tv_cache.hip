@@ -78,14 +78,18 @@ __device__ __forceinline__ long long scan(long long x, long long (&part)[kScanWa
 template <bool kSlots>
 __global__ void __launch_bounds__(kScanThreads) extend_kernel(tv::ExtendArgs a) {
   __shared__ long long part[kScanWaves];
-  __shared__ int seqs[kScanThreads], adds[kScanThreads], helds[kScanThreads], tops[kScanThreads];
+  __shared__ int seqs[kScanThreads], adds[kScanThreads], helds[kScanThreads], tops[kScanThreads],
+      needs[kScanThreads];
   const int tid = threadIdx.x, lane = tid & 63;
   const int shift = 31 - __builtin_clz(a.page_size);
+  __shared__ int most;                 // pages taken
+  if (tid == 0) most = 0;
   const int count = min(max(a.free_count[0], 0), a.num_pages);
   long long pushed = 0;
+  Request r{};
   for (int b0 = 0; b0 < a.batch; b0 += kScanThreads) {
     const int b = b0 + tid;
-    const Request r = b < a.batch ? request(a, b) : Request{};
+    r = b < a.batch ? request(a, b) : Request{};
     if (!__syncthreads_or(r.back > 0)) continue;
     long long total;
     const long long at = count + pushed + scan(r.back, part, total);
@@ -105,10 +109,9 @@ __global__ void __launch_bounds__(kScanThreads) extend_kernel(tv::ExtendArgs a) 
   __syncthreads();
   const int avail = static_cast<int>(min<long long>(count + pushed, a.num_pages));
   long long before = 0;
-  int used = 0;
   for (int b0 = 0; b0 < a.batch; b0 += kScanThreads) {
     const int b = b0 + tid;
-    Request r = b < a.batch ? request(a, b) : Request{};
+    if (a.batch > kScanThreads) r = b < a.batch ? request(a, b) : Request{};
     long long total;
     const long long at = before + scan(r.need, part, total);
     before += total;
@@ -116,25 +119,29 @@ __global__ void __launch_bounds__(kScanThreads) extend_kernel(tv::ExtendArgs a) 
       r.status = TV_CACHE_FULL;
       r.add = r.need = 0;
     }
-    if (r.need > 0) used = static_cast<int>(at) + r.need;
+    if (r.need > 0) atomicMax(&most, static_cast<int>(at) + r.need);
     // page j of the new ones is free_pages[top - j]
     const int top = avail - 1 - static_cast<int>(r.need > 0 ? at : 0);
-    for (uint64_t m = __ballot(r.need > 0); m; m &= m - 1) {
-      const int l = __builtin_ctzll(m);
-      const int n = __shfl(r.need, l, 64), from = __shfl(top, l, 64);
-      const size_t to = static_cast<size_t>(b - lane + l) * a.table_width + __shfl(r.held, l, 64);
-      for (int j = lane; j < n; j += 64) a.block_table[to + j] = a.free_pages[from - j];
-    }
+    if (r.need > 0)
+      a.block_table[static_cast<size_t>(b) * a.table_width + r.held] = a.free_pages[top];
+    seqs[tid] = r.seq;
+    adds[tid] = r.add;
+    helds[tid] = r.held;
+    tops[tid] = top;
+    needs[tid] = r.need;
     if (b < a.batch) {
       a.status[b] = r.status;
       a.new_seq_len[b] = r.ends ? 0 : r.seq + r.add;
     }
+    // a request's further pages by a wavefront, the requests by all wavefronts
+    if (__syncthreads_or(r.need > 1)) {
+      for (int q = tid >> 6; q < min(kScanThreads, a.batch - b0); q += kScanWaves) {
+        const int n = needs[q], from = tops[q];
+        const size_t to = static_cast<size_t>(b0 + q) * a.table_width + helds[q];
+        for (int j = 1 + lane; j < n; j += 64) a.block_table[to + j] = a.free_pages[from - j];
+      }
+    }
     if constexpr (kSlots) {
-      seqs[tid] = r.seq;
-      adds[tid] = r.add;
-      helds[tid] = r.held;
-      tops[tid] = top;
-      __syncthreads();
       const int n = min(kScanThreads, a.batch - b0) * a.max_new;
       for (int i = tid; i < n; i += kScanThreads) {
         const int q = i / a.max_new, k = i - q * a.max_new;
@@ -150,11 +157,6 @@ __global__ void __launch_bounds__(kScanThreads) extend_kernel(tv::ExtendArgs a) 
       }
     }
   }
-  __shared__ int most;
-  if (tid == 0) most = 0;
-  __syncthreads();
-  if (used > 0) atomicMax(&most, used);
-  __syncthreads();
   if (tid == 0) a.new_free_count[0] = avail - most;
 }
 
