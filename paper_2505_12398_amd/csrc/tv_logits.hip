@@ -148,7 +148,7 @@ struct Params {
 
 // kMasks: nodes have masks. kOnce: past the caches, for more than these hold.
 template <class T, bool kMasks, bool kOnce>
-__global__ void __launch_bounds__(kThreads, 4) logits_kernel(Params P) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) logits_kernel(Params P) {
   const tv::LogitsArgs& a = P.a;
   __shared__ uint32_t words[kChunk];
   __shared__ int32_t toks[TV_MAX_NODES];   // place in this chunk, or -1
@@ -209,10 +209,16 @@ __global__ void __launch_bounds__(kThreads, 4) logits_kernel(Params P) {
       if (t < static_cast<unsigned>(width)) atomicMax(&words[t], static_cast<uint32_t>(j + 1));
     }
     __syncthreads();
+    // (few threads have any)
+    uint32_t any = 0;
 #pragma unroll
-    for (int e = 0; e < kOwn; ++e) {
-      const uint32_t j = words[place(e)];
-      if (j) off[e] = bias[j - 1];
+    for (int e = 0; e < kOwn; ++e) any |= words[place(e)];
+    if (any) {
+#pragma unroll
+      for (int e = 0; e < kOwn; ++e) {
+        const uint32_t j = words[place(e)];
+        if (j) off[e] = bias[j - 1];
+      }
     }
     __syncthreads();
     clear();
@@ -241,10 +247,27 @@ __global__ void __launch_bounds__(kThreads, 4) logits_kernel(Params P) {
       }
     }
   }
-  // links skip nodes whose token is elsewhere (any ancestor read meanwhile is one)
+  // Links skip nodes whose token is elsewhere: a few steps of every node's path at
+  // first, which do for most trees, then by doubling (any ancestor read meanwhile is one).
   if (a.parents) {
-    bool more;
-    do {
+    constexpr int kSteps = 8, kPer = TV_MAX_NODES / kThreads;
+    int16_t up[kPer];
+    bool more = false;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const int i = tid + k * kThreads;
+      if (i >= n1) break;
+      int u = ups[i];
+      for (int step = 0; step < kSteps && u > 0 && toks[u] < 0; ++step) u = ups[u];
+      up[k] = static_cast<int16_t>(u);
+      more |= u > 0 && toks[u] < 0;
+    }
+    more = __syncthreads_or(more);
+#pragma unroll
+    for (int k = 0; k < kPer; ++k)
+      if (tid + k * kThreads < n1) ups[tid + k * kThreads] = up[k];
+    __syncthreads();
+    while (more) {
       more = false;
       for (int i = tid; i < n1; i += kThreads) {
         const int u = ups[i];
@@ -254,7 +277,7 @@ __global__ void __launch_bounds__(kThreads, 4) logits_kernel(Params P) {
         }
       }
       more = __syncthreads_or(more);
-    } while (more);
+    }
   } else {
     __syncthreads();
   }
@@ -412,8 +435,10 @@ hipError_t run(const Params& P, unsigned grid, size_t bytes, hipStream_t stream)
   return hipGetLastError();
 }
 
-// Workgroups that fill the device a few times over.
-constexpr int kEnough = 2048;
+// Workgroups that fill the device: four on a CU, or three of fp32 (their rows take more
+// registers). Each counts its chunk's history anew, so more of them cost more than they
+// gain: one tree of 65 nodes 30.1 us, with twice as many 33.8, with half 34.2.
+constexpr int kEnough = 1024, kEnoughF32 = 768;
 
 }  // namespace
 
@@ -430,7 +455,7 @@ int launch_logits(const LogitsArgs& a, void* workspace, hipStream_t stream) {
   }
   P.k32 = static_cast<float>(1.4426950408889634 / static_cast<double>(a.temperature));
   const int64_t per = static_cast<int64_t>(a.batch) * P.chunks;
-  const int64_t want = (kEnough + per - 1) / per;
+  const int64_t want = ((a.dtype == TV_DTYPE_BF16 ? kEnough : kEnoughF32) + per - 1) / per;
   P.slabs = static_cast<int>(want < a.num_rows ? want : a.num_rows);
   P.rows = (a.num_rows + P.slabs - 1) / P.slabs;
   P.slabs = (a.num_rows + P.rows - 1) / P.rows;
