@@ -891,22 +891,22 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
               *reinterpret_cast<f32x4*>(P.pre + row * SH::DP + 16 * db + 4 * eg) = acc[db][mt];
             if (eg == 0) P.pre_ml[row] = f32x2{m[mt], l[mt]};
           } else {
-            float a = 1.0f, c2 = 0.0f;
-            f32x2 ml = {0.0f, 0.0f};
-            if (R.shared) {
-              ml = P.pre_ml[row];
-              const float both = fmaxf(m[mt], ml[0]);
-              a = to_frame(m[mt], both, P.k);
-              c2 = to_frame(ml[0], both, P.k);
-            }
-            const float inv = 1.0f / (l[mt] * a + ml[1] * c2);
+            if (R.shared) {       // the prefix' part: all of it read before a row is written
+              f32x4 pre[DB];
+              const f32x2 ml = P.pre_ml[row];
 #pragma unroll
-            for (int db = 0; db < DB; ++db) {
-              f32x4 o = acc[db][mt] * a;
-              if (R.shared)
-                o += c2 * *reinterpret_cast<const f32x4*>(P.pre + row * SH::DP + 16 * db + 4 * eg);
-              write_out<T, SH>(P, row, 16 * db + 4 * eg, o * inv);
+              for (int db = 0; db < DB; ++db)
+                pre[db] = *reinterpret_cast<const f32x4*>(P.pre + row * SH::DP + 16 * db + 4 * eg);
+              const float both = fmaxf(m[mt], ml[0]);
+              const float own = to_frame(m[mt], both, P.k), theirs = to_frame(ml[0], both, P.k);
+              l[mt] = l[mt] * own + ml[1] * theirs;
+#pragma unroll
+              for (int db = 0; db < DB; ++db) acc[db][mt] = acc[db][mt] * own + pre[db] * theirs;
             }
+            const float inv = 1.0f / l[mt];
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+              write_out<T, SH>(P, row, 16 * db + 4 * eg, acc[db][mt] * inv);
           }
         }
       }
@@ -973,11 +973,15 @@ __global__ void __launch_bounds__(64 * kMergeWaves) merge_kernel(Pass P) {
   const float inv = 1.0f / (l * own + ml[1] * pre);
   bool odd = false;
   for (int i = 0; i < count; ++i) odd |= part(i)[SH::PART - 1] != 0.0f;
+  if (shared)
+#pragma unroll
+    for (int k = 0; k < DBW; ++k)
+      acc[k] = acc[k] * own +
+               pre * *reinterpret_cast<const f32x4*>(P.pre + row * SH::DP + 16 * (db0 + k) + 4 * g);
+#pragma unroll
   for (int k = 0; k < DBW; ++k) {
     const int at = 16 * (db0 + k) + 4 * g;
-    f32x4 o = acc[k] * own;
-    if (shared) o += pre * *reinterpret_cast<const f32x4*>(P.pre + row * SH::DP + at);
-    write_out<T, SH>(P, row, at, o * inv);
+    write_out<T, SH>(P, row, at, acc[k] * inv);
     if (odd) add_odd<T, SH>(P, b, d[1], r, row, at);
   }
 }
