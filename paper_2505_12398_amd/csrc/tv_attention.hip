@@ -27,6 +27,13 @@
 // that the keys leave HBM once. An item that is cut leaves its parts' (maximum, sum,
 // accumulators) in the workspace, and a second kernel merges them.
 //
+// What bounds it. 256 trees of 65 nodes on contexts of 1000 to 2900, 32 heads over 8:
+// 876 us, 610 TFLOP/s, 2.7 TB/s of keys and values; the matrix units are busy for 37% of
+// it at the 2.0 GHz that such a load runs at. A lone wavefront's round of 32 keys takes
+// 1950 cycles (scores 490, weights 465, values 440, eight loads 43 each), so that the
+// issue of its own instructions bounds it: 815 us remain without the loads. Single
+// tokens of 64 sequences: 282 us, 5.6 TB/s, which is the rate of a large read.
+//
 // A common prefix is an item of its own whose rows are those of all trees; its
 // (maximum, sum, accumulators) wait in the workspace for the trees' own parts.
 #include <hip/hip_runtime.h>
@@ -41,12 +48,17 @@
 
 namespace {
 
-constexpr int kMergeWaves = 4;
+constexpr int kMergeWaves = 4, kMergeAhead = 8;
 constexpr int kKeys = 32, kHalf = 16;     // keys of a tile and of a half
 constexpr int kXcds = 8, kMaxCus = 256;
 constexpr int kWavesPerCu = 8;            // resident wavefronts, two on a SIMD
 constexpr int kMaxTeam = 32;              // workgroups of a team: the CUs of an XCD
-constexpr int kMinTiles = 8;              // of a part
+// Of a part: smaller parts use more CUs and leave more to merge. One tree of 65 nodes on
+// a context of 1024: parts of 4 / 8 / 16 / 32 tiles 33 / 34 / 41 / 50 us; 16 trees of 24
+// on 4096: 8 / 16 / 32 88 / 88 / 69.
+constexpr int kMinTiles = 8;
+// Up to how many nodes the rows' paths are kept as words (in LDS, 32 bytes a node): 256
+// trees of 65 nodes 885 us, walked per tile 895.
 constexpr int kWordNodes = 256;
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
@@ -743,7 +755,7 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
     int stage = ring, before = ring + kLast;                 // places of tiles i and i - 1
     // hot: the tile itself and those it loads are full and lie in pages. Such rounds run
     // without branches: a wavefront's own instructions, at five cycles or more each, are
-    // what a round without them takes (general rounds alone: 1.3 times the time).
+    // what a round without them takes (general rounds alone 906 us where this is 883).
     auto round = [&](auto hot_c, int i, int t) {
       constexpr bool kHot = hot_c.value;
       f32x4 s[MT][2];
@@ -940,20 +952,44 @@ __global__ void __launch_bounds__(64 * kMergeWaves) merge_kernel(Pass P) {
                              : static_cast<size_t>(team + i - 1) * 2;
     return P.parts + (at * P.team + member) * SH::PART;
   };
+  // kMergeAhead parts at a time, all their loads in flight: a part comes from another
+  // XCD, and one after the other 16 of them took 50 us.
   float m = -INFINITY, l = 0.0f;
-  for (int i = 0; i < count; ++i)
-    m = fmaxf(m, part(i)[SH::PART_ACC + (block * 16 + n) * 2]);
+  bool odd = false;
   f32x4 acc[DBW];
-  for (int k = 0; k < DBW; ++k) acc[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int i = 0; i < count; ++i) {
-    const float* const from = part(i);
-    const f32x2 ml = *reinterpret_cast<const f32x2*>(from + SH::PART_ACC + (block * 16 + n) * 2);
-    const float f = to_frame(ml[0], m, P.k);
-    l += ml[1] * f;
 #pragma unroll
-    for (int k = 0; k < DBW; ++k)
-      acc[k] += f * *reinterpret_cast<const f32x4*>(
-                        from + (block * SH::DB + wave * DBW + k) * 256 + lane * 4);
+  for (int k = 0; k < DBW; ++k) acc[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int i0 = 0; i0 < count; i0 += kMergeAhead) {
+    f32x2 ml[kMergeAhead];
+    f32x4 of[kMergeAhead][DBW];
+    float flag[kMergeAhead];
+#pragma unroll
+    for (int j = 0; j < kMergeAhead; ++j) {
+      const float* const from = part(min(i0 + j, count - 1));
+      ml[j] = *reinterpret_cast<const f32x2*>(from + SH::PART_ACC + (block * 16 + n) * 2);
+      flag[j] = from[SH::PART - 1];
+#pragma unroll
+      for (int k = 0; k < DBW; ++k)
+        of[j][k] = *reinterpret_cast<const f32x4*>(
+            from + (block * SH::DB + wave * DBW + k) * 256 + lane * 4);
+    }
+    float top = m;
+#pragma unroll
+    for (int j = 0; j < kMergeAhead; ++j) top = fmaxf(top, ml[j][0]);
+    const float f = to_frame(m, top, P.k);
+    m = top;
+    l *= f;
+#pragma unroll
+    for (int k = 0; k < DBW; ++k) acc[k] *= f;
+#pragma unroll
+    for (int j = 0; j < kMergeAhead; ++j) {
+      if (i0 + j >= count) continue;
+      const float fj = to_frame(ml[j][0], top, P.k);
+      l += ml[j][1] * fj;
+      odd |= flag[j] != 0.0f;
+#pragma unroll
+      for (int k = 0; k < DBW; ++k) acc[k] += fj * of[j][k];
+    }
   }
   if (r >= P.rows) return;
   const int b = d[0];
@@ -971,8 +1007,6 @@ __global__ void __launch_bounds__(64 * kMergeWaves) merge_kernel(Pass P) {
   const float both = fmaxf(m, ml[0]);
   const float own = to_frame(m, both, P.k), pre = to_frame(ml[0], both, P.k);
   const float inv = 1.0f / (l * own + ml[1] * pre);
-  bool odd = false;
-  for (int i = 0; i < count; ++i) odd |= part(i)[SH::PART - 1] != 0.0f;
   if (shared)
 #pragma unroll
     for (int k = 0; k < DBW; ++k)
@@ -986,12 +1020,19 @@ __global__ void __launch_bounds__(64 * kMergeWaves) merge_kernel(Pass P) {
   }
 }
 
-// Rows per workgroup for `rows` query rows: 16, 32 or 48 of one wavefront's width, or
-// two or four of 48, whichever pads less.
-int block_rows(int64_t rows) {
+// Rows per workgroup for `items` (trees times key heads) of `rows` query rows: 16, 32 or
+// 48 of one wavefront's width, or two or four of 48, whichever pads less. A workgroup of
+// 48 has four groups of keys, so a wavefront reads all its keys and values for 48 rows
+// alone; one of 192 has one, which its wavefronts share, and a part is a wavefront's, not
+// a workgroup's. Batch 256, contexts of 2048, 32 heads over 8, by 48 / 96 / 192 rows:
+// 260 rows 1038 / 809 / 927 us, 192 rows 649 / 486 / 467, 128 rows 517 / 467 / 443.
+// Few items are cut into many parts, of which 48 rows leave a quarter as many to merge:
+// contexts of 4096, by 48 or else, 260 rows of 8 / 16 / 32 / 64 items 33 or 47, 37 or 51,
+// 55 or 57, 74 or 71 us; 192 rows of 32 / 64 / 128 items 41 or 81, 54 or 89, 75 or 92.
+int block_rows(int64_t rows, int64_t items) {
   if (rows <= 16) return 16;
   if (rows <= 32) return 32;
-  if (rows <= 48) return 48;
+  if (rows <= 48 || (rows + 47) / 48 * items <= kMaxCus) return 48;
   const int64_t two = (rows + 95) / 96 * 96, four = (rows + 191) / 192 * 192;
   return four <= two ? 192 : 96;
 }
@@ -1000,9 +1041,9 @@ struct Plan {
   int rows_per_wg, team, chunks, teams;
   size_t parts_bytes;
 };
-Plan plan(int64_t rows, int padded, int cus) {
+Plan plan(int64_t rows, int64_t items, int padded, int cus) {
   Plan p{};
-  p.rows_per_wg = block_rows(rows);
+  p.rows_per_wg = block_rows(rows, items);
   const int64_t tiles = (rows + p.rows_per_wg - 1) / p.rows_per_wg;
   p.chunks = static_cast<int>((tiles + kMaxTeam - 1) / kMaxTeam);
   p.team = static_cast<int>((tiles + p.chunks - 1) / p.chunks);
@@ -1022,9 +1063,9 @@ Layout layout(int64_t batch, int num_nodes, int heads, int kv_heads, int head_di
   Layout L{};
   L.desc = 0;
   L.parts = tv::align256(kMaxCus * kWavesPerCu * sizeof(i32x4));
-  size_t parts = plan(rows, padded, kMaxCus).parts_bytes;
+  size_t parts = plan(rows, batch * kv_heads, padded, kMaxCus).parts_bytes;
   if (prefix_len > 0) {
-    const size_t p = plan(rows * batch, padded, kMaxCus).parts_bytes;
+    const size_t p = plan(rows * batch, kv_heads, padded, kMaxCus).parts_bytes;
     parts = parts > p ? parts : p;
   }
   L.pre = tv::align256(L.parts + parts);
@@ -1077,7 +1118,8 @@ hipError_t run_rows(const Pass& P, int rows_per_wg, hipStream_t stream) {
 
 hipError_t run_pass(Pass P, int dtype, int cus, hipStream_t stream) {
   const int padded = P.head_dim <= 64 ? 64 : 128;
-  const Plan p = plan(P.rows, padded, cus);
+  const int64_t items = P.prefix_pass ? P.kv_heads : static_cast<int64_t>(P.batch) * P.kv_heads;
+  const Plan p = plan(P.rows, items, padded, cus);
   P.team = p.team;
   P.chunks = p.chunks;
   P.teams = p.teams;
