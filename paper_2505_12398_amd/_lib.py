@@ -390,29 +390,37 @@ def _check(name, t, shape, dtype, dev):
 
 class _On:
     """The device of a call as the current one, and the stream to enqueue on (the given one or
-    that device's current stream)."""
+    that device's current stream). A given stream is the current one meanwhile: tensors made
+    for the call belong to it, and are not given to another stream's work before it is done."""
 
-    __slots__ = ("index", "before", "stream")
+    __slots__ = ("index", "before", "stream", "current")
 
     def __init__(self, dev, stream):
-        self.index = None
+        self.index = self.current = None
         self.stream = stream
         if dev.type == "cuda":
             import torch
             index = torch.cuda.current_device() if dev.index is None else dev.index
             if index != torch.cuda.current_device():
                 self.index = index
+            now = torch._C._cuda_getCurrentRawStream(index)
             if stream is None:
-                self.stream = torch._C._cuda_getCurrentRawStream(index)
+                self.stream = now
+            elif stream != now:
+                self.current = torch.cuda.stream(torch.cuda.ExternalStream(stream, device=dev))
 
     def __enter__(self):
         if self.index is not None:
             import torch
             self.before = torch.cuda.current_device()
             torch.cuda.set_device(self.index)
+        if self.current is not None:
+            self.current.__enter__()
         return self.stream
 
     def __exit__(self, *_):
+        if self.current is not None:
+            self.current.__exit__(None, None, None)
         if self.index is not None:
             import torch
             torch.cuda.set_device(self.before)
@@ -482,16 +490,16 @@ def tree_attention(q, k_new, v_new, parents, k_cache, v_cache, block_table, ctx_
         raise ValueError("k_cache and v_cache must have the same strides")
     if prefix_len and prefix_pages is None:
         prefix_pages = block_table[0, :prefix_len // ps]
-    if out is None:
-        out = torch.empty((B, n1, H, D), dtype=dt, device=dev)
     width = block_table.shape[-1]
     parents = _check("parents", parents, (B, n1), i32, dev)
     table = _check("block_table", block_table, (B, width), i32, dev)
     ctx = _check("ctx_len", ctx_len, (B,), i32, dev)
-    to = _check("out", out, (B, n1, H, D), dt, dev)
     prefix = _check("prefix_pages", prefix_pages, (prefix_len // ps,), i32, dev)
     lib = load_library()
     with _On(dev, stream) as at:
+        if out is None:
+            out = torch.empty((B, n1, H, D), dtype=dt, device=dev)
+        to = _check("out", out, (B, n1, H, D), dt, dev)
         ws, nbytes = _workspace(
             lib.tv_tree_attention_workspace_size(B, n1, H, KH, D, prefix_len), workspace, dev)
         st = lib.tv_tree_attention(
@@ -519,14 +527,11 @@ def process_logits(logits, temperature, parents=None, tokens=None, history=None,
     dev, i32, f32 = logits.device, torch.int32, torch.float32
     first, count = (0, n1) if nodes is None else nodes
     dtype = _dtype_code(logits)
-    if out is None:
-        out = torch.empty_like(logits)
     H = history.shape[-1] if history is not None else 0
     nb = bias_tokens.shape[-1] if bias_tokens is not None else 0
     nm = masks.shape[0] if masks is not None else 0
     per_row, per_tree = (B, n1), (B,)
     z = _check("logits", logits, (B, n1, V), logits.dtype, dev)
-    to = _check("out", out, (B, n1, V), logits.dtype, dev)
     ins = (_check("parents", parents, per_row, i32, dev),
            _check("tokens", tokens, per_row, i32, dev),
            _check("history", history, (B, H), i32, dev), H,
@@ -543,6 +548,9 @@ def process_logits(logits, temperature, parents=None, tokens=None, history=None,
     nbytes = 0
     lib = load_library()
     with _On(dev, stream) as at:
+        if out is None:
+            out = torch.empty_like(logits)
+        to = _check("out", out, (B, n1, V), logits.dtype, dev)
         if want_stats:
             row_max = torch.empty(per_row, dtype=f32, device=dev)
             row_sum = torch.empty(per_row, dtype=torch.float64, device=dev)
@@ -571,25 +579,25 @@ def cache_extend(new_len, seq_len, block_table, free_pages, free_count, page_siz
     return."""
     import torch
     B, dev, i32 = new_len.shape[0], block_table.device, torch.int32
-    if out is None:
-        if B == 0:
-            return CacheGrowth(new_len.new_empty((0, max_new)), seq_len.clone(),
-                               free_count.clone(), new_len.new_empty(0))
-        out = CacheGrowth(torch.empty((B, max_new), dtype=i32, device=dev),
-                          torch.empty(B, dtype=i32, device=dev),
-                          torch.empty(1, dtype=i32, device=dev),
-                          torch.empty(B, dtype=i32, device=dev))
+    if out is None and B == 0:
+        return CacheGrowth(new_len.new_empty((0, max_new)), seq_len.clone(),
+                           free_count.clone(), new_len.new_empty(0))
     width, pages, per = block_table.shape[-1], free_pages.shape[0], (B,)
     new = _check("new_len", new_len, per, i32, dev)
     seq = _check("seq_len", seq_len, per, i32, dev)
     table = _check("block_table", block_table, (B, width), i32, dev)
     free = _check("free_pages", free_pages, (pages,), i32, dev)
     count = _check("free_count", free_count, (1,), i32, dev)
-    slots = _check("slots", out.slots, (B, max_new), i32, dev)
-    out_seq = _check("out.seq_len", out.seq_len, per, i32, dev)
-    out_count = _check("out.free_count", out.free_count, (1,), i32, dev)
-    status = _check("status", out.status, per, i32, dev)
     with _On(dev, stream) as at:
+        if out is None:
+            out = CacheGrowth(torch.empty((B, max_new), dtype=i32, device=dev),
+                              torch.empty(B, dtype=i32, device=dev),
+                              torch.empty(1, dtype=i32, device=dev),
+                              torch.empty(B, dtype=i32, device=dev))
+        slots = _check("slots", out.slots, (B, max_new), i32, dev)
+        out_seq = _check("out.seq_len", out.seq_len, per, i32, dev)
+        out_count = _check("out.free_count", out.free_count, (1,), i32, dev)
+        status = _check("status", out.status, per, i32, dev)
         st = load_library().tv_cache_extend(B, new, max_new, seq, out_seq, table, width, page_size,
                                             prefix_len, free, pages, count, out_count, slots,
                                             status, at)
@@ -625,15 +633,14 @@ def cache_commit(k_new, v_new, k_cache, v_cache, new_len, slots, path_nodes=None
     if not same or L > 1 and (v_new.stride(0) != new_layer or v_cache.stride(0) != layer):
         raise ValueError("keys and values must have the same strides")
     most, width, path = slots.shape[-1], 0, None
-    if path_nodes is not None:
-        width = path_nodes.shape[-1]
-        if path_nodes.dim() == 2 and path_nodes.stride(0) != width:
-            path_nodes = path_nodes.contiguous()
-        path = _check("path_nodes", path_nodes, (B, width), i32, dev)
     new = _check("new_len", new_len, (B,), i32, dev)
     at_slots = _check("slots", slots, (B, most), i32, dev)
     e = k_new.element_size()
     with _On(dev, stream) as at:
+        if path_nodes is not None:
+            width = path_nodes.shape[-1]
+            path_nodes = path_nodes.contiguous()
+            path = _check("path_nodes", path_nodes, (B, width), i32, dev)
         st = load_library().tv_cache_commit(
             L, B, n1, KH, D * e, k_new.data_ptr(), v_new.data_ptr(), new_layer * e, node * e,
             k_cache.data_ptr(), v_cache.data_ptr(), layer * e, page * e, P, ps, new, most,

@@ -158,6 +158,57 @@ def test_commit_from_a_projection_into_side_by_side_caches():
     assert torch.equal(both, want)
 
 
+def test_commit_of_a_long_prompt():
+    """More rows than the launch's workgroups take in one step each."""
+    n1, ps, KH = 20011, 1024, 2
+    P = -(-n1 // ps) + 1
+    k, v = (torch.randint(0, 256, (1, 1, n1, KH, 16), dtype=torch.uint8, device=DEV)
+            for _ in range(2))
+    caches = torch.zeros((2, 1, P, KH, ps, 16), dtype=torch.uint8, device=DEV)
+    slots = torch.randperm(P * ps, device=DEV)[:n1].int().view(1, n1)
+    n = torch.tensor([n1 - 3], dtype=torch.int32, device=DEV)
+    tv.cache_commit(k, v, caches[0], caches[1], n, slots)
+    want = torch.zeros_like(caches)
+    at = slots[0, :n1 - 3].long()
+    for c, t in ((0, k), (1, v)):
+        want[c, 0, at // ps, :, at % ps] = t[0, 0, :n1 - 3]
+    assert torch.equal(caches, want)
+
+
+def test_calls_on_a_given_stream():
+    """Everything that a call allocates belongs to the stream that it is given: work that the
+    current stream starts meanwhile, on memory of the same sizes, changes no result."""
+    s = torch.cuda.Stream()
+    B, n1, H, KH, D_, ps, width = 3, 9, 8, 2, 64, 16, 12
+    gen = torch.Generator(DEV).manual_seed(5)
+    q = torch.randn((B, n1, H, D_), device=DEV, generator=gen).bfloat16()
+    kv = torch.randn((B, n1, KH, D_), device=DEV, generator=gen).bfloat16()
+    cache = torch.randn((B * width, KH, ps, D_), device=DEV, generator=gen).bfloat16()
+    table = torch.arange(B * width, dtype=torch.int32, device=DEV).view(B, width)
+    ctx = torch.tensor([0, 17, 150], dtype=torch.int32, device=DEV)
+    parents = torch.arange(-1, n1 - 1, dtype=torch.int32, device=DEV).repeat(B, 1)
+    logits = torch.randn((B, n1, 5000), device=DEV, generator=gen)
+    new = torch.tensor([3, 0, 2], dtype=torch.int32, device=DEV)
+    path = torch.tensor([[1, 2, 0], [4, 0, 0], [5, 0, 0]], dtype=torch.int32, device=DEV)[:, :2]
+
+    def calls(stream):
+        free = torch.arange(B * width, dtype=torch.int32, device=DEV)
+        count = torch.tensor([B * width], dtype=torch.int32, device=DEV)
+        grown, caches = table.clone(), torch.zeros((2, 1, *cache.shape), device=DEV).bfloat16()
+        torch.cuda.synchronize()
+        out = tv.tree_attention(q, kv, kv, parents, cache, cache, table, ctx, 0.1, stream=stream)
+        rows = tv.process_logits(logits, 0.7, stream=stream)
+        g = tv.cache_extend(new, ctx, grown, free, count, ps, 4, stream=stream)
+        tv.cache_commit(kv[None], kv[None], *caches, new, g.slots, path_nodes=path, stream=stream)
+        for t in (out, *rows, torch.empty(1 << 22, dtype=torch.uint8, device=DEV)):
+            torch.empty_like(t).fill_(7)
+        torch.cuda.synchronize()
+        return out, *rows, g.slots, g.seq_len, g.free_count, g.status, grown, caches
+
+    for a, b in zip(calls(None), calls(s.cuda_stream)):
+        assert torch.equal(a, b)
+
+
 def test_captured_growth():
     """A captured cycle's growth in place, replayed: every replay grows the requests again."""
     rng = np.random.default_rng(8)
