@@ -488,7 +488,7 @@ def tree_attention(q, k_new, v_new, parents, k_cache, v_cache, block_table, ctx_
     page_stride = _pages("k_cache", k_cache, dev, dt, (P, KH, ps, D))
     if _pages("v_cache", v_cache, dev, dt, (P, KH, ps, D)) != page_stride:
         raise ValueError("k_cache and v_cache must have the same strides")
-    if prefix_len and prefix_pages is None:
+    if prefix_len and prefix_pages is None and B:
         prefix_pages = block_table[0, :prefix_len // ps]
     width = block_table.shape[-1]
     parents = _check("parents", parents, (B, n1), i32, dev)
@@ -521,7 +521,8 @@ def process_logits(logits, temperature, parents=None, tokens=None, history=None,
     ``logits``). ``nodes`` = (first, count) restricts the call to those nodes of
     every tree. Returns (out, row_max [B, N+1] float32, row_sum [B, N+1] float64),
     the statistics ``verify_batch`` takes (None without ``want_stats``); rows of
-    other nodes are left as they were. Raises on a non-OK return."""
+    other nodes are left as they were (new tensors hold nothing there). Raises on a
+    non-OK return."""
     import torch
     B, n1, V = logits.shape
     dev, i32, f32 = logits.device, torch.int32, torch.float32

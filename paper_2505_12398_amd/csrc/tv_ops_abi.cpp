@@ -135,6 +135,10 @@ int validate(const tv::CacheCommitArgs& a) {
   const int64_t row = static_cast<int64_t>(a.kv_heads) * a.head_bytes;
   if (a.node_stride < row || (a.num_pages > 0 && a.page_stride < row * a.page_size))
     return TV_ERR_INVALID_ARG;
+  // layers whose pages would overlap
+  if (a.layers > 1 && a.num_pages > 0 && a.cache_layer_stride < row * a.page_size &&
+      a.cache_layer_stride > -row * a.page_size)
+    return TV_ERR_INVALID_ARG;
   if (a.new_layer_stride % 16 || a.node_stride % 16 || a.cache_layer_stride % 16 ||
       a.page_stride % 16)
     return TV_ERR_UNSUPPORTED;

@@ -182,6 +182,48 @@ def test_prefix_of_many_single_tokens():
     check(host, call)
 
 
+@pytest.mark.parametrize("prefix", [0, 48])
+@pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("f16", 128), ("bf16", 64), ("f16", 40)])
+@pytest.mark.parametrize("n1,kind", [(24, "tree"), (48, "chain"), (65, "tree"), (300, "tree")])
+def test_rows_of_many_trees(n1, kind, dtype, dim, prefix):
+    """Enough trees that workgroups take 96 or 192 rows at a time."""
+    batch = 130 if n1 < 300 else 24
+    rng = np.random.default_rng(n1)
+    ctx = rng.integers(-3, 200, batch)
+    ctx[:4] = 200, 0, 48, 47
+    host, call = inputs(batch, n1, 8, 2, dim, 16, ctx, dtype, kind, prefix=prefix)
+    check(host, call, dtype)
+
+
+@pytest.mark.parametrize("heads", [4, 8])
+def test_garbage_and_pages_that_are_none_in_many_trees(heads):
+    """As above for one tree: no other node and no other tree sees any of it."""
+    batch, n1 = 130, 40
+    rng = np.random.default_rng(3)
+    host, call = inputs(batch, n1, heads, 2, 64, 16, rng.integers(17, 150, batch))
+    par = np.full((batch, n1), -1, np.int32)
+    par[:, 1], par[:, 2] = 0, 0
+    par[:, 3:] = np.arange(1, n1 - 2)
+    call["parents"] = torch.as_tensor(par, device=DEV)
+    host["parents"] = par
+    clean = check(host, call)
+    k, v, table = call["k_new"].clone(), call["v_new"].clone(), call["block_table"].clone()
+    k[::3, 8::2] = float("nan")
+    v[::3, 8::2, 0] = float("inf")
+    v[1::3, 20, :, 3] = float("inf")
+    table[5, 1], table[127, 0] = -1, call["k_cache"].shape[0]
+    got = tv.tree_attention(**dict(call, k_new=k, v_new=v, block_table=table)).double().cpu().numpy()
+    assert np.isnan(got[[5, 127]]).all()
+    keep = np.ones((batch, n1, heads, 64), bool)
+    keep[[5, 127]] = False
+    keep[::3, 8::2] = False
+    keep[1::3, 20::2, :, 3] = False
+    np.testing.assert_array_equal(got[keep], clean[keep])
+    others = [b for b in range(batch) if b not in (5, 127)]
+    assert np.isnan(got[[b for b in others if b % 3 == 0], 8::2]).all()
+    assert (got[[b for b in others if b % 3 == 1], 20::2, :, 3] == np.inf).all()
+
+
 def test_peaked_and_large_scores():
     """Scores of several hundred: one key holds nearly all of a row's weight."""
     host, call = inputs(3, 9, 4, 2, 64, 16, [100, 33, 5], scale_q=40.0)

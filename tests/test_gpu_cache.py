@@ -175,6 +175,32 @@ def test_commit_of_a_long_prompt():
     assert torch.equal(caches, want)
 
 
+def test_pages_beyond_32_bits():
+    """Pages 2^28 bytes apart: what is committed to far pages is what attention reads there."""
+    n1, KH, D_, ps, P, apart = 40, 2, 64, 16, 20, 1 << 27
+    far = [torch.empty((P - 1) * apart + KH * ps * D_, dtype=torch.bfloat16, device=DEV)
+           .as_strided((P, KH, ps, D_), (apart, ps * D_, D_, 1)) for _ in range(2)]
+    near = torch.zeros((2, P, KH, ps, D_), dtype=torch.bfloat16, device=DEV)
+    k, v = (torch.randn((1, 1, n1, KH, D_), device=DEV).bfloat16() for _ in range(2))
+    pages = torch.tensor([[19, 17, 8]], dtype=torch.int32, device=DEV)
+    at = torch.arange(n1, device=DEV)
+    slots = (pages[:, at // ps] * ps + at % ps).int()
+    n = torch.tensor([n1], dtype=torch.int32, device=DEV)
+    for caches in (far, near):
+        tv.cache_commit(k, v, caches[0][None], caches[1][None], n, slots)
+    out = []
+    for caches in (far, near):
+        q = torch.arange(5 * 4 * D_, device=DEV).view(1, 5, 4, D_).sin().bfloat16()
+        new = torch.arange(5 * KH * D_, device=DEV).view(1, 5, KH, D_).cos().bfloat16()
+        parents = torch.tensor([[-1, 0, 0, 2, 1]], dtype=torch.int32, device=DEV)
+        out.append(tv.tree_attention(q, new, new, parents, caches[0], caches[1], pages, n, 0.1))
+    for p in pages[0].tolist():
+        for c in range(2):
+            m = n1 - 32 if p == 8 else ps
+            assert torch.equal(far[c][p, :, :m], near[c][p, :, :m])
+    assert torch.equal(*out) and bool(out[0].isfinite().all())
+
+
 def test_calls_on_a_given_stream():
     """Everything that a call allocates belongs to the stream that it is given: work that the
     current stream starts meanwhile, on memory of the same sizes, changes no result."""

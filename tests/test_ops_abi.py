@@ -143,6 +143,8 @@ def call_commit(**kw):
     (dict(node_stride=264), UNS), (dict(page_stride=4104), UNS), (dict(new_layer_stride=24), UNS),
     (dict(layers=tv.TV_MAX_LAYERS + 1), UNS), (dict(max_new=tv.TV_MAX_NEW + 1), UNS),
     (dict(num_pages=1 << 27), UNS),
+    (dict(cache_layer_stride=0), BAD), (dict(cache_layer_stride=4080), BAD),
+    (dict(cache_layer_stride=-2048), BAD),
 ])
 def test_commit_refusals(kw, want):
     assert call_commit(**kw) == want
