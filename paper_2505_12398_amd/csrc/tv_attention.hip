@@ -17,9 +17,9 @@
 //
 // Keys and values come through LDS, in 16-key halves (a page holds whole halves)
 // by buffer loads that write LDS directly, chunks of 16 bytes of row r at position
-// c ^ f(r) so that the reads touch all banks. A workgroup of four wavefronts has RW
-// row groups of 16 MT rows and KW = 4 / RW groups of keys, which take the tiles in
-// turn and are merged at the end.
+// c ^ f(r) so that the reads touch all banks. A workgroup has RW row groups of 16 MT
+// rows, a wavefront each: one with four groups of keys, which take the tiles in turn
+// and are merged at the end, or two or four that share every tile.
 //
 // Work. The tiles of all trees and key heads form one line that is cut into equal
 // parts, so ragged contexts keep every CU as busy as equal ones. A part is taken by
@@ -53,9 +53,9 @@ constexpr int kKeys = 32, kHalf = 16;     // keys of a tile and of a half
 constexpr int kXcds = 8, kMaxCus = 256;
 constexpr int kWavesPerCu = 8;            // resident wavefronts, two on a SIMD
 constexpr int kMaxTeam = 32;              // workgroups of a team: the CUs of an XCD
-// Of a part: smaller parts use more CUs and leave more to merge. One tree of 65 nodes on
-// a context of 1024: parts of 4 / 8 / 16 / 32 tiles 33 / 34 / 41 / 50 us; 16 trees of 24
-// on 4096: 8 / 16 / 32 88 / 88 / 69.
+// Of a part: smaller parts use more CUs and leave more to merge. One tree of 65 nodes by
+// rows of 96, parts of 2 / 4 / 8 / 16 tiles: 41 / 34 / 36 / 42 us (parts merged one after
+// the other), 8 / 16 / 32: 34 / 41 / 50 (eight at a time); by rows of 48, 8 / 16: 32 / 33.
 constexpr int kMinTiles = 8;
 // Up to how many nodes the rows' paths are kept as words (in LDS, 32 bytes a node): 256
 // trees of 65 nodes 885 us, walked per tile 895.
