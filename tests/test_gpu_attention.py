@@ -394,3 +394,69 @@ def test_offsets_beyond_32_bits():
     near = tv.tree_attention(*args, near_k, near_v,
                              torch.arange(4, dtype=torch.int32, device=DEV)[None], ctx, 0.088)
     assert torch.equal(far, near) and not torch.isnan(far).any()
+
+
+
+def rounded_weights_tolerance(host, call, b, i, h, dtype, extra=0.0):
+    """Where the sum of the weights is that of the rounded ones, sum w (1 + d) v / sum w (1 + d)
+    differs from the exact out by at most half a step of sum p |v - out|; the output's own
+    rounding; fp32 as in ``tolerance``; fp16 weights below 2^-21 of the largest are rounded to
+    multiples of 2^-31 of it at worst: half of that a key, of |v - out|."""
+    see = sorted(D.path(host["parents"][b], i))
+    ctx = int(host["ctx"][b])
+    kh = h // (host["q"].shape[2] // host["k_new"].shape[2])
+    k = np.concatenate([D.cached(host["k_cache"], host["table"][b], ctx), host["k_new"][b][see]])[:, kh]
+    v = np.concatenate([D.cached(host["v_cache"], host["table"][b], ctx), host["v_new"][b][see]])[:, kh]
+    s = call["scale"] * (k @ host["q"][b, i, h])
+    p = np.exp(s - s.max())
+    p /= p.sum()
+    out = p @ v
+    half, fp = torch.finfo(TYPES[dtype]).eps / 2, 2.0 ** -24
+    big = call["scale"] * (np.abs(k) @ np.abs(host["q"][b, i, h])).max()
+    far = np.abs(v - out)
+    tol = half * np.abs(out) + 1.1 * half * (p @ far) + \
+        (4 * (k.shape[1] + 8) * fp * big + 16 * fp + 2 * len(s) * fp) * (p @ np.abs(v))
+    if dtype == "f16":
+        tol = tol + 1.1 * 2.0 ** -32 * far.sum(0) * p.max() + 2.0 ** -25
+    return out, tol + extra
+
+
+def one_request(ctx, scores, values, dtype, dim=64, heads=2, seed=0):
+    """A single token on a context whose keys have these scores (natural) and values [ctx, dim];
+    its own key's score is that of the lowest."""
+    host, call = inputs(1, 1, heads, 1, dim, 64, [ctx], dtype, seed=seed)
+    dt = TYPES[dtype]
+    # two dimensions hold a score: what one rounds away is in the other
+    q = torch.zeros((1, 1, heads, dim), dtype=dt)
+    q[..., 0] = q[..., 1] = 8.0
+    s = torch.tensor(np.append(scores, min(scores))) / (8.0 * call["scale"])
+    k = torch.zeros((ctx + 1, dim), dtype=dt)
+    k[:, 0] = s.to(dt)
+    k[:, 1] = (s - k[:, 0].double()).to(dt)
+    kc, vc = call["k_cache"].cpu(), call["v_cache"].cpu()
+    for x in range(ctx):
+        page = int(host["table"][0, x // 64])
+        kc[page, :, x % 64] = k[x]
+        vc[page, :, x % 64] = torch.as_tensor(values[x]).to(dt)
+    call.update(q=q.to(DEV), k_cache=kc.to(DEV), v_cache=vc.to(DEV),
+                k_new=k[None, None, None, ctx].to(DEV),
+                v_new=torch.zeros((1, 1, 1, dim), dtype=dt, device=DEV))
+    host.update(q=q.double().numpy(), **{n: call[n].double().cpu().numpy()
+                                         for n in ("k_cache", "v_cache", "k_new", "v_new")})
+    return host, call
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("above", [3.1, 4.3, 5.4])
+def test_a_key_that_holds_nearly_all_weight(dtype, above):
+    """Its weight in the frame of a smaller, earlier maximum is no power of two; the output is its
+    value all the same, to the output's own rounding and the others' share."""
+    rng = np.random.default_rng(2)
+    scores = rng.uniform(-20.0, -15.0, 200)
+    scores[0], scores[150] = -above, 0.0
+    host, call = one_request(200, scores + 12.0, rng.normal(0, 1, (200, 64)), dtype)
+    got = tv.tree_attention(**call).double().cpu().numpy()
+    for h in range(2):
+        want, tol = rounded_weights_tolerance(host, call, 0, 0, h, dtype)
+        err = np.abs(got[0, 0, h] - want)
+        assert (err <= tol).all(), float((err / tol).max())
