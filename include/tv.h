@@ -378,7 +378,8 @@ int tv_commit_paths(int32_t batch, int32_t num_nodes, const int32_t* parents,
  * [batch][table_width]; ctx_len int32 [batch], negative for a tree that takes
  * no part: its outputs are left as they were. Sums are formed in fp32 from
  * products on the matrix cores; weights are rounded to dtype before they
- * multiply values and are summed.
+ * multiply values and are summed (in fp16 those below 2^-21 of a row's largest
+ * to multiples of 2^-31 of it).
  *
  * A common prefix: the first prefix_len positions (a multiple of page_size, 0
  * for none) lie on the same pages for every tree with ctx_len >= prefix_len.

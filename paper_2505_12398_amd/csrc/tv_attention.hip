@@ -12,7 +12,7 @@
 //
 // The frame is a maximum seen so far; it moves only once some score exceeds it by
 // 8 in powers of two, so that most tiles rescale nothing (weights up to 2^8 in
-// their frame; sums in fp32). Weights are rounded to the type of the values, the
+// their frame, and 2^15 for fp16, which has few exponents below 1; sums in fp32). Weights are rounded to the type of the values, the
 // operand type of the product, and summed as rounded: the quotient is off by at most
 // half a step of sum p |v - out|, and nothing where one key holds all weight.
 //
@@ -94,6 +94,7 @@ struct Bf16 {
   }
   static __device__ __forceinline__ float value(uint16_t x) { return __uint_as_float(uint32_t{x} << 16); }
   static constexpr uint32_t kExponent = 0x7f80;
+  static constexpr float kLift = 0.0f;
 };
 struct F16 {
   static __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c) {
@@ -111,6 +112,10 @@ struct F16 {
     return static_cast<float>(__builtin_bit_cast(_Float16, x));
   }
   static constexpr uint32_t kExponent = 0x7c00;
+  // Weights of up to 2^15 (the largest fp16 is below 2^16): those below 2^-21 of the largest
+  // are rounded to multiples of 2^-31 of it. Without the lift these are 2^-14 and 2^-24, and
+  // 30000 keys at e^-18 of one key's weight lost 51% of what they add.
+  static constexpr float kLift = 7.0f;
 };
 
 // One pass: the trees over their own positions, or all their rows over the prefix.
@@ -230,16 +235,18 @@ __device__ __forceinline__ void unrolled(F&& f) {
   unrolled(f, std::make_integer_sequence<int, N>{});
 }
 
-// The frame of a maximum, -m k (0 where there is none), rounded by itself: sums are
-// moved between frames by the differences of these.
+// The frame of a maximum, -m k and the type's lift (0 where there is none), rounded by
+// itself: sums are moved between frames by the differences of these.
+template <class T>
 __device__ __forceinline__ float frame(float m, float k) {
 #pragma clang fp contract(off)
-  return m > -INFINITY ? -m * k : 0.0f;
+  return m > -INFINITY ? -m * k + T::kLift : 0.0f;
 }
 // What takes a sum from the frame of m to that of top >= m. (0 where nothing was
 // seen; a sum that is NaN stays NaN.)
+template <class T>
 __device__ __forceinline__ float to_frame(float m, float top, float k) {
-  return m > -INFINITY ? __builtin_amdgcn_exp2f(frame(top, k) - frame(m, k)) : 0.0f;
+  return m > -INFINITY ? __builtin_amdgcn_exp2f(frame<T>(top, k) - frame<T>(m, k)) : 0.0f;
 }
 
 // Positions of tree b that this pass reads from pages, where they start, and whether
@@ -675,9 +682,9 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
           float u = fmaxf(m[mt], top[mt]);
           u = fmaxf(u, __shfl_xor(u, 16, 64));
           u = fmaxf(u, __shfl_xor(u, 32, 64));
-          const float f = to_frame(m[mt], u, P.k);
+          const float f = to_frame<T>(m[mt], u, P.k);
           m[mt] = u;
-          c[mt] = frame(u, P.k);
+          c[mt] = frame<T>(u, P.k);
           l[mt] *= f;
 #pragma unroll
           for (int db = 0; db < DB; ++db) acc[db][mt] *= f;
@@ -876,14 +883,14 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
           o[j] = *(const LDS(f32x2)*)(lds + SH::ACC + (((j - 1) * RW + rg) * MT + mt) * 512 + el * 8);
           top = fmaxf(top, o[j][0]);
         }
-        const float f = to_frame(m[mt], top, P.k);
+        const float f = to_frame<T>(m[mt], top, P.k);
         m[mt] = top;
         l[mt] *= f;
 #pragma unroll
         for (int db = 0; db < DB; ++db) acc[db][mt] *= f;
 #pragma unroll
         for (int j = 1; j < KW; ++j) {
-          const float fj = to_frame(o[j][0], top, P.k);
+          const float fj = to_frame<T>(o[j][0], top, P.k);
           l[mt] += o[j][1] * fj;
 #pragma unroll
           for (int db = 0; db < DB; ++db) {
@@ -921,7 +928,7 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
               for (int db = 0; db < DB; ++db)
                 pre[db] = *reinterpret_cast<const f32x4*>(P.pre + row * SH::DP + 16 * db + 4 * eg);
               const float both = fmaxf(m[mt], ml[0]);
-              const float own = to_frame(m[mt], both, P.k), theirs = to_frame(ml[0], both, P.k);
+              const float own = to_frame<T>(m[mt], both, P.k), theirs = to_frame<T>(ml[0], both, P.k);
               l[mt] = l[mt] * own + ml[1] * theirs;
 #pragma unroll
               for (int db = 0; db < DB; ++db) acc[db][mt] = acc[db][mt] * own + pre[db] * theirs;
@@ -987,7 +994,7 @@ __global__ void __launch_bounds__(64 * kMergeWaves) merge_kernel(Pass P) {
     float top = m;
 #pragma unroll
     for (int j = 0; j < kMergeAhead; ++j) top = fmaxf(top, ml[j][0]);
-    const float f = to_frame(m, top, P.k);
+    const float f = to_frame<T>(m, top, P.k);
     m = top;
     l *= f;
 #pragma unroll
@@ -995,7 +1002,7 @@ __global__ void __launch_bounds__(64 * kMergeWaves) merge_kernel(Pass P) {
 #pragma unroll
     for (int j = 0; j < kMergeAhead; ++j) {
       if (i0 + j >= count) continue;
-      const float fj = to_frame(ml[j][0], top, P.k);
+      const float fj = to_frame<T>(ml[j][0], top, P.k);
       l += ml[j][1] * fj;
       odd |= flag[j] != 0.0f;
 #pragma unroll
@@ -1016,7 +1023,7 @@ __global__ void __launch_bounds__(64 * kMergeWaves) merge_kernel(Pass P) {
   const bool shared = P.prefix_len > 0 && P.ctx_len[b] >= P.prefix_len;
   if (shared) ml = P.pre_ml[row];
   const float both = fmaxf(m, ml[0]);
-  const float own = to_frame(m, both, P.k), pre = to_frame(ml[0], both, P.k);
+  const float own = to_frame<T>(m, both, P.k), pre = to_frame<T>(ml[0], both, P.k);
   const float inv = 1.0f / (l * own + ml[1] * pre);
   if (shared)
 #pragma unroll

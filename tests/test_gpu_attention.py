@@ -396,7 +396,6 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(far, near) and not torch.isnan(far).any()
 
 
-
 def rounded_weights_tolerance(host, call, b, i, h, dtype, extra=0.0):
     """Where the sum of the weights is that of the rounded ones, sum w (1 + d) v / sum w (1 + d)
     differs from the exact out by at most half a step of sum p |v - out|; the output's own
@@ -460,3 +459,26 @@ def test_a_key_that_holds_nearly_all_weight(dtype, above):
         want, tol = rounded_weights_tolerance(host, call, 0, 0, h, dtype)
         err = np.abs(got[0, 0, h] - want)
         assert (err <= tol).all(), float((err / tol).max())
+
+
+@pytest.mark.parametrize("rows", [1, 65])
+@pytest.mark.parametrize("gap", [12.0, 16.0, 18.0])
+def test_a_key_far_above_many_others_in_fp16(gap, rows):
+    """30000 keys at e^-gap of the first one's weight: together they count, though each of them
+    is below the smallest fp16 number next to 1. The requests have the same context, and there
+    are so many of them that one workgroup takes all of a context."""
+    rng = np.random.default_rng(1)
+    n, batch = 30000, 600 if rows == 1 else 260
+    scores = np.append([gap], rng.uniform(-1.0, 0.0, n - 1))
+    values = np.concatenate([np.zeros((1, 64)), rng.uniform(0.5, 1.5, (n - 1, 64))])
+    host, call = one_request(n, scores, values, "f16")
+    for name in ("q", "k_new", "v_new"):
+        call[name] = call[name].repeat(batch, rows, 1, 1)
+    call["parents"] = torch.zeros((batch, rows), dtype=torch.int32, device=DEV) - 1
+    call["block_table"] = call["block_table"].repeat(batch, 1)
+    call["ctx_len"] = call["ctx_len"].repeat(batch)
+    got = tv.tree_attention(**call).double().cpu().numpy()
+    for h in range(2):
+        want, tol = rounded_weights_tolerance(host, call, 0, 0, h, "f16")
+        err = np.abs(got[:, :, h] - want)
+        assert (err <= tol).all(), (float(err.max()), float(tol.min()), float(want.min()))
