@@ -391,7 +391,8 @@ int tv_commit_paths(int32_t batch, int32_t num_nodes, const int32_t* parents,
  * A tree whose block table names a page outside [0, num_pages) for a position
  * below ctx_len, or whose ctx_len exceeds table_width * page_size, gets NaN in
  * every output. The order of a tree's sums, and so its last bits, depends on the
- * lengths of all trees of the call; the same call gives the same bits.
+ * lengths of all trees of the call, and on nothing else of the others; the same
+ * call gives the same bits.
  *
  * head_dim: a multiple of 8 up to TV_MAX_HEAD_DIM; heads a multiple of
  * kv_heads; heads * head_dim at most TV_MAX_HIDDEN; page_size a power of two

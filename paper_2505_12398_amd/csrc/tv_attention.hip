@@ -682,6 +682,8 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
           float u = fmaxf(m[mt], top[mt]);
           u = fmaxf(u, __shfl_xor(u, 16, 64));
           u = fmaxf(u, __shfl_xor(u, 32, 64));
+          // (a row whose own scores do not ask for it stays, whatever its neighbours' do)
+          u = u > m[mt] + P.slack ? u : m[mt];
           const float f = to_frame<T>(m[mt], u, P.k);
           m[mt] = u;
           c[mt] = frame<T>(u, P.k);

@@ -482,3 +482,19 @@ def test_a_key_far_above_many_others_in_fp16(gap, rows):
         want, tol = rounded_weights_tolerance(host, call, 0, 0, h, "f16")
         err = np.abs(got[:, :, h] - want)
         assert (err <= tol).all(), (float(err.max()), float(tol.min()), float(want.min()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_other_rows_scores_change_no_bits(dtype):
+    """A request's bits do not depend on what other requests of the call, or other nodes of its
+    tree, ask for: with and without a common prefix, at the same lengths."""
+    for n1, prefix in ((1, 0), (1, 256), (9, 0), (9, 256)):
+        host, call = inputs(6, n1, 8, 2, 64, 16, [prefix + 300] * 6, dtype, "star", prefix=prefix)
+        want = tv.tree_attention(**call)
+        q = call["q"].clone()
+        q[1::2] *= 30
+        assert torch.equal(tv.tree_attention(**dict(call, q=q))[::2], want[::2]), (n1, prefix)
+        q = call["q"].clone()
+        q[:, 1::2] *= 30
+        q[:, :, 1::2] *= 30
+        assert torch.equal(tv.tree_attention(**dict(call, q=q))[:, ::2, ::2], want[:, ::2, ::2])
