@@ -413,7 +413,7 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
   auto offset = [&](int ln, int i, int last, int stride) {
     const int r = i * kRowsPer + ln / SH::CH;
     const int c = ln % SH::CH ^ swizzle(r);
-    return 8 * c < P.head_dim ? min(r, last) * stride + 16 * c : kPastRange;
+    return 8 * c < P.head_dim && r <= last ? r * stride + 16 * c : kPastRange;
   };
   const int dbytes = P.head_dim * 2;
   // this wavefront's halves of a tile, and its loads of a half
@@ -549,8 +549,9 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
       }
     };
     // Where the tile to load lies: each half's keys, how much further the values are, its
-    // last row and the rows' distance. A tile behind the last has no range: its loads
-    // write zeros and read nothing, so that every round has the same loads in flight.
+    // last row (below 0: none) and the rows' distance. Rows behind the last are zeros: their
+    // weight 0 must not meet a value that is not finite. A tile behind the last has no range:
+    // its loads write zeros and read nothing, so that every round has the same loads in flight.
     uint64_t at_k[kHalves] = {};
     uint64_t to_v = 0;
     int last[kHalves] = {}, stride = dbytes, range = 0;
@@ -569,17 +570,18 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
         stride = dbytes;
 #pragma unroll
         for (int hh = 0; hh < kHalves; ++hh) {
-          const int key = min(first_key(t, h0 + hh), last_key);
-          last[hh] = last_key - key;                // rows past the context: its last one again
-          at_k[hh] = key_at(page[hh], key);
+          const int key = first_key(t, h0 + hh);
+          last[hh] = last_key - key;
+          at_k[hh] = key_at(page[hh], min(key, last_key));
         }
       } else if (t < tile_end) {                    // nodes, the last ones first
         to_v = reinterpret_cast<uint64_t>(P.v_new) - reinterpret_cast<uint64_t>(P.k_new);
         stride = static_cast<int>(P.kv_stride) * 2;
 #pragma unroll
         for (int hh = 0; hh < kHalves; ++hh) {
-          const int from = min((R.tiles - 1 - t) * kKeys + (h0 + hh) * kHalf, P.num_nodes - 1);
-          last[hh] = P.num_nodes - 1 - from;
+          const int half = (R.tiles - 1 - t) * kKeys + (h0 + hh) * kHalf;
+          const int from = min(half, P.num_nodes - 1);
+          last[hh] = P.num_nodes - 1 - half;
           at_k[hh] = reinterpret_cast<uint64_t>(
               P.k_new + (static_cast<int64_t>(b) * P.num_nodes + from) * P.kv_stride +
               kh * P.head_dim);

@@ -498,3 +498,20 @@ def test_other_rows_scores_change_no_bits(dtype):
         q[:, 1::2] *= 30
         q[:, :, 1::2] *= 30
         assert torch.equal(tv.tree_attention(**dict(call, q=q))[:, ::2, ::2], want[:, ::2, ::2])
+
+
+@pytest.mark.parametrize("n1", [1, 3, 65])
+@pytest.mark.parametrize("ctx", [1, 5, 31, 33, 48, 79])
+def test_infinite_last_value_of_a_context(n1, ctx):
+    """A value that is infinite at the last cached position is infinite in the output and in its
+    own dimension alone, wherever the context ends in a tile."""
+    host, call = inputs(2, n1, 4, 2, 64, 16, [ctx, ctx + 200])
+    clean = check(host, call)
+    v = call["v_cache"].clone()
+    for b in range(2):
+        x = int(host["ctx"][b]) - 1
+        v[int(host["table"][b, x // 16]), :, x % 16, 3] = float("inf")
+    got = tv.tree_attention(**dict(call, v_cache=v)).double().cpu().numpy()
+    assert (got[..., 3] == np.inf).all()
+    rest = [d for d in range(64) if d != 3]
+    assert np.array_equal(got[..., rest], clean[..., rest])
