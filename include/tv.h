@@ -384,9 +384,9 @@ int tv_commit_paths(int32_t batch, int32_t num_nodes, const int32_t* parents,
  * A common prefix: the first prefix_len positions (a multiple of page_size, 0
  * for none) lie on the same pages for every tree with ctx_len >= prefix_len.
  * They are read once for the batch, from prefix_pages int32
- * [prefix_len / page_size] (any such tree's row of the block table will do),
- * and those trees' own entries for them are not read. A tree with a shorter
- * context is computed from its own entries alone.
+ * [prefix_len / page_size], and those trees' own entries for them are not read;
+ * prefix_pages = block_table stands for the row of the first such tree. A tree
+ * with a shorter context is computed from its own entries alone.
  *
  * A tree whose block table names a page outside [0, num_pages) for a position
  * below ctx_len, or whose ctx_len exceeds table_width * page_size, gets NaN in

@@ -471,8 +471,8 @@ def tree_attention(q, k_new, v_new, parents, k_cache, v_cache, block_table, ctx_
     [B, N+1, kv_heads, D] (bfloat16 or float16; views of one projection's output
     will do), k_cache and v_cache [pages, kv_heads, page_size, D], block_table
     [B, width] and ctx_len [B] int32. ``prefix_pages`` [prefix_len / page_size]
-    int32 are the pages of the common prefix (default: those of tree 0). Returns
-    out [B, N+1, heads, D]; raises on a non-OK return."""
+    int32 are the pages of the common prefix (default: those of the first tree that
+    has it). Returns out [B, N+1, heads, D]; raises on a non-OK return."""
     import torch
     if q.dim() != 4 or k_new.dim() != 4 or k_cache.dim() != 4:
         raise ValueError("q, k_new, v_new and the caches have four dimensions")
@@ -488,13 +488,13 @@ def tree_attention(q, k_new, v_new, parents, k_cache, v_cache, block_table, ctx_
     page_stride = _pages("k_cache", k_cache, dev, dt, (P, KH, ps, D))
     if _pages("v_cache", v_cache, dev, dt, (P, KH, ps, D)) != page_stride:
         raise ValueError("k_cache and v_cache must have the same strides")
-    if prefix_len and prefix_pages is None and B:
-        prefix_pages = block_table[0, :prefix_len // ps]
     width = block_table.shape[-1]
     parents = _check("parents", parents, (B, n1), i32, dev)
     table = _check("block_table", block_table, (B, width), i32, dev)
     ctx = _check("ctx_len", ctx_len, (B,), i32, dev)
     prefix = _check("prefix_pages", prefix_pages, (prefix_len // ps,), i32, dev)
+    if prefix_len and prefix_pages is None:
+        prefix = table
     lib = load_library()
     with _On(dev, stream) as at:
         if out is None:

@@ -127,7 +127,8 @@ struct Pass {
   const uint16_t* v_cache;
   const int32_t* parents;
   const int32_t* table;
-  const int32_t* ctx_len;       // NULL in the prefix pass
+  const int32_t* ctx_len;       // in the prefix pass NULL, or that of `trees` trees: the table's
+  int trees;                    // row of the first one that has the prefix names its pages
   uint16_t* out;
   int64_t q_stride, kv_stride, page_stride;
   int num_pages, page_shift, table_width;
@@ -433,6 +434,19 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
   // the next node on the path of each of this wavefront's rows
   LDS(int16_t)* const walk = (LDS(int16_t)*)(lds + SH::WALK) + wave * 16 * MT;
 
+  int table_row = 0;            // of the prefix
+  if (P.prefix_pass && P.ctx_len) {
+    for (int b0 = 0; b0 < P.trees; b0 += 64) {
+      const int at = min(b0 + lane, P.trees - 1);
+      const uint64_t has = __builtin_amdgcn_ballot_w64(P.ctx_len[at] >= P.prefix_len);
+      if (has) {
+        table_row = min(b0 + __builtin_ctzll(has), P.trees - 1);
+        break;
+      }
+    }
+    table_row = uniform(table_row);
+  }
+
   bool opened = false;
   int word_tree = -1, word_chunk = -1;   // whose words are there
   for (long long pos = begin; pos < end;) {
@@ -528,7 +542,7 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
 
     // Loads of tile t: this wavefront's part of its keys (0) and values (1).
     CONSTANT(int)* const pages =
-        (CONSTANT(int)*)(P.table + static_cast<size_t>(b) * P.table_width);
+        (CONSTANT(int)*)(P.table + static_cast<size_t>(b + table_row) * P.table_width);
     uint32_t worst = 0;           // the largest page number seen
     bool odd = false;             // a node's value that is not finite
     const int ring = kg * SH::S * SH::STAGE;
@@ -1189,8 +1203,9 @@ int launch_attention(const AttentionArgs& a, void* workspace, hipStream_t stream
   P.head_dim = a.head_dim;
   P.group = a.heads / a.kv_heads;
   P.rows = a.num_nodes * P.group;
-  // (without pages a tree that has a context has bad ones, the prefix among them)
-  P.prefix_len = a.num_pages > 0 ? a.prefix_len : 0;
+  // (without pages a tree that has a context has bad ones, the prefix among them, and so has
+  // a tree with a prefix that its table cannot hold)
+  P.prefix_len = a.num_pages > 0 && a.prefix_len <= a.table_width * a.page_size ? a.prefix_len : 0;
   P.k = static_cast<float>(static_cast<double>(a.scale) * 1.4426950408889634);
   const double slack = 8.0 / static_cast<double>(P.k);
   P.slack = slack < 3.0e38 ? static_cast<float>(slack) : 3.0e38f;
@@ -1204,6 +1219,11 @@ int launch_attention(const AttentionArgs& a, void* workspace, hipStream_t stream
     X.table = a.prefix_pages;
     X.table_width = 0;
     X.ctx_len = nullptr;
+    if (a.prefix_pages == a.block_table) {
+      X.table_width = a.table_width;
+      X.ctx_len = a.ctx_len;
+      X.trees = a.batch;
+    }
     X.parents = nullptr;
     X.batch = 1;
     X.num_nodes = a.batch * a.num_nodes;

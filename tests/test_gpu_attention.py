@@ -515,3 +515,30 @@ def test_infinite_last_value_of_a_context(n1, ctx):
     assert (got[..., 3] == np.inf).all()
     rest = [d for d in range(64) if d != 3]
     assert np.array_equal(got[..., rest], clean[..., rest])
+
+
+def test_default_prefix_pages_are_those_of_a_tree_that_has_the_prefix():
+    """The first trees of a batch may take no part or have shorter contexts."""
+    for first in (1, 3, 70):
+        ctx = [-1, 20, 0] + [63] * 67
+        ctx = ctx[:first] + [64 + 30, 64, 64 + 5, 10, 64 + 77]
+        host, call = inputs(len(ctx), 3, 4, 2, 64, 16, ctx, prefix=64)
+        check(host, call)
+    none = dict(call, ctx_len=call["ctx_len"].clamp(max=63))
+    host["ctx"] = np.minimum(host["ctx"], 63)
+    check(host, none)
+
+
+def test_prefix_longer_than_the_table():
+    """No tree can have it: contexts the table holds are computed, longer ones have bad pages."""
+    host, call = inputs(3, 3, 4, 2, 64, 16, [40, 64, 5])
+    width = call["block_table"].shape[1]
+    lens = call["ctx_len"].clone()
+    lens[1] = (width + 2) * 16
+    far = torch.zeros(width + 1, dtype=torch.int32, device=DEV)
+    for pages in (None, far):
+        got = tv.tree_attention(**dict(call, ctx_len=lens, prefix_len=(width + 1) * 16),
+                                prefix_pages=pages)
+        assert torch.isnan(got[1]).all()
+        host["ctx"][1] = -1
+        check(host, call, out=got)
