@@ -396,9 +396,11 @@ int tv_commit_paths(int32_t batch, int32_t num_nodes, const int32_t* parents,
  *
  * head_dim: a multiple of 8 up to TV_MAX_HEAD_DIM; heads a multiple of
  * kv_heads; heads * head_dim at most TV_MAX_HIDDEN; page_size a power of two
- * from TV_MIN_PAGE to TV_MAX_PAGE; scale positive and finite; q, k_new, v_new,
- * caches and out 16-byte aligned, strides multiples of 8; the nodes of a tree,
- * and the distance of two pages, at most 2^29 bytes; batch * num_nodes * heads at most 2^31 - 1.
+ * from TV_MIN_PAGE to TV_MAX_PAGE; scale positive and at most 2^127, scores s
+ * of up to 2^22 either way (beyond them an fp32 exponent does not tell weights
+ * apart, and a row may be NaN); q, k_new, v_new, caches and out 16-byte aligned,
+ * strides multiples of 8; the nodes of a tree, and the distance of two pages, at
+ * most 2^29 bytes; batch * num_nodes * heads at most 2^31 - 1.
  * out dtype [batch][num_nodes][heads][head_dim]. workspace:
  * tv_tree_attention_workspace_size() bytes (0 for invalid sizes), 256-byte
  * aligned. Nothing is allocated. Returns a tv_status_t; argument errors

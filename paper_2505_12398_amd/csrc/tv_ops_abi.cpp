@@ -19,6 +19,7 @@ bool page_size_ok(int32_t page_size) {
 }
 
 constexpr int64_t kMaxBytes = int64_t{1} << 29;   // of a tree's nodes, and of a page
+constexpr float kMaxScale = 0x1p127f;             // its product with log2(e) is finite
 
 // TV_OK if an attention call of these sizes is taken
 int attention_sizes(int32_t batch, int32_t num_nodes, int32_t heads, int32_t kv_heads,
@@ -40,7 +41,7 @@ int validate(const tv::AttentionArgs& a, void* workspace, size_t workspace_bytes
   if (a.dtype != TV_DTYPE_BF16 && a.dtype != TV_DTYPE_F16) return TV_ERR_INVALID_ARG;
   if (a.num_pages < 0 || a.page_size < 1 || a.table_width < 0) return TV_ERR_INVALID_ARG;
   if (!(a.scale > 0.0f) || !isfinite(a.scale)) return TV_ERR_INVALID_ARG;
-  if (!page_size_ok(a.page_size)) return TV_ERR_UNSUPPORTED;
+  if (!page_size_ok(a.page_size) || a.scale > kMaxScale) return TV_ERR_UNSUPPORTED;
   if (a.prefix_len % a.page_size) return TV_ERR_INVALID_ARG;
   if (a.table_width > INT32_MAX / a.page_size) return TV_ERR_UNSUPPORTED;
   const int64_t kv_row = static_cast<int64_t>(a.kv_heads) * a.head_dim;

@@ -56,6 +56,12 @@ def test_attention_empty_batch_and_workspace_size():
     assert size(1, 5, 8, 2, 64, 0) > 0 and size(256, 65, 32, 8, 128, 64) % 256 == 0
 
 
+def test_attention_scale_whose_exponents_are_not_finite():
+    for scale in (3.4e38, 2.4e38, 1.8e38):
+        assert call_attention(scale=scale) == UNS
+    assert call_attention(scale=2.0 ** 127, workspace=None) == WSP
+
+
 def call_logits(**kw):
     args = dict(batch=2, num_nodes=5, vocab=1000, first_node=0, num_rows=5, logits=A,
                 dtype=tv.TV_DTYPE_BF16, temperature=1.0, parents=A, tokens=A, history=A,
