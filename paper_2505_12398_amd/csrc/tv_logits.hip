@@ -113,14 +113,20 @@ __device__ __forceinline__ float where_bit(uint32_t bits, int e, float x, float 
 }
 
 struct Penalties {
-  float rho, inv, alpha, beta;
+  float rho, alpha, beta;
+  float up, div, inv;   // a power of two, rho up, 1 / (rho up): rho may be any positive number
 };
+__device__ __forceinline__ Penalties penalties(float rho, float alpha, float beta) {
+  const float up = rho < 0x1p-100f ? 0x1p64f : rho > 0x1p100f ? 0x1p-64f : 1.0f;
+  return {rho, alpha, beta, up, rho * up, 1.0f / (rho * up)};
+}
 
-// z / rho or z * rho. The quotient is the product with 1 / rho corrected by its
-// own remainder, which rounds as the division does.
+// z / rho or z * rho. The quotient is the product with the reciprocal, at most the largest
+// number, corrected by its own remainder: it rounds as the division does, to infinity too
+// (but for the last bit of subnormal quotients).
 __device__ __forceinline__ float repeated(float z, const Penalties& p) {
-  const float q = z * p.inv;
-  const float d = __builtin_amdgcn_div_fixupf(fmaf(fmaf(-q, p.rho, z), p.inv, q), p.rho, z);
+  const float n = z * p.up, q = fminf(n * p.inv, 0x1.fffffep127f);
+  const float d = fmaf(fmaf(-q, p.div, n), p.inv, q);
   return z > 0.0f ? d : z * p.rho;
 }
 
@@ -152,9 +158,9 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) logits_kerne
   const int slab = rest % P.slabs, b = rest / P.slabs;
   const int V = a.vocab, n1 = a.num_nodes;
   const int base = chunk * kChunk, width = min(kChunk, V - base);
-  const Penalties pen = {a.repetition ? a.repetition[b] : 1.0f,
-                         1.0f / (a.repetition ? a.repetition[b] : 1.0f),
-                         a.presence ? a.presence[b] : 0.0f, a.frequency ? a.frequency[b] : 0.0f};
+  const Penalties pen = penalties(a.repetition ? a.repetition[b] : 1.0f,
+                                  a.presence ? a.presence[b] : 0.0f,
+                                  a.frequency ? a.frequency[b] : 0.0f);
   auto clear = [&] {
     for (int i = tid; i < kChunk / 4; i += kThreads)
       *reinterpret_cast<u32x4*>(&words[4 * i]) = u32x4{0, 0, 0, 0};

@@ -327,3 +327,46 @@ def test_statistics_feed_the_verifier():
     a = parity.host_outputs(tv.verify_batch(*args, stats=(tm, ts, dm, ds)))
     rep = parity.check(dict(bt, target=target, draft=draft), False, gpu=a, label="processed")
     assert not rep.failures, rep.failures[:3]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_penalised_quotients_are_those_of_a_division(dtype):
+    """z / repetition for repetitions below and above 1 and down to subnormal ones, at logits up
+    to the largest: as the host divides, infinite where that is."""
+    rng = np.random.default_rng(4)
+    rho = np.array([0.7, 0.999, 1e-3, 1e-20, 1e-37, 1e-40, 3e-45, 1.0, 1.3, 7.0, 1e10, 2e38],
+                   np.float32)
+    top = torch.finfo(dtype).max
+    z = np.concatenate([rng.normal(0, 4, 40), 10.0 ** rng.uniform(-20, 38.4, 40),
+                        [3e38, top, top * 0.7, 1e-10, 2.0, 0.0, -0.0]])
+    z = torch.tensor(np.repeat(z[None, None], len(rho), 0)).to(dtype).to(DEV)
+    V = z.shape[-1]
+    hist = torch.arange(V, dtype=torch.int32, device=DEV).repeat(len(rho), 1)
+    n = torch.full((len(rho),), V, dtype=torch.int32, device=DEV)
+    out, mx, _ = tv.process_logits(z, 1.0, history=hist, history_len=n, prompt_len=n,
+                                   repetition=torch.tensor(rho, device=DEV))
+    x = z.float().cpu().numpy()
+    with np.errstate(over="ignore"):
+        want = np.where(x > 0, x / rho[:, None, None], x * rho[:, None, None]).astype(np.float32)
+    want = torch.tensor(want).to(dtype)
+    # (quotients that are no normal numbers are not claimed to the bit)
+    small = want.double().abs() < 2.0 ** -126
+    got = out.cpu()
+    assert torch.equal(got[~small], want[~small])
+    assert (got.double()[small] - want.double()[small]).abs().max() <= 2.0 ** -126 * \
+        torch.finfo(dtype).eps
+    assert torch.equal(mx.cpu(), want.float().amax(-1))
+
+
+def test_penalised_quotients_on_the_path():
+    """The same for tokens that a node's path has."""
+    z = torch.tensor([[[3e38, 3e38, 1.0, 1e-10]] * 2] * 2, device=DEV)
+    par = torch.tensor([[-1, 0]] * 2, dtype=torch.int32, device=DEV)
+    rho = torch.tensor([0.7, 1e-40], device=DEV)
+    for t in range(4):
+        tok = torch.tensor([[0, t]] * 2, dtype=torch.int32, device=DEV)
+        out, _, _ = tv.process_logits(z, 1.0, parents=par, tokens=tok, repetition=rho)
+        with np.errstate(over="ignore"):
+            want = z.cpu().numpy().copy()
+            want[:, 1, t] = want[:, 1, t] / rho.cpu().numpy()
+        assert np.array_equal(out.cpu().numpy(), want)
