@@ -15,7 +15,10 @@
 //
 // The statistics are a maximum and a sum of 2^((z - max) k), k = log2(e)/T, per
 // wavefront and row, in fp32 in the frame of the maximum; a second kernel merges
-// them in fp64.
+// them in fp64. The frame is the product -max k as rounded, which z k - max k (one
+// instruction) is off by alike, unless that product is so large that its rounding
+// moves the exponents themselves, as where all of a wavefront's tokens are masked with
+// a large negative number: from 2^20 on the difference is taken first.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -31,6 +34,7 @@ constexpr int kChunk = tv::kLogitsChunk;
 constexpr int kGroups = kChunk / (8 * kThreads);   // groups of 8 consecutive tokens of a thread
 constexpr int kOwn = 8 * kGroups;                  // tokens of a thread
 static_assert(kOwn == 32, "a thread's tokens are the bits of a word");
+constexpr float kFrames = 0x1p20f;                 // below it the frame is the rounded product
 constexpr uint32_t kTold = 0x80000000u;            // in the prompt; below it the count
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
@@ -118,7 +122,11 @@ struct Penalties {
 };
 __device__ __forceinline__ Penalties penalties(float rho, float alpha, float beta) {
   const float up = rho < 0x1p-100f ? 0x1p64f : rho > 0x1p100f ? 0x1p-64f : 1.0f;
-  return {rho, alpha, beta, up, rho * up, 1.0f / (rho * up)};
+  auto uniform = [](float x) {
+    return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x)));
+  };
+  return {uniform(rho), uniform(alpha), uniform(beta),
+          uniform(up),  uniform(rho * up), uniform(1.0f / (rho * up))};
 }
 
 // z / rho or z * rho. The quotient is the product with the reciprocal, at most the largest
@@ -370,12 +378,14 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) logits_kerne
       }
     mx = over_wave(mx, [](float x, float y) { return fmaxf(x, y); });
     // a row with no finite value keeps the frame 0, so its terms are 0 as well
-    const float c = mx > -INFINITY ? -mx * P.k32 : 0.0f;
+    const float f = mx > -INFINITY ? -mx * P.k32 : 0.0f;
+    const bool near = fabsf(f) < kFrames;
+    const float from = near ? 0.0f : mx, c = near ? f : 0.0f;
     float s = 0.0f;
 #pragma unroll
     for (int g = 0; g < kGroups; ++g)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s += __builtin_amdgcn_exp2f(fmaf(v[g][e], P.k32, c));
+      for (int e = 0; e < 8; ++e) s += __builtin_amdgcn_exp2f(fmaf(v[g][e] - from, P.k32, c));
     s = over_wave(s, [](float x, float y) { return x + y; });
     if (lane == 0) {
       const size_t part = (row * P.chunks + chunk) * kWaves + wave;
@@ -385,8 +395,14 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) logits_kerne
   }
 }
 
-// Merges a row's partials, a wavefront a row: each moves from its frame, the fp32
-// product -max k, to that of the row's maximum.
+// The frame of a sum: the rounded product, or the exact one (see above).
+__device__ __forceinline__ double frame_of(float m, float k) {
+  const float c = -m * k;
+  return fabsf(c) < kFrames ? static_cast<double>(c) : -static_cast<double>(m) * static_cast<double>(k);
+}
+
+// Merges a row's partials, a wavefront a row: each moves from its frame to that of the
+// row's maximum.
 __global__ void __launch_bounds__(kThreads) logits_merge_kernel(Params P) {
   const tv::LogitsArgs& a = P.a;
   const int lane = threadIdx.x & 63;
@@ -401,12 +417,12 @@ __global__ void __launch_bounds__(kThreads) logits_merge_kernel(Params P) {
   for (int t = lane; t < parts; t += 64) m = fmaxf(m, pm[t]);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  const double cm = static_cast<double>(-m * P.k32);
+  const double cm = frame_of(m, P.k32);
   double s = 0.0;
   for (int t = lane; t < parts; t += 64) {
     const float mt = pm[t];
     const double st = static_cast<double>(ps[t]);
-    s += mt > -INFINITY ? st * exp2(cm - static_cast<double>(-mt * P.k32)) : st;
+    s += mt > -INFINITY ? st * exp2(cm - frame_of(mt, P.k32)) : st;
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);

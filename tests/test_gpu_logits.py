@@ -370,3 +370,37 @@ def test_penalised_quotients_on_the_path():
             want = z.cpu().numpy().copy()
             want[:, 1, t] = want[:, 1, t] / rho.cpu().numpy()
         assert np.array_equal(out.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T", [1.0, 0.05, 1e-3, 1e3])
+@pytest.mark.parametrize("low", [-1e9, -3e10, -1e20, -1e30, -1e37, -3.3e38, None])
+def test_statistics_of_rows_masked_with_low_values(dtype, T, low):
+    """Masks by a large negative number, down to the type's lowest: on part of a row, in whole
+    wavefronts' and workgroups' parts, in all of it. Terms as in ``check``: exponents of finite
+    range here (a masked entry's is below -800 next to one that is not)."""
+    V = 20003
+    rng = np.random.default_rng(6)
+    low = torch.finfo(dtype).min if low is None else low
+    z = torch.tensor(rng.normal(0, 1, (1, 8, V)))
+    z[0, 0, ::3] = low
+    z[0, 1, :9000] = low
+    z[0, 2, 5:] = low
+    z[0, 3, :-1] = low
+    z[0, 4] = low
+    z[0, 5] = low
+    z[0, 5, 8192:8200] = -math.inf
+    z[0, 6] = low
+    z[0, 6, 17] = low * 0.5
+    z[0, 7, 9000] = -low
+    z = z.to(dtype).to(DEV)
+    out, mx, sm = tv.process_logits(z, T)
+    assert torch.equal(out, z)
+    row = z[0].double()
+    assert torch.equal(mx[0].double(), row.amax(-1))
+    x = (row - row.amax(-1, keepdim=True)) / float(np.float32(T))
+    total = x.exp().sum(-1)
+    # exponents with errors of 2^-22 |x|; a thread's 32 terms, the wavefront's and an exponential's
+    # roundings
+    slack = (x.abs() * x.exp()).nan_to_num(0.0).sum(-1) * 2.0 ** -22 + total * 42 * 2.0 ** -24
+    assert ((sm[0] - total).abs() <= slack).all(), (sm[0].tolist(), total.tolist())
