@@ -447,7 +447,8 @@ int tv_tree_attention(int32_t batch, int32_t num_nodes, int32_t heads, int32_t k
  * set where t is allowed; mask_index int32 [batch][num_nodes] the mask of each
  * node, negative for none (NULL: no masks); num_masks or more allows nothing.
  * Tokens outside [0, vocab) in tokens, history and bias_tokens are passed over;
- * lengths outside [0, max_history] count as the nearer end.
+ * lengths outside [0, max_history] count as the nearer end. batch times the
+ * vocabulary in 8192s (rounded up) below 2^24.
  * workspace: tv_process_logits_workspace_size() bytes (0 for invalid sizes),
  * 256-byte aligned, not needed without statistics. Nothing is allocated. Returns
  * a tv_status_t; argument errors launch nothing.

@@ -152,6 +152,7 @@ struct Params {
   float* part_max;           // [batch][num_nodes][chunks][wavefront]
   float* part_sum;
   float k32;                 // log2(e) / T rounded to fp32
+  long long first_row;       // of the launch that merges
 };
 
 // kMasks: nodes have masks.
@@ -406,7 +407,7 @@ __device__ __forceinline__ double frame_of(float m, float k) {
 __global__ void __launch_bounds__(kThreads) logits_merge_kernel(Params P) {
   const tv::LogitsArgs& a = P.a;
   const int lane = threadIdx.x & 63;
-  const long long r = static_cast<long long>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
+  const long long r = P.first_row + static_cast<long long>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
   if (r >= static_cast<long long>(a.batch) * a.num_rows) return;
   const long long b = r / a.num_rows;
   const size_t row = static_cast<size_t>(b) * a.num_nodes + a.first_node + (r - b * a.num_rows);
@@ -449,6 +450,9 @@ hipError_t run(const Params& P, unsigned grid, hipStream_t stream) {
 // gain: one tree of 65 nodes 30.1 us, with twice as many 33.8, with half 34.2.
 constexpr int kEnough = 1024, kEnoughF32 = 768;
 
+// Workgroups of a launch: one has fewer than 2^32 threads.
+constexpr int64_t kMostGroups = (int64_t{1} << 24) - 1;
+
 }  // namespace
 
 namespace tv {
@@ -468,16 +472,21 @@ int launch_logits(const LogitsArgs& a, void* workspace, hipStream_t stream) {
   P.slabs = static_cast<int>(want < a.num_rows ? want : a.num_rows);
   P.rows = (a.num_rows + P.slabs - 1) / P.slabs;
   P.slabs = (a.num_rows + P.rows - 1) / P.rows;
-  if (per * P.slabs > INT32_MAX) return TV_ERR_UNSUPPORTED;
+  if (per * P.slabs > kMostGroups) return TV_ERR_UNSUPPORTED;
   const unsigned grid = static_cast<unsigned>(per * P.slabs);
   const hipError_t e = a.dtype == TV_DTYPE_BF16 ? run<uint16_t>(P, grid, stream)
                                                 : run<float>(P, grid, stream);
   if (e != hipSuccess) return TV_ERR_HIP;
   if (!a.row_max) return TV_OK;
   const int64_t rows = static_cast<int64_t>(a.batch) * a.num_rows;
-  hipLaunchKernelGGL(logits_merge_kernel, dim3(static_cast<unsigned>((rows + kWaves - 1) / kWaves)),
-                     dim3(kThreads), 0, stream, P);
-  return hipGetLastError() == hipSuccess ? TV_OK : TV_ERR_HIP;
+  constexpr int64_t kMost = kMostGroups * kWaves;   // rows of a launch
+  for (P.first_row = 0; P.first_row < rows; P.first_row += kMost) {
+    const int64_t n = rows - P.first_row < kMost ? rows - P.first_row : kMost;
+    hipLaunchKernelGGL(logits_merge_kernel, dim3(static_cast<unsigned>((n + kWaves - 1) / kWaves)),
+                       dim3(kThreads), 0, stream, P);
+    if (hipGetLastError() != hipSuccess) return TV_ERR_HIP;
+  }
+  return TV_OK;
 }
 
 }  // namespace tv

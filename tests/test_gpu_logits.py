@@ -404,3 +404,18 @@ def test_statistics_of_rows_masked_with_low_values(dtype, T, low):
     # roundings
     slack = (x.abs() * x.exp()).nan_to_num(0.0).sum(-1) * 2.0 ** -22 + total * 42 * 2.0 ** -24
     assert ((sm[0] - total).abs() <= slack).all(), (sm[0].tolist(), total.tolist())
+
+
+def test_more_rows_than_one_grid_of_wavefronts():
+    """2^26 rows and more of a vocabulary of two."""
+    B, n1 = 65537, 1024
+    g = torch.Generator(device=DEV).manual_seed(3)
+    z = torch.randn((B, n1, 2), generator=g, device=DEV).bfloat16()
+    out, mx, sm = tv.process_logits(z, 1.0, want_stats=True)
+    assert torch.equal(out, z)
+    for part in (slice(0, 100), slice(-100, None), slice(32000, 34000)):
+        r = z[part].double()
+        assert torch.equal(mx[part].double(), r.amax(-1))
+        want = (r - r.amax(-1, keepdim=True)).exp().sum(-1)
+        assert ((sm[part] - want).abs() <= 2e-6 * want).all()
+    assert bool(((sm > 1.0) & (sm <= 2.0 + 1e-5)).all())

@@ -103,6 +103,11 @@ def test_logits_empty_calls_and_workspace_size():
     assert tv.tv_process_logits_workspace_size(256, 65, 128256) >= 256 * 65 * 16 * 4 * 8
 
 
+def test_logits_of_more_workgroups_than_a_launch_has():
+    assert call_logits(batch=1 << 20, num_nodes=1, num_rows=1, vocab=17 * 8192,
+                       workspace_bytes=1 << 60) == UNS
+
+
 def call_extend(**kw):
     args = dict(batch=2, new_len=A, max_new=4, seq_len=A, new_seq_len=A, block_table=A,
                 table_width=8, page_size=16, prefix_len=0, free_pages=A, num_pages=32,
