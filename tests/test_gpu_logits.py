@@ -419,3 +419,41 @@ def test_more_rows_than_one_grid_of_wavefronts():
         want = (r - r.amax(-1, keepdim=True)).exp().sum(-1)
         assert ((sm[part] - want).abs() <= 2e-6 * want).all()
     assert bool(((sm > 1.0) & (sm <= 2.0 + 1e-5)).all())
+
+
+def test_drafted_tokens_of_long_bias_lists():
+    """The bias of a drafted token is not looked for in the list row by row: 50000 biases cost a
+    call about what 500 cost."""
+    B, n1, V = 4, 33, 32000
+    z = torch.randn((B, n1, V), device=DEV).bfloat16()
+    par = torch.arange(-1, n1 - 1, dtype=torch.int32, device=DEV).repeat(B, 1)
+    tok = torch.arange(n1, dtype=torch.int32, device=DEV).repeat(B, 1) * 3
+    us = {}
+    for n in (500, 50000):
+        at = (V - 1 - torch.arange(n, device=DEV) % (V - 200)).int().repeat(B, 1)
+        at[:, :300] = torch.arange(300, device=DEV).int()      # drafted tokens at the list's start
+        val = torch.randn((B, n), device=DEV)
+        kw = dict(parents=par, tokens=tok, bias_tokens=at.contiguous(), bias_values=val,
+                  frequency=torch.full((B,), 0.5, device=DEV))
+        out, _, _ = tv.process_logits(z, 1.0, **kw)
+        last = torch.zeros((B, V), device=DEV)
+        for b in range(B):
+            keep = {}
+            for j, t in enumerate(at[b].tolist()):
+                keep[t] = j
+            idx = torch.tensor(list(keep.items()), device=DEV)
+            last[b, idx[:, 0]] = val[b, idx[:, 1]]
+        seen = torch.zeros((B, n1, V), device=DEV)
+        for i in range(1, n1):
+            seen[:, i:, 3 * i] = 0.5
+        want = (z.float() - (seen - last[:, None])).bfloat16()
+        assert torch.equal(out, want)
+        e = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+        torch.cuda.synchronize()
+        e[0].record()
+        for _ in range(3):
+            tv.process_logits(z, 1.0, **kw)
+        e[1].record()
+        torch.cuda.synchronize()
+        us[n] = e[0].elapsed_time(e[1]) / 3 * 1e3
+    assert us[50000] < 40 * us[500] + 2000, us
