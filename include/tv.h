@@ -516,8 +516,8 @@ int tv_cache_extend(int32_t batch, const int32_t* new_len, int32_t max_new,
  * Any element type: sizes and strides are in bytes. k_new, v_new: layers
  * new_layer_stride apart, nodes node_stride apart (trees num_nodes *
  * node_stride), each node [kv_heads][head_bytes]. k_cache, v_cache: layers
- * cache_layer_stride apart (a page at least), pages page_stride, each [kv_heads]
- * [page_size][head_bytes]. head_bytes a multiple of 16 up to 4096; strides multiples of
+ * cache_layer_stride apart, pages page_stride, each [kv_heads]
+ * [page_size][head_bytes]; no two layers' pages may share bytes. head_bytes a multiple of 16 up to 4096; strides multiples of
  * 16, pointers 16-byte aligned. No workspace; nothing is allocated. Returns a
  * tv_status_t; argument errors launch nothing.
  */

@@ -125,6 +125,23 @@ int validate(const tv::ExtendArgs& a) {
   return TV_OK;
 }
 
+// Whether pages of two layers share bytes: layers begin cache_layer_stride apart, and a
+// layer's pages of `size` bytes page_stride (no less).
+bool layers_overlap(const tv::CacheCommitArgs& a, int64_t size) {
+  using Wide = __int128;
+  const Wide apart = a.cache_layer_stride < 0 ? -static_cast<Wide>(a.cache_layer_stride)
+                                              : static_cast<Wide>(a.cache_layer_stride);
+  const Wide step = a.page_stride, last = (a.num_pages - 1) * step;   // the last page
+  if (a.layers < 2 || apart >= last + size) return false;
+  for (int l = 1; l < a.layers; ++l) {
+    // the first page of the layer l on: behind a page's end, and before the next one's start
+    const Wide at = l * apart, page = at / step * step;
+    if (page <= last && at - page < size) return true;
+    if (page + step <= last && page + step - at < size) return true;
+  }
+  return false;
+}
+
 int validate(const tv::CacheCommitArgs& a) {
   if (a.layers < 0 || a.batch < 0 || a.num_nodes < 1 || a.kv_heads < 1 || a.head_bytes < 1 ||
       a.num_pages < 0 || a.page_size < 1 || a.max_new < 0 || a.path_width < 0)
@@ -136,10 +153,7 @@ int validate(const tv::CacheCommitArgs& a) {
   const int64_t row = static_cast<int64_t>(a.kv_heads) * a.head_bytes;
   if (a.node_stride < row || (a.num_pages > 0 && a.page_stride < row * a.page_size))
     return TV_ERR_INVALID_ARG;
-  // layers whose pages would overlap
-  if (a.layers > 1 && a.num_pages > 0 && a.cache_layer_stride < row * a.page_size &&
-      a.cache_layer_stride > -row * a.page_size)
-    return TV_ERR_INVALID_ARG;
+  if (a.num_pages > 0 && layers_overlap(a, row * a.page_size)) return TV_ERR_INVALID_ARG;
   if (a.new_layer_stride % 16 || a.node_stride % 16 || a.cache_layer_stride % 16 ||
       a.page_stride % 16)
     return TV_ERR_UNSUPPORTED;

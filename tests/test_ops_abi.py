@@ -161,6 +161,28 @@ def test_commit_refusals(kw, want):
     assert call_commit(**kw) == want
 
 
+def test_commit_refuses_layers_that_share_bytes():
+    """Every small layout against all pairs of pages (an empty batch: nothing is launched)."""
+    page, refused = 256, 0
+    for layers in (1, 2, 3, 5):
+        for pages in (1, 2, 3, 7):
+            for step in (256, 272, 512, 768, 1280):
+                for apart in list(range(-3840, 3841, 80)) + [256 * k for k in range(-9, 10)]:
+                    starts = np.array([[i * apart + p * step for p in range(pages)]
+                                       for i in range(layers)])
+                    shared = any((np.abs(starts[i][:, None] - starts[j]) < page).any()
+                                 for i in range(layers) for j in range(i))
+                    got = call_commit(layers=layers, batch=0, kv_heads=1, head_bytes=16,
+                                      page_size=16, num_pages=pages, page_stride=step,
+                                      cache_layer_stride=apart)
+                    assert got == (BAD if shared else tv.TV_OK), (layers, pages, step, apart)
+                    refused += shared
+    assert refused > 100
+    far = dict(batch=0, layers=tv.TV_MAX_LAYERS, page_stride=1 << 62, num_pages=(1 << 27) - 1)
+    assert call_commit(cache_layer_stride=(1 << 62) + 4096, **far) == tv.TV_OK
+    assert call_commit(cache_layer_stride=(1 << 62) + 2048, **far) == BAD
+
+
 @pytest.mark.parametrize("kw", [dict(layers=0), dict(batch=0), dict(max_new=0), dict(num_pages=0)])
 def test_commit_empty_calls(kw):
     assert call_commit(**kw, k_new=None, new_len=None, slots=None) == tv.TV_OK
