@@ -495,8 +495,9 @@ enum {
  * free_count outside [0, num_pages] counts as the nearer end. page_size a power
  * of two from TV_MIN_PAGE to TV_MAX_PAGE, prefix_len a multiple of it; num_pages *
  * page_size and table_width * page_size at most 2^31 - 1; slots may be NULL if
- * max_new is 0. No workspace; nothing is allocated. Returns a tv_status_t;
- * argument errors launch nothing.
+ * max_new is 0. A batch of 0 has its new_free_count written and nothing else. No
+ * workspace; nothing is allocated. Returns a tv_status_t; argument errors launch
+ * nothing.
  */
 int tv_cache_extend(int32_t batch, const int32_t* new_len, int32_t max_new,
                     const int32_t* seq_len, int32_t* new_seq_len, int32_t* block_table,

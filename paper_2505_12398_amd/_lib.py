@@ -582,7 +582,7 @@ def cache_extend(new_len, seq_len, block_table, free_pages, free_count, page_siz
     B, dev, i32 = new_len.shape[0], block_table.device, torch.int32
     if out is None and B == 0:
         return CacheGrowth(new_len.new_empty((0, max_new)), seq_len.clone(),
-                           free_count.clone(), new_len.new_empty(0))
+                           free_count.clamp(0, free_pages.shape[0]), new_len.new_empty(0))
     width, pages, per = block_table.shape[-1], free_pages.shape[0], (B,)
     new = _check("new_len", new_len, per, i32, dev)
     seq = _check("seq_len", seq_len, per, i32, dev)

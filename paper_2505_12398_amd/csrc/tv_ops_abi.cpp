@@ -104,6 +104,11 @@ int validate(const tv::LogitsArgs& a, void* workspace, size_t workspace_bytes) {
   return TV_OK;
 }
 
+// An empty batch whose count of free pages goes to another place.
+bool count_alone(const tv::ExtendArgs& a) {
+  return a.batch == 0 && a.free_count && a.new_free_count && a.free_count != a.new_free_count;
+}
+
 int validate(const tv::ExtendArgs& a) {
   if (a.batch < 0 || a.max_new < 0 || a.table_width < 0 || a.page_size < 1 || a.prefix_len < 0 ||
       a.num_pages < 0)
@@ -113,7 +118,9 @@ int validate(const tv::ExtendArgs& a) {
   if (a.prefix_len % a.page_size) return TV_ERR_INVALID_ARG;
   if (a.num_pages > INT32_MAX / a.page_size || a.table_width > INT32_MAX / a.page_size)
     return TV_ERR_UNSUPPORTED;
-  if (a.batch == 0) return TV_OK;
+  if (a.batch == 0)
+    return count_alone(a) && (bits(a.free_count) | bits(a.new_free_count)) % 4 ? TV_ERR_INVALID_ARG
+                                                                               : TV_OK;
   if (!a.new_len || !a.seq_len || !a.new_seq_len || !a.free_count || !a.new_free_count ||
       !a.status || (a.max_new > 0 && !a.slots) || (a.table_width > 0 && !a.block_table) ||
       (a.num_pages > 0 && !a.free_pages))
@@ -234,7 +241,7 @@ int tv_cache_extend(int32_t batch, const int32_t* new_len, int32_t max_new,
                          block_table, table_width,   page_size,  prefix_len, free_pages,
                          num_pages,  free_count,     new_free_count, slots, status};
   const int st = validate(a);
-  if (st != TV_OK || batch == 0) return st;
+  if (st != TV_OK || (batch == 0 && !count_alone(a))) return st;
   return tv::launch_extend(a, stream);
 }
 

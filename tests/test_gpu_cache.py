@@ -351,3 +351,16 @@ def test_decoding_cycles():
     # every request ends: all pages are free again
     e = tv.cache_extend(torch.full_like(seq, tv.TV_CACHE_RELEASE), seq, table, free, count, ps, 1)
     assert int(e.free_count) == 64 and sorted(free.tolist()) == list(range(64))
+
+
+@pytest.mark.parametrize("count,want", [(5, 5), (0, 0), (-3, 0), (99, 8)])
+def test_extend_of_an_empty_batch(count, want):
+    """The count of free pages is passed on, also where the caller has a place for it."""
+    def i32(*shape):
+        return torch.zeros(shape, dtype=torch.int32, device=DEV)
+    n = torch.tensor([count], dtype=torch.int32, device=DEV)
+    out = tv.CacheGrowth(i32(0, 4), i32(0), i32(1) - 7, i32(0))
+    args = (i32(0), i32(0), i32(0, 3), i32(8), n, 16, 4)
+    assert tv.cache_extend(*args, out=out) is out
+    assert out.free_count.tolist() == [want] and n.tolist() == [count]
+    assert tv.cache_extend(*args).free_count.tolist() == [want]

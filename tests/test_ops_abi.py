@@ -134,6 +134,12 @@ def test_extend_empty_batch():
     assert call_extend(batch=0, new_len=None, seq_len=None, status=None) == tv.TV_OK
 
 
+def test_extend_empty_batch_checks_the_counts():
+    assert call_extend(batch=0, free_count=A + 2) == BAD
+    assert call_extend(batch=0, new_free_count=A + 2) == BAD
+    assert call_extend(batch=0, new_free_count=None) == tv.TV_OK
+
+
 def call_commit(**kw):
     args = dict(layers=2, batch=2, num_nodes=5, kv_heads=2, head_bytes=128, k_new=A, v_new=A,
                 new_layer_stride=1 << 16, node_stride=256, k_cache=A, v_cache=A,
