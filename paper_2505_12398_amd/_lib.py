@@ -407,7 +407,9 @@ class _On:
             if stream is None:
                 self.stream = now
             elif stream != now:
-                self.current = torch.cuda.stream(torch.cuda.ExternalStream(stream, device=dev))
+                # (wrapped, the default stream's handle 0 would give a new stream)
+                self.current = torch.cuda.stream(torch.cuda.ExternalStream(stream, device=dev)
+                                                 if stream else torch.cuda.default_stream(dev))
 
     def __enter__(self):
         if self.index is not None:

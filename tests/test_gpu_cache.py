@@ -364,3 +364,35 @@ def test_extend_of_an_empty_batch(count, want):
     assert tv.cache_extend(*args, out=out) is out
     assert out.free_count.tolist() == [want] and n.tolist() == [count]
     assert tv.cache_extend(*args).free_count.tolist() == [want]
+
+
+def test_the_given_stream_is_the_current_one_meanwhile():
+    """Whatever stream is current, the default one given by its handle 0 among them; a cycle's
+    calls then equal those on the current stream."""
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    dev = torch.device(DEV)
+    for now in (torch.cuda.default_stream(), side):
+        with torch.cuda.stream(now):
+            for given in (None, 0, side.cuda_stream, other.cuda_stream):
+                with tv._lib._On(dev, given) as at:
+                    assert at == (now.cuda_stream if given is None else given)
+                    assert torch.cuda.current_stream().cuda_stream == at
+                assert torch.cuda.current_stream() == now
+    z = torch.randn((3, 5, 4001), device=DEV)
+    n = torch.tensor([2, 0, 4], dtype=torch.int32, device=DEV)
+    path = torch.tensor([[1, 0, 9, 0, 2, 0]] * 3, dtype=torch.int32, device=DEV)[:, ::2]
+    k = torch.randn((1, 3, 5, 2, 8), device=DEV)
+    slots = torch.arange(12, dtype=torch.int32, device=DEV).view(3, 4)
+
+    def calls(stream):
+        cache = torch.zeros((2, 1, 4, 2, 16, 8), device=DEV)
+        torch.cuda.synchronize()
+        rows = tv.process_logits(z, 0.7, stream=stream)
+        tv.cache_commit(k, k, cache[0], cache[1], n, slots, path_nodes=path, stream=stream)
+        torch.cuda.synchronize()
+        return *rows, cache
+    want = calls(None)
+    with torch.cuda.stream(side):
+        for stream in (0, other.cuda_stream):
+            for a, b in zip(calls(stream), want):
+                assert torch.equal(a, b)

@@ -1,6 +1,8 @@
 """Refusals of the operators around a verification, through the C-ABI with fake
 addresses and through the binding with CPU tensors: nothing reaches the GPU."""
 
+import contextlib
+
 import numpy as np
 import pytest
 import torch
@@ -195,6 +197,47 @@ def test_commit_empty_calls(kw):
 
 
 # --- the binding ---------------------------------------------------------------
+
+
+class Streams:
+    """The parts of torch.cuda that the binding asks, with streams that are numbers; wrapping the
+    handle 0 makes a stream of its own, as torch does."""
+
+    def __init__(self, monkeypatch, device, now):
+        self.device, self.now, self.default = device, dict(now), 0
+        patch = monkeypatch.setattr
+        patch(torch.cuda, "current_device", lambda: self.device)
+        patch(torch.cuda, "set_device", lambda d: setattr(self, "device", d))
+        patch(torch._C, "_cuda_getCurrentRawStream", lambda d: self.now[d], raising=False)
+        patch(torch.cuda, "ExternalStream", lambda h, device=None: (h or 77, self.index(device)))
+        patch(torch.cuda, "default_stream", lambda device=None: (0, self.index(device)))
+        patch(torch.cuda, "stream", self.stream)
+
+    def index(self, device):
+        index = device.index if isinstance(device, torch.device) else device
+        return self.device if index is None else index
+
+    @contextlib.contextmanager
+    def stream(self, s):
+        before = self.device, dict(self.now)
+        self.device, self.now[s[1]] = s[1], s[0]
+        yield
+        self.device, self.now = before
+
+
+@pytest.mark.parametrize("device", ["cuda", "cuda:0", "cuda:1"])
+@pytest.mark.parametrize("current", [0, 5])
+@pytest.mark.parametrize("given", [None, 0, 5, 9])
+def test_the_stream_of_a_call_is_current_meanwhile(monkeypatch, device, current, given):
+    """What a call allocates belongs to the stream that it enqueues on, the default one (handle 0)
+    too; afterwards device and streams are those of before."""
+    s = Streams(monkeypatch, 0, {0: current, 1: 3})
+    dev = torch.device(device)
+    index = dev.index or 0
+    want = s.now[index] if given is None else given
+    with tv._lib._On(dev, given) as at:
+        assert at == want and s.device == index and s.now[index] == want
+    assert s.device == 0 and s.now == {0: current, 1: 3}
 
 
 def attention_tensors(dtype=torch.bfloat16):
