@@ -429,6 +429,12 @@ class _On:
         return False
 
 
+def _on_gpu(dev, what):
+    """Refuses a call that would start on tensors elsewhere, whose addresses no kernel may use."""
+    if dev.type != "cuda":
+        raise TvError(TV_ERR_INVALID_ARG, f"{what} on tensors of {dev}")
+
+
 def _workspace(need, workspace, dev):
     import torch
     if workspace is None:
@@ -504,6 +510,8 @@ def tree_attention(q, k_new, v_new, parents, k_cache, v_cache, block_table, ctx_
         to = _check("out", out, (B, n1, H, D), dt, dev)
         ws, nbytes = _workspace(
             lib.tv_tree_attention_workspace_size(B, n1, H, KH, D, prefix_len), workspace, dev)
+        if B:
+            _on_gpu(dev, "tv_tree_attention")
         st = lib.tv_tree_attention(
             B, n1, H, KH, D, TV_DTYPE_BF16 if dt == torch.bfloat16 else TV_DTYPE_F16, parents,
             q.data_ptr(), q_stride, k_new.data_ptr(), v_new.data_ptr(), kv_stride,
@@ -558,6 +566,8 @@ def process_logits(logits, temperature, parents=None, tokens=None, history=None,
             row_max = torch.empty(per_row, dtype=f32, device=dev)
             row_sum = torch.empty(per_row, dtype=torch.float64, device=dev)
             ws, nbytes = _workspace(lib.tv_process_logits_workspace_size(B, n1, V), workspace, dev)
+        if B and count:
+            _on_gpu(dev, "tv_process_logits")
         st = lib.tv_process_logits(B, n1, V, first, count, z, dtype, temperature, *ins, to,
                                    _ptr(row_max), _ptr(row_sum), _ptr(ws), nbytes, at)
     if st != TV_OK:
@@ -601,6 +611,7 @@ def cache_extend(new_len, seq_len, block_table, free_pages, free_count, page_siz
         out_seq = _check("out.seq_len", out.seq_len, per, i32, dev)
         out_count = _check("out.free_count", out.free_count, (1,), i32, dev)
         status = _check("status", out.status, per, i32, dev)
+        _on_gpu(dev, "tv_cache_extend")
         st = load_library().tv_cache_extend(B, new, max_new, seq, out_seq, table, width, page_size,
                                             prefix_len, free, pages, count, out_count, slots,
                                             status, at)
@@ -644,6 +655,8 @@ def cache_commit(k_new, v_new, k_cache, v_cache, new_len, slots, path_nodes=None
             width = path_nodes.shape[-1]
             path_nodes = path_nodes.contiguous()
             path = _check("path_nodes", path_nodes, (B, width), i32, dev)
+        if B and most and P:
+            _on_gpu(dev, "tv_cache_commit")
         st = load_library().tv_cache_commit(
             L, B, n1, KH, D * e, k_new.data_ptr(), v_new.data_ptr(), new_layer * e, node * e,
             k_cache.data_ptr(), v_cache.data_ptr(), layer * e, page * e, P, ps, new, most,

@@ -322,6 +322,30 @@ def test_cache_binding_checks():
                                         slots=s), **bad))
 
 
+def test_tensors_that_are_not_on_a_gpu_are_refused():
+    """Valid calls, whose addresses would be the host's; empty ones start nothing and pass."""
+    i32 = dict(dtype=torch.int32)
+    a = attention_tensors()
+    z = torch.zeros(2, 3, 10)
+    n, s = torch.ones(2, **i32), torch.zeros(2, 2, **i32)
+    k, c = torch.zeros(1, 2, 4, 2, 16), torch.zeros(1, 5, 2, 16, 16)
+    growth = (n, n * 0, torch.zeros(2, 4, **i32), torch.zeros(8, **i32), torch.zeros(1, **i32), 16, 4)
+    for call in (lambda: tv.tree_attention(**a), lambda: tv.process_logits(z, 1.0),
+                 lambda: tv.process_logits(z, 1.0, want_stats=False),
+                 lambda: tv.cache_extend(*growth),
+                 lambda: tv.cache_commit(k, k, c, c.clone(), n, s)):
+        with pytest.raises(tv.TvError) as e:
+            call()
+        assert e.value.code == BAD
+    none = {name: t[:0] if name in ("q", "k_new", "v_new", "parents", "block_table", "ctx_len")
+            else t for name, t in a.items()}
+    assert tv.tree_attention(**none).shape == (0, 3, 4, 32)
+    assert tv.process_logits(z, 1.0, nodes=(3, 0))[0].shape == z.shape
+    assert tv.process_logits(z[:0], 1.0)[0].shape == (0, 3, 10)
+    tv.cache_commit(k, k, c, c.clone(), n, s[:, :0].contiguous())
+    tv.cache_commit(k[:, :0], k[:, :0], c, c.clone(), n[:0], s[:0])
+
+
 def test_constants_match_header():
     import os
     import re
