@@ -542,3 +542,22 @@ def test_prefix_longer_than_the_table():
         assert torch.isnan(got[1]).all()
         host["ctx"][1] = -1
         check(host, call, out=got)
+
+
+@pytest.mark.parametrize("prefix", [0, 1024])
+@pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("f16", 64)])
+@pytest.mark.parametrize("n1,kind,batch", [(24, "tree", 80), (65, "tree", 50), (48, "chain", 40),
+                                           (384, "tree", 6), (384, "chain", 6)])
+def test_wide_blocks_on_long_contexts(n1, kind, batch, dtype, dim, prefix):
+    """Workgroups of 96 and 192 rows over 60 tiles and more, in the common prefix too, with nodes
+    kept as words and walked; contexts that end around a tile's end. Some of the trees are
+    compared (all row tiles and heads of them), and the others' outputs are finite."""
+    rng = np.random.default_rng(n1)
+    ctx = rng.integers(1800, 2100, batch)
+    ctx[:6] = 2000, 2016, 2015, 2033, 1024, 3
+    host, call = inputs(batch, n1, 8, 2, dim, 16, ctx, dtype, kind, prefix=prefix)
+    got = tv.tree_attention(**call)
+    assert bool(got.isfinite().all())
+    host["ctx"][2:4] = -1
+    host["ctx"][6:-1] = -1
+    check(host, call, dtype, out=got)
