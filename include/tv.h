@@ -401,7 +401,7 @@ int tv_commit_paths(int32_t batch, int32_t num_nodes, const int32_t* parents,
  * apart, and a row may be NaN); q, k_new, v_new, caches and out 16-byte aligned,
  * strides multiples of 8; the nodes of a tree, and the distance of two pages, at
  * most 2^29 bytes; batch * num_nodes * heads at most 2^31 - 1.
- * out dtype [batch][num_nodes][heads][head_dim]. workspace:
+ * out dtype [batch][num_nodes][heads][head_dim], apart from all inputs. workspace:
  * tv_tree_attention_workspace_size() bytes (0 for invalid sizes), 256-byte
  * aligned. Nothing is allocated. Returns a tv_status_t; argument errors
  * launch nothing.

@@ -29,11 +29,18 @@
 // accumulators) in the workspace, and a second kernel merges them.
 //
 // What bounds it. 256 trees of 65 nodes on contexts of 1000 to 2900, 32 heads over 8:
-// 876 us, 610 TFLOP/s, 2.7 TB/s of keys and values; the matrix units are busy for 37% of
-// it at the 2.0 GHz that such a load runs at. A lone wavefront's round of 32 keys takes
-// 1950 cycles (scores 490, weights 465, values 440, eight loads 43 each), so that the
-// issue of its own instructions bounds it: 815 us remain without the loads. Single
-// tokens of 64 sequences: 282 us, 5.6 TB/s, which is the rate of a large read.
+// 827 us, 640 TFLOP/s, 2.9 TB/s of keys and values, of which its three workgroups a tree
+// bring every key into LDS once each. A wavefront's round of 32 keys takes 3900 to 4500
+// cycles beside the other one of its SIMD (scores 620 to 940, weights 580 to 760, values
+// 590 to 770, eight loads 620 to 1100, waits and barriers 620 to 1100, stamped): the issue
+// of instructions bounds it, a quarter of them those that load. Single tokens of 64
+// sequences: 288 us, 5.5 TB/s, near the rate of a large read (5.85). One tree: 31.6 us;
+// a part of it takes 25 thousand cycles, of which its rounds take 6.5 (the cut 4.4, queries
+// 1.8, the first loads' issue 1.6, links and words 1, the key groups' merge and the part's
+// way out 10), and one that goes on in the next key head's item all but the cut again.
+//
+// Heads of 72 to 120 are computed as heads of 128, padded with zeros in LDS (what they
+// read is not): where instructions bound it they cost what 128 cost.
 //
 // A common prefix is an item of its own whose rows are those of all trees; its
 // (maximum, sum, accumulators) wait in the workspace for the trees' own parts.
@@ -59,7 +66,7 @@ constexpr int kMaxTeam = 32;              // workgroups of a team: the CUs of an
 // the other), 8 / 16 / 32: 34 / 41 / 50 (eight at a time); by rows of 48, 8 / 16: 32 / 33.
 constexpr int kMinTiles = 8;
 // Up to how many nodes the rows' paths are kept as words (in LDS, 32 bytes a node): 256
-// trees of 65 nodes 885 us, walked per tile 895.
+// trees of 65 nodes 831 us, walked per tile 839.
 constexpr int kWordNodes = 256;
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
@@ -790,8 +797,8 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
     constexpr int kLast = (SH::S - 1) * SH::STAGE;
     int stage = ring, before = ring + kLast;                 // places of tiles i and i - 1
     // hot: the tile itself and those it loads are full and lie in pages. Such rounds run
-    // without branches: a wavefront's own instructions, at five cycles or more each, are
-    // what a round without them takes (general rounds alone 906 us where this is 883).
+    // without branches, of which every instruction counts (general rounds alone: 844 us
+    // where 256 trees take 831).
     auto round = [&](auto hot_c, int i, int t) {
       constexpr bool kHot = hot_c.value;
       f32x4 s[MT][2];
@@ -1062,7 +1069,8 @@ __global__ void __launch_bounds__(64 * kMergeWaves) merge_kernel(Pass P) {
 // alone; one of 192 has one, which its wavefronts share, and a part is a wavefront's, not
 // a workgroup's. Batch 256, contexts of 2048, 32 heads over 8, by 48 / 96 / 192 rows:
 // 260 rows 1038 / 809 / 927 us, 192 rows 649 / 486 / 467, 128 rows 517 / 467 / 443.
-// Few items are cut into many parts, of which 48 rows leave a quarter as many to merge:
+// (Other contexts were not compared: on long ones few items have rounds enough that 96
+// rows may be the better choice for them too.) Few items are cut into many parts, of which 48 rows leave a quarter as many to merge:
 // contexts of 4096, by 48 or else, 260 rows of 8 / 16 / 32 / 64 items 33 or 47, 37 or 51,
 // 55 or 57, 74 or 71 us; 192 rows of 32 / 64 / 128 items 41 or 81, 54 or 89, 75 or 92.
 int block_rows(int64_t rows, int64_t items) {

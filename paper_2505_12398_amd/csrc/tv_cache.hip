@@ -188,7 +188,7 @@ constexpr int kRows = 16;   // rows of a workgroup
 
 // Workgroup (b, layer, z): every gridDim.z-th kRows rows' keys and values, 16 bytes a
 // thread and step. Bound by HBM, in rows of a few hundred bytes to each head's page:
-// 256 requests, 32 layers of 8 heads of 128, 5.5 rows each: 61 us, 6.1 TB/s read and
+// 256 requests, 32 layers of 8 heads of 128, 4.9 rows each: 61 us, 5.4 TB/s read and
 // written (within what the last-level cache holds of it).
 __global__ void __launch_bounds__(kCopyThreads) cache_commit_kernel(tv::CacheCommitArgs a) {
   const int b = blockIdx.x, layer = blockIdx.y, all = min(a.new_len[b], a.max_new);

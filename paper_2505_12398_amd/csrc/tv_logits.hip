@@ -9,9 +9,10 @@
 // a node's path change few logits: their owners compute those again.
 //
 // What bounds it is HBM: 256 trees of 65 nodes and 128256 tokens in bfloat16 take
-// 1.80 ms, 4.75 TB/s read and written (a large copy: 4.74). One tree takes 28 us,
-// bound by its launches and the count of its history. (Accesses marked as used once:
-// 1.78 ms of those 256 trees, but 250 us instead of 228 of 16 in float32.)
+// 1.80 ms, 4.75 TB/s read and written (a large copy: 4.74). One tree takes 25 us,
+// bound by its launches and a set-up of reads that wait for each other (biases, tokens
+// and links, history). (Accesses marked as used once: 1.78 ms of those 256 trees, but
+// 250 us instead of 228 of 16 in float32, before biases were kept from the set-up.)
 //
 // The statistics are a maximum and a sum of 2^((z - max) k), k = log2(e)/T, per
 // wavefront and row, in fp32 in the frame of the maximum; a second kernel merges
@@ -457,7 +458,8 @@ hipError_t run(const Params& P, unsigned grid, hipStream_t stream) {
 
 // Workgroups that fill the device: four on a CU, or three of fp32 (their rows take more
 // registers). Each counts its chunk's history anew, so more of them cost more than they
-// gain: one tree of 65 nodes 30.1 us, with twice as many 33.8, with half 34.2.
+// gain: 16 trees of 41 nodes in float32 45.4 us, with twice as many 49.0, with half 49.4
+// (one tree of 65 in bfloat16 within 3% by all three).
 constexpr int kEnough = 1024, kEnoughF32 = 768;
 
 // Workgroups of a launch: one has fewer than 2^32 threads.
