@@ -131,13 +131,15 @@ enum {
 #define TV_NUM_COUNTERS 4
 #define TV_MAX_LMHEAD_ROWS (1 << 18)    /* rows of one tv_lmhead_stats call */
 #define TV_MAX_HIDDEN (1 << 16)         /* hidden size of tv_lmhead_stats */
-#define TV_MAX_HEAD_DIM 128             /* head size of tv_tree_attention */
+#define TV_MAX_HEAD_DIM 128             /* head size of the attentions */
 #define TV_MIN_PAGE 16                  /* tokens of a cache page, a power of two */
 #define TV_MAX_PAGE 1024
 #define TV_MAX_HISTORY (1 << 24)        /* tokens of one request's history */
 #define TV_MAX_BIAS (1 << 16)           /* biased tokens of one request */
 #define TV_MAX_NEW (1 << 20)            /* positions appended to one request by one call */
 #define TV_MAX_LAYERS 4096              /* layers of one tv_cache_commit call */
+#define TV_FP4_BLOCK 32                 /* elements that share an exponent in a cache of 4 bits */
+#define TV_FP4_BLOCK_BYTES 17           /* and their bytes */
 
 /*
  * Bytes of device workspace tv_verify / tv_verify_tokenlevel need for these
@@ -529,6 +531,100 @@ int tv_cache_commit(int32_t layers, int32_t batch, int32_t num_nodes, int32_t kv
                     int32_t page_size, const int32_t* new_len, int32_t max_new,
                     const int32_t* slots, const int32_t* path_nodes, int32_t path_width,
                     hipStream_t stream);
+
+/*
+ * Attention of whole prompts, or of pieces of them: for sequence b the queries are the rows
+ * q_start[b] .. q_start[b + 1] - 1 of q, and its keys and values the rows k_start[b] ..
+ * k_start[b + 1] - 1 of k and v. Its queries are the last positions of its keys: with nq and nk
+ * of them, query i sees the keys 0 .. i + nk - nq (causal; with earlier positions' keys, read back
+ * by tv_cache_read_fp4 say, in front of its own, a prompt is attended piece by piece). With query
+ * head h reading key head h / (heads / kv_heads),
+ *   out[i][h] = sum_j exp(s(i, j)) value j / sum_j exp(s(i, j)),  s(i, j) = scale * <q[i][h], key j>
+ * over the keys that query i sees; a query that sees none (nq > nk) gets zeros. Sums are formed in
+ * fp32 from products on the matrix cores; weights are rounded as by tv_tree_attention.
+ *
+ * Inputs (device): q [num_queries][heads][head_dim], k and v [num_keys][kv_heads][head_dim] of type
+ * dtype (TV_DTYPE_BF16 or TV_DTYPE_F16), consecutive rows q_stride and kv_stride elements apart (so
+ * that all three may lie in one projection's output); q_start, k_start int32 [batch + 1], k_start NULL
+ * for the same starts. Starts outside the tensors count as the nearer end, and starts that decrease as
+ * the largest before them. A key or value that a query does not see changes nothing of its output,
+ * whatever it holds. A sequence's outputs do not depend on the other sequences, but for the last bits,
+ * which depend on num_queries and batch; the same call gives the same bits.
+ *
+ * head_dim: a multiple of 8 up to TV_MAX_HEAD_DIM; heads a multiple of kv_heads; heads * head_dim at
+ * most TV_MAX_HIDDEN; num_queries * heads below 2^29 and batch * kv_heads below 2^22; kv_stride at
+ * most 2^24; scale as for tv_tree_attention; q, k, v and out 16-byte aligned, strides multiples of 8.
+ * out dtype [num_queries][heads][head_dim], apart from all inputs; rows of no sequence are left as
+ * they were. workspace: tv_prompt_attention_workspace_size() bytes (0 for invalid sizes), 256-byte
+ * aligned. Nothing is allocated. Returns a tv_status_t; argument errors launch nothing.
+ */
+size_t tv_prompt_attention_workspace_size(int32_t batch, int32_t num_queries, int32_t num_keys,
+                                          int32_t heads, int32_t kv_heads, int32_t head_dim);
+int tv_prompt_attention(int32_t batch, int32_t num_queries, int32_t num_keys, int32_t heads,
+                        int32_t kv_heads, int32_t head_dim, int32_t dtype, const void* q,
+                        int64_t q_stride, const void* k, const void* v, int64_t kv_stride,
+                        const int32_t* q_start, const int32_t* k_start, float scale, void* out,
+                        void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * A cache of 4 bits. A page of one layer holds for each key head tv_fp4_page_bytes() bytes: its
+ * page_size rows of head_dim / 2 bytes, element 2 i of a row in the low half of byte i and element
+ * 2 i + 1 in the high one, then page_size rows of head_dim / TV_FP4_BLOCK exponents. An element is a
+ * sign (its highest bit) and one of 0, 1/2, 1, 3/2, 2, 3, 4, 6 (e2m1, codes 0 to 7), times 2^(e - 127)
+ * with the exponent e of its block of TV_FP4_BLOCK elements of the row; a block with e = 255 is NaN.
+ * Tables, slots and pages are those of tv_cache_extend. head_dim: a multiple of TV_FP4_BLOCK up to
+ * TV_MAX_HEAD_DIM. tv_fp4_page_bytes: 0 for sizes that are not taken.
+ */
+size_t tv_fp4_page_bytes(int32_t page_size, int32_t head_dim);
+
+/*
+ * tv_cache_commit into a cache of 4 bits: the same rows to the same slots. The exponent of a block is
+ * the least with amax <= 7 * 2^(e - 127), amax its largest magnitude, and at least 1 (from fp16 at most
+ * 140, so that it reads back as finite numbers); elements are rounded to the nearest of the values
+ * above, ties to the even code, beyond 6 to 6. A block with an element that is not finite is NaN.
+ * dtype (TV_DTYPE_BF16 or TV_DTYPE_F16) is that of k_new and v_new, whose strides are in elements and
+ * multiples of 8; the caches' strides are in bytes and multiples of 16, pages page_stride apart, each
+ * [kv_heads][tv_fp4_page_bytes()]. No two layers' pages may share bytes. Pointers 16-byte aligned. No
+ * workspace; nothing is allocated. Returns a tv_status_t; argument errors launch nothing.
+ */
+int tv_cache_commit_fp4(int32_t layers, int32_t batch, int32_t num_nodes, int32_t kv_heads,
+                        int32_t head_dim, int32_t dtype, const void* k_new, const void* v_new,
+                        int64_t new_layer_stride, int64_t node_stride, void* k_cache, void* v_cache,
+                        int64_t cache_layer_stride, int64_t page_stride, int32_t num_pages,
+                        int32_t page_size, const int32_t* new_len, int32_t max_new,
+                        const int32_t* slots, const int32_t* path_nodes, int32_t path_width,
+                        hipStream_t stream);
+
+/*
+ * Positions out of a cache of 4 bits, of all layers at once: positions first[b] .. first[b] + length[b]
+ * - 1 of request b (first NULL: from 0) to the rows row_start[b] .. of k_out and v_out, type dtype
+ * (TV_DTYPE_BF16: the values themselves; TV_DTYPE_F16: the nearest), layers out_layer_stride apart,
+ * rows row_stride, each [kv_heads][head_dim], in elements and multiples of 8. Positions that the block
+ * table int32 [batch][table_width] does not hold, and those on pages outside [0, num_pages), are NaN;
+ * rows outside [0, num_rows) are passed over, and all other rows left as they were. The rows of a call
+ * must differ. Caches as for tv_cache_commit_fp4. No workspace; nothing is allocated. Returns a
+ * tv_status_t; argument errors launch nothing.
+ */
+int tv_cache_read_fp4(int32_t layers, int32_t batch, int32_t kv_heads, int32_t head_dim, int32_t dtype,
+                      const void* k_cache, const void* v_cache, int64_t cache_layer_stride,
+                      int64_t page_stride, int32_t num_pages, int32_t page_size,
+                      const int32_t* block_table, int32_t table_width, const int32_t* first,
+                      const int32_t* length, const int32_t* row_start, int32_t num_rows, void* k_out,
+                      void* v_out, int64_t out_layer_stride, int64_t row_stride, hipStream_t stream);
+
+/*
+ * tv_tree_attention over a cache of 4 bits (page_stride in bytes, a multiple of 16): as that of the
+ * cache's values in dtype. q, k_new and v_new are of type dtype; workspace:
+ * tv_tree_attention_workspace_size() bytes.
+ */
+int tv_tree_attention_fp4(int32_t batch, int32_t num_nodes, int32_t heads, int32_t kv_heads,
+                          int32_t head_dim, int32_t dtype, const int32_t* parents, const void* q,
+                          int64_t q_stride, const void* k_new, const void* v_new, int64_t kv_stride,
+                          const void* k_cache, const void* v_cache, int64_t page_stride,
+                          int32_t num_pages, int32_t page_size, const int32_t* block_table,
+                          int32_t table_width, const int32_t* ctx_len, const int32_t* prefix_pages,
+                          int32_t prefix_len, float scale, void* out, void* workspace,
+                          size_t workspace_bytes, hipStream_t stream);
 
 /* Static, human-readable name of a tv_status_t value ("unknown status" otherwise). */
 const char* tv_status_string(int code);

@@ -1,6 +1,6 @@
 """Plain 64-bit forms of the operators around a verification: attention of tree
-nodes over a paged cache, penalties, biases and masks on logits, growth of block
-tables, commit of accepted keys and values. Written from their definitions, one
+nodes over a paged cache and of prompts, penalties, biases and masks on logits, growth
+of block tables, commit of accepted keys and values, in 4 bits too. Written from their definitions, one
 tree, node and token at a time; no code of the library."""
 
 import numpy as np
@@ -149,3 +149,117 @@ def cache_commit(k_new, k_cache, new_len, slots, path_nodes):
             if 0 <= s < P * ps and 0 <= node < n1:
                 cache[:, s // ps, :, s % ps] = k_new[:, b, node]
     return cache
+
+
+def prompt_attention(q, k, v, scale):
+    """Outputs of one sequence [nq, heads, D], whose queries are the last positions of its keys
+    [nk, kv_heads, D], with sum_j p_j |v_j| and the largest scale * sum_d |q_d k_d| of the keys that
+    a query sees; zeros for a query that sees none."""
+    (nq, H, D), (nk, KH) = q.shape, k.shape[:2]
+    out, mass, big = np.zeros((nq, H, D)), np.zeros((nq, H, D)), np.zeros((nq, H))
+    for i in range(nq):
+        see = i + nk - nq + 1
+        if see <= 0:
+            continue
+        for h in range(H):
+            kh, vh = k[:see, h // (H // KH)], v[:see, h // (H // KH)]
+            s = scale * (kh @ q[i, h])
+            w = np.exp(s - s.max())
+            w /= w.sum()
+            out[i, h] = w @ vh
+            mass[i, h] = w @ np.abs(vh)
+            big[i, h] = scale * (np.abs(kh) @ np.abs(q[i, h])).max()
+    return out, mass, big
+
+
+FP4_VALUES = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+
+
+def fp4_encode(x, largest=254):
+    """Codes and exponent of a block of 32 numbers: the least e of 1 .. largest with
+    max |x| <= 7 * 2^(e - 127), each number to the nearest value, of two as near the even code."""
+    a = [abs(float(y)) for y in x]
+    if not all(np.isfinite(a)):
+        return [0] * len(a), 255
+    e = 1
+    while max(a) > 7.0 * 2.0 ** (e - 127) and e < largest:
+        e += 1
+    codes = []
+    for y, z in zip(a, x):
+        gap = [abs(y / 2.0 ** (e - 127) - t) for t in FP4_VALUES]
+        near = [c for c in range(8) if gap[c] == min(gap)]
+        c = near[0] if len(near) == 1 else [c for c in near if c % 2 == 0][0]
+        codes.append(c + 8 * bool(np.signbit(z)))
+    return codes, e
+
+
+def fp4_values(codes, e):
+    """The numbers of a block in 64 bits."""
+    if e == 255:
+        return np.full(len(codes), np.nan)
+    return np.array([(-1.0 if c >= 8 else 1.0) * FP4_VALUES[c % 8] * 2.0 ** (int(e) - 127)
+                     for c in codes])
+
+
+def fp4_row(page, ps, dim, row):
+    """Row ``row`` of a head's page of bytes, in 64 bits."""
+    got = []
+    for b in range(dim // 32):
+        raw = page[row * dim // 2 + 16 * b:row * dim // 2 + 16 * b + 16]
+        codes = [int(x) >> s & 15 for x in raw for s in (0, 4)]
+        got.append(fp4_values(codes, int(page[ps * dim // 2 + row * dim // 32 + b])))
+    return np.concatenate(got)
+
+
+def fp4_put(page, ps, dim, row, x, largest=254):
+    """Writes a row of numbers into a head's page of bytes."""
+    for b in range(dim // 32):
+        codes, e = fp4_encode(x[32 * b:32 * b + 32], largest)
+        at = row * dim // 2 + 16 * b
+        page[at:at + 16] = [codes[2 * i] | codes[2 * i + 1] << 4 for i in range(16)]
+        page[ps * dim // 2 + row * dim // 32 + b] = e
+
+
+def fp4_cache(cache, ps, dim):
+    """[pages, kv_heads, page_size, D]: all values of one layer's cache of bytes
+    [pages, kv_heads, bytes]."""
+    P, KH = cache.shape[:2]
+    out = np.empty((P, KH, ps, dim))
+    for p in range(P):
+        for h in range(KH):
+            for r in range(ps):
+                out[p, h, r] = fp4_row(cache[p, h], ps, dim, r)
+    return out
+
+
+def cache_commit_fp4(k_new, cache, ps, new_len, slots, path_nodes, largest=254):
+    """The cache of bytes [layers, pages, kv_heads, bytes] after a call (keys or values)."""
+    L, B, n1, KH, dim = k_new.shape
+    cache = cache.copy()
+    for b in range(B):
+        for k in range(min(int(new_len[b]), slots.shape[1])):
+            node = k
+            if path_nodes is not None and k > 0:
+                node = int(path_nodes[b, k - 1]) if k <= path_nodes.shape[1] else -1
+            s = int(slots[b, k])
+            if 0 <= s < cache.shape[1] * ps and 0 <= node < n1:
+                for i in range(L):
+                    for h in range(KH):
+                        fp4_put(cache[i, s // ps, h], ps, dim, s % ps, k_new[i, b, node, h], largest)
+    return cache
+
+
+def cache_read_fp4(cache, ps, dim, table, first, length, row_start, out):
+    """``out`` [layers, rows, kv_heads, D] after a call (keys or values)."""
+    out = out.copy()
+    for b in range(len(length)):
+        for k in range(int(length[b])):
+            x, to = int(first[b]) + k, int(row_start[b]) + k
+            if not 0 <= to < out.shape[1]:
+                continue
+            page = int(table[b, x // ps]) if 0 <= x < table.shape[1] * ps else -1
+            for i in range(out.shape[0]):
+                for h in range(out.shape[2]):
+                    out[i, to, h] = fp4_row(cache[i, page, h], ps, dim, x % ps) \
+                        if 0 <= page < cache.shape[1] else np.nan
+    return out

@@ -26,4 +26,7 @@ from ._lib import (  # noqa: F401
     tv_tree_attention_workspace_size, tv_tree_attention, tree_attention,
     tv_process_logits_workspace_size, tv_process_logits, process_logits,
     tv_cache_extend, cache_extend, CacheGrowth, tv_cache_commit, cache_commit,
+    tv_prompt_attention_workspace_size, tv_prompt_attention, prompt_attention,
+    TV_FP4_BLOCK, TV_FP4_BLOCK_BYTES, tv_fp4_page_bytes, fp4_cache_shape, tv_cache_commit_fp4,
+    cache_commit_fp4, tv_cache_read_fp4, cache_read_fp4, tv_tree_attention_fp4, tree_attention_fp4,
 )

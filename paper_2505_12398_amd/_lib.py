@@ -27,6 +27,7 @@ TV_MAX_HISTORY = 1 << 24
 TV_MAX_BIAS = 1 << 16
 TV_MAX_NEW = 1 << 20
 TV_MAX_LAYERS = 4096
+TV_FP4_BLOCK, TV_FP4_BLOCK_BYTES = 32, 17
 TV_CACHE_RELEASE = -(1 << 31)
 TV_CACHE_OK, TV_CACHE_FULL, TV_CACHE_OVERFLOW, TV_CACHE_BAD_LENGTH = range(4)
 
@@ -106,6 +107,21 @@ def load_library(path: str = LIB_PATH):
         lib.tv_cache_commit.argtypes = ([i32] * 5 + [ptr, ptr, i64, i64, ptr, ptr, i64, i64, i32,
                                                      i32, ptr, i32, ptr, ptr, i32, ptr])
         lib.tv_cache_commit.restype = ctypes.c_int
+        lib.tv_prompt_attention_workspace_size.argtypes = [i32] * 6
+        lib.tv_prompt_attention_workspace_size.restype = size
+        lib.tv_prompt_attention.argtypes = (
+            [i32] * 7 + [ptr, i64, ptr, ptr, i64, ptr, ptr, ctypes.c_float, ptr, ptr, size, ptr])
+        lib.tv_prompt_attention.restype = ctypes.c_int
+        lib.tv_fp4_page_bytes.argtypes = [i32, i32]
+        lib.tv_fp4_page_bytes.restype = size
+        lib.tv_cache_commit_fp4.argtypes = [i32] + lib.tv_cache_commit.argtypes
+        lib.tv_cache_commit_fp4.restype = ctypes.c_int
+        lib.tv_cache_read_fp4.argtypes = (
+            [i32] * 5 + [ptr, ptr, i64, i64, i32, i32, ptr, i32, ptr, ptr, ptr, i32, ptr, ptr, i64,
+                         i64, ptr])
+        lib.tv_cache_read_fp4.restype = ctypes.c_int
+        lib.tv_tree_attention_fp4.argtypes = lib.tv_tree_attention.argtypes
+        lib.tv_tree_attention_fp4.restype = ctypes.c_int
         lib.tv_status_string.argtypes = [ctypes.c_int]
         lib.tv_status_string.restype = ctypes.c_char_p
         _lib = lib
@@ -375,6 +391,70 @@ def tv_cache_commit(layers, batch, num_nodes, kv_heads, head_bytes, k_new, v_new
         int(max_new), _ptr(slots), _ptr(path_nodes), int(path_width), _ptr(stream)))
 
 
+def tv_prompt_attention_workspace_size(batch, num_queries, num_keys, heads, kv_heads,
+                                       head_dim) -> int:
+    return int(load_library().tv_prompt_attention_workspace_size(
+        batch, num_queries, num_keys, heads, kv_heads, head_dim))
+
+
+def tv_prompt_attention(batch, num_queries, num_keys, heads, kv_heads, head_dim, dtype, q, q_stride,
+                        k, v, kv_stride, q_start, k_start, scale, out, workspace, workspace_bytes,
+                        stream=None) -> int:
+    """C-ABI ``tv_prompt_attention``: pointers may be torch tensors or raw ints;
+    returns the status."""
+    return int(load_library().tv_prompt_attention(
+        int(batch), int(num_queries), int(num_keys), int(heads), int(kv_heads), int(head_dim),
+        int(dtype), _ptr(q), int(q_stride), _ptr(k), _ptr(v), int(kv_stride), _ptr(q_start),
+        _ptr(k_start), float(scale), _ptr(out), _ptr(workspace), int(workspace_bytes),
+        _ptr(stream)))
+
+
+def tv_fp4_page_bytes(page_size, head_dim) -> int:
+    return int(load_library().tv_fp4_page_bytes(page_size, head_dim))
+
+
+def tv_cache_commit_fp4(layers, batch, num_nodes, kv_heads, head_dim, dtype, k_new, v_new,
+                        new_layer_stride, node_stride, k_cache, v_cache, cache_layer_stride,
+                        page_stride, num_pages, page_size, new_len, max_new, slots, path_nodes,
+                        path_width, stream=None) -> int:
+    """C-ABI ``tv_cache_commit_fp4`` (the caches' strides in bytes): pointers may be
+    torch tensors or raw ints; returns the status."""
+    return int(load_library().tv_cache_commit_fp4(
+        int(layers), int(batch), int(num_nodes), int(kv_heads), int(head_dim), int(dtype),
+        _ptr(k_new), _ptr(v_new), int(new_layer_stride), int(node_stride), _ptr(k_cache),
+        _ptr(v_cache), int(cache_layer_stride), int(page_stride), int(num_pages), int(page_size),
+        _ptr(new_len), int(max_new), _ptr(slots), _ptr(path_nodes), int(path_width),
+        _ptr(stream)))
+
+
+def tv_cache_read_fp4(layers, batch, kv_heads, head_dim, dtype, k_cache, v_cache,
+                      cache_layer_stride, page_stride, num_pages, page_size, block_table,
+                      table_width, first, length, row_start, num_rows, k_out, v_out,
+                      out_layer_stride, row_stride, stream=None) -> int:
+    """C-ABI ``tv_cache_read_fp4`` (the caches' strides in bytes): pointers may be
+    torch tensors or raw ints; returns the status."""
+    return int(load_library().tv_cache_read_fp4(
+        int(layers), int(batch), int(kv_heads), int(head_dim), int(dtype), _ptr(k_cache),
+        _ptr(v_cache), int(cache_layer_stride), int(page_stride), int(num_pages), int(page_size),
+        _ptr(block_table), int(table_width), _ptr(first), _ptr(length), _ptr(row_start),
+        int(num_rows), _ptr(k_out), _ptr(v_out), int(out_layer_stride), int(row_stride),
+        _ptr(stream)))
+
+
+def tv_tree_attention_fp4(batch, num_nodes, heads, kv_heads, head_dim, dtype, parents, q, q_stride,
+                          k_new, v_new, kv_stride, k_cache, v_cache, page_stride, num_pages,
+                          page_size, block_table, table_width, ctx_len, prefix_pages, prefix_len,
+                          scale, out, workspace, workspace_bytes, stream=None) -> int:
+    """C-ABI ``tv_tree_attention_fp4`` (page_stride in bytes): pointers may be torch
+    tensors or raw ints; returns the status."""
+    return int(load_library().tv_tree_attention_fp4(
+        int(batch), int(num_nodes), int(heads), int(kv_heads), int(head_dim), int(dtype),
+        _ptr(parents), _ptr(q), int(q_stride), _ptr(k_new), _ptr(v_new), int(kv_stride),
+        _ptr(k_cache), _ptr(v_cache), int(page_stride), int(num_pages), int(page_size),
+        _ptr(block_table), int(table_width), _ptr(ctx_len), _ptr(prefix_pages), int(prefix_len),
+        float(scale), _ptr(out), _ptr(workspace), int(workspace_bytes), _ptr(stream)))
+
+
 def _check(name, t, shape, dtype, dev):
     """``t`` contiguous on ``dev`` with that shape and type (None passes); its address."""
     if t is None:
@@ -522,6 +602,138 @@ def tree_attention(q, k_new, v_new, parents, k_cache, v_cache, block_table, ctx_
     return out
 
 
+def _packed(name, t, dev, dtype, shape):
+    """Stride between the rows of a [rows, heads, head_dim] tensor, each row's heads together (a
+    slice of a projection's output)."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    n, H, D = shape
+    sn, sh, sd = t.stride()
+    if t.device != dev or sd != 1 and D > 1 or sh != D and H > 1:
+        raise ValueError(f"{name}: rows must lie on {dev}, their heads contiguous")
+    return sn if n > 1 else H * D
+
+
+def _pages4(name, t, dev, shape):
+    """Stride between the pages of a [pages, kv_heads, bytes of a head's page] cache of 4 bits."""
+    if t.dtype != _uint8():
+        raise TypeError(f"{name} must be torch.uint8, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    P, KH, size = shape
+    sp, sh, sb = t.stride()
+    if t.device != dev or sb != 1 or sh != size and KH > 1:
+        raise ValueError(f"{name}: pages must be contiguous on {dev}")
+    return sp if P > 1 else KH * size
+
+
+def _uint8():
+    import torch
+    return torch.uint8
+
+
+def _code16(what, dtype):
+    import torch
+    if dtype == torch.bfloat16:
+        return TV_DTYPE_BF16
+    if dtype != torch.float16:
+        raise TypeError(f"{what} must be bfloat16 or float16, got {dtype}")
+    return TV_DTYPE_F16
+
+
+def fp4_cache_shape(pages, kv_heads, page_size, head_dim):
+    """Shape of one layer's uint8 tensor of a cache of 4 bits, for keys or for values."""
+    size = tv_fp4_page_bytes(page_size, head_dim)
+    if not size:
+        raise TvError(TV_ERR_UNSUPPORTED, f"a cache of 4 bits of pages of {page_size} rows of {head_dim}")
+    return pages, kv_heads, size
+
+
+def prompt_attention(q, k, v, q_start, scale, k_start=None, out=None, stream=None, workspace=None):
+    """Causal attention of packed prompts (``tv_prompt_attention``): q [queries, heads, D], k and v
+    [keys, kv_heads, D] (bfloat16 or float16; views of one projection's output will do); sequence b
+    has the rows q_start[b] .. q_start[b + 1] - 1 of q and k_start[b] .. k_start[b + 1] - 1 of k and v
+    (int32 [B + 1]; ``k_start`` None: the same), its queries being the last positions of its keys.
+    Returns out [queries, heads, D] (rows of no sequence are left as they were; new tensors hold
+    nothing there); raises on a non-OK return."""
+    import torch
+    if q.dim() != 3 or k.dim() != 3 or q_start.dim() != 1 or not len(q_start):
+        raise ValueError("q, k and v have three dimensions, q_start one and at least one entry")
+    (nq, H, D), (nk, KH, _), B = q.shape, k.shape, q_start.shape[0] - 1
+    dev, dt, i32 = q.device, q.dtype, torch.int32
+    code = _code16("q", dt)
+    q_stride = _packed("q", q, dev, dt, (nq, H, D))
+    kv_stride = _packed("k", k, dev, dt, (nk, KH, D))
+    if _packed("v", v, dev, dt, (nk, KH, D)) != kv_stride:
+        raise ValueError("k and v must have the same strides")
+    if k_start is None and nk != nq:
+        raise ValueError(f"{nk} keys for {nq} queries need a k_start")
+    qs = _check("q_start", q_start, (B + 1,), i32, dev)
+    ks = _check("k_start", k_start, (B + 1,), i32, dev)
+    lib = load_library()
+    with _On(dev, stream) as at:
+        if out is None:
+            out = torch.empty((nq, H, D), dtype=dt, device=dev)
+        to = _check("out", out, (nq, H, D), dt, dev)
+        ws, nbytes = _workspace(
+            lib.tv_prompt_attention_workspace_size(B, nq, nk, H, KH, D), workspace, dev)
+        if B and nq:
+            _on_gpu(dev, "tv_prompt_attention")
+        st = lib.tv_prompt_attention(B, nq, nk, H, KH, D, code, q.data_ptr(), q_stride, k.data_ptr(),
+                                     v.data_ptr(), kv_stride, qs, ks, scale, to, ws.data_ptr(),
+                                     nbytes, at)
+    if st != TV_OK:
+        raise TvError(st, "tv_prompt_attention")
+    return out
+
+
+def tree_attention_fp4(q, k_new, v_new, parents, k_cache, v_cache, page_size, block_table, ctx_len,
+                       scale, prefix_len=0, prefix_pages=None, out=None, stream=None,
+                       workspace=None):
+    """``tree_attention`` over a cache of 4 bits (``tv_tree_attention_fp4``): k_cache and v_cache
+    uint8 [pages, kv_heads, bytes] (``fp4_cache_shape``) of ``page_size`` rows a page."""
+    import torch
+    if q.dim() != 4 or k_new.dim() != 4 or k_cache.dim() != 3:
+        raise ValueError("q, k_new and v_new have four dimensions, the caches three")
+    B, n1, H, D = q.shape
+    P, KH, _ = k_cache.shape
+    dev, dt, i32 = q.device, q.dtype, torch.int32
+    code = _code16("q", dt)
+    q_stride = _rows("q", q, dev, dt, (B, n1, H, D))
+    kv_stride = _rows("k_new", k_new, dev, dt, (B, n1, KH, D))
+    if _rows("v_new", v_new, dev, dt, (B, n1, KH, D)) != kv_stride:
+        raise ValueError("k_new and v_new must have the same strides")
+    shape = fp4_cache_shape(P, KH, page_size, D)
+    page_stride = _pages4("k_cache", k_cache, dev, shape)
+    if _pages4("v_cache", v_cache, dev, shape) != page_stride:
+        raise ValueError("k_cache and v_cache must have the same strides")
+    width = block_table.shape[-1]
+    parents = _check("parents", parents, (B, n1), i32, dev)
+    table = _check("block_table", block_table, (B, width), i32, dev)
+    ctx = _check("ctx_len", ctx_len, (B,), i32, dev)
+    prefix = _check("prefix_pages", prefix_pages, (prefix_len // page_size,), i32, dev)
+    if prefix_len and prefix_pages is None:
+        prefix = table
+    lib = load_library()
+    with _On(dev, stream) as at:
+        if out is None:
+            out = torch.empty((B, n1, H, D), dtype=dt, device=dev)
+        to = _check("out", out, (B, n1, H, D), dt, dev)
+        ws, nbytes = _workspace(
+            lib.tv_tree_attention_workspace_size(B, n1, H, KH, D, prefix_len), workspace, dev)
+        if B:
+            _on_gpu(dev, "tv_tree_attention_fp4")
+        st = lib.tv_tree_attention_fp4(
+            B, n1, H, KH, D, code, parents, q.data_ptr(), q_stride, k_new.data_ptr(),
+            v_new.data_ptr(), kv_stride, k_cache.data_ptr(), v_cache.data_ptr(), page_stride, P,
+            page_size, table, width, ctx, prefix, prefix_len, scale, to, ws.data_ptr(), nbytes, at)
+    if st != TV_OK:
+        raise TvError(st, "tv_tree_attention_fp4")
+    return out
+
+
 def process_logits(logits, temperature, parents=None, tokens=None, history=None, history_len=None,
                    prompt_len=None, repetition=None, presence=None, frequency=None,
                    bias_tokens=None, bias_values=None, masks=None, mask_index=None, nodes=None,
@@ -663,6 +875,105 @@ def cache_commit(k_new, v_new, k_cache, v_cache, new_len, slots, path_nodes=None
             at_slots, path, width, at)
     if st != TV_OK:
         raise TvError(st, "tv_cache_commit")
+
+
+def _layers4(k_cache, v_cache, page_size, head_dim, dev):
+    """Layers, pages, key heads and strides between layers and pages of the caches of 4 bits
+    [layers, pages, kv_heads, bytes]."""
+    if k_cache.dim() != 4 or v_cache.dim() != 4 or v_cache.shape[0] != k_cache.shape[0]:
+        raise ValueError("the caches have four dimensions and as many layers")
+    L, P, KH, _ = k_cache.shape
+    shape = fp4_cache_shape(P, KH, page_size, head_dim)
+    if L == 0:
+        return L, P, KH, 0, 0
+    page = _pages4("k_cache", k_cache[0], dev, shape)
+    layer = k_cache.stride(0) if L > 1 else 0
+    if _pages4("v_cache", v_cache[0], dev, shape) != page or L > 1 and v_cache.stride(0) != layer:
+        raise ValueError("k_cache and v_cache must have the same strides")
+    return L, P, KH, layer, page
+
+
+def cache_commit_fp4(k_new, v_new, k_cache, v_cache, page_size, new_len, slots, path_nodes=None,
+                     stream=None):
+    """``cache_commit`` into a cache of 4 bits (``tv_cache_commit_fp4``): k_new and v_new
+    [layers, B, N+1, kv_heads, D] bfloat16 or float16, k_cache and v_cache uint8
+    [layers, pages, kv_heads, bytes] (``fp4_cache_shape``) of ``page_size`` rows a page."""
+    if k_new.dim() != 5 or v_new.dim() != 5 or v_new.shape[0] != k_new.shape[0]:
+        raise ValueError("k_new and v_new have five dimensions and as many layers")
+    _, B, n1, KH, D = k_new.shape
+    dev, dt = k_cache.device, k_new.dtype
+    code = _code16("k_new", dt)
+    L, P, heads, layer, page = _layers4(k_cache, v_cache, page_size, D, dev)
+    if k_new.shape[0] != L or heads != KH:
+        raise ValueError(f"k_new has {k_new.shape[0]} layers of {KH} heads, the caches {L} of {heads}")
+    if L == 0:
+        return
+    node = _rows("k_new", k_new[0], dev, dt, (B, n1, KH, D))
+    new_layer = k_new.stride(0) if L > 1 else 0
+    if _rows("v_new", v_new[0], dev, dt, (B, n1, KH, D)) != node or \
+            L > 1 and v_new.stride(0) != new_layer:
+        raise ValueError("k_new and v_new must have the same strides")
+    import torch
+    i32, most, width, path = torch.int32, slots.shape[-1], 0, None
+    new = _check("new_len", new_len, (B,), i32, dev)
+    at_slots = _check("slots", slots, (B, most), i32, dev)
+    with _On(dev, stream) as at:
+        if path_nodes is not None:
+            width = path_nodes.shape[-1]
+            path_nodes = path_nodes.contiguous()
+            path = _check("path_nodes", path_nodes, (B, width), i32, dev)
+        if B and most and P:
+            _on_gpu(dev, "tv_cache_commit_fp4")
+        st = load_library().tv_cache_commit_fp4(
+            L, B, n1, KH, D, code, k_new.data_ptr(), v_new.data_ptr(), new_layer, node,
+            k_cache.data_ptr(), v_cache.data_ptr(), layer, page, P, page_size, new, most, at_slots,
+            path, width, at)
+    if st != TV_OK:
+        raise TvError(st, "tv_cache_commit_fp4")
+
+
+def cache_read_fp4(k_cache, v_cache, page_size, block_table, length, row_start, rows, first=None,
+                   dtype=None, out=None, stream=None):
+    """Positions first[b] .. first[b] + length[b] - 1 of every request (``first`` None: from 0) out of
+    a cache of 4 bits [layers, pages, kv_heads, bytes] into rows row_start[b] .. of two tensors
+    [layers, ``rows``, kv_heads, D] (``tv_cache_read_fp4``; int32 tensors [B], block_table
+    [B, width]): new ones of ``dtype`` (bfloat16 by default), or ``out`` = (k, v), whose rows may
+    lie apart. Returns them; rows that no request names are left as they were (new tensors hold
+    nothing there). Raises on a non-OK return."""
+    import torch
+    dev, i32 = k_cache.device, torch.int32
+    if k_cache.dim() != 4 or block_table.dim() != 2:
+        raise ValueError("the caches have four dimensions, block_table two")
+    D = k_cache.shape[-1] * TV_FP4_BLOCK // (page_size * TV_FP4_BLOCK_BYTES) if page_size > 0 else 0
+    L, P, KH, layer, page = _layers4(k_cache, v_cache, page_size, D, dev)
+    B, width = block_table.shape
+    table = _check("block_table", block_table, (B, width), i32, dev)
+    n = _check("length", length, (B,), i32, dev)
+    to = _check("row_start", row_start, (B,), i32, dev)
+    begin = _check("first", first, (B,), i32, dev)
+    with _On(dev, stream) as at:
+        if out is None:
+            dtype = torch.bfloat16 if dtype is None else dtype
+            out = tuple(torch.empty((L, rows, KH, D), dtype=dtype, device=dev) for _ in range(2))
+        k, v = out
+        dt = k.dtype
+        code = _code16("k", dt)
+        if k.dim() != 4 or v.dim() != 4 or k.shape[0] != L or v.shape[0] != L:
+            raise ValueError(f"the outputs have four dimensions and {L} layers")
+        if L == 0:
+            return out
+        row = _packed("k", k[0], dev, dt, (rows, KH, D))
+        out_layer = k.stride(0) if L > 1 else 0
+        if _packed("v", v[0], dev, dt, (rows, KH, D)) != row or L > 1 and v.stride(0) != out_layer:
+            raise ValueError("k and v must have the same strides")
+        if B and rows:
+            _on_gpu(dev, "tv_cache_read_fp4")
+        st = load_library().tv_cache_read_fp4(
+            L, B, KH, D, code, k_cache.data_ptr(), v_cache.data_ptr(), layer, page, P, page_size,
+            table, width, begin, n, to, rows, k.data_ptr(), v.data_ptr(), out_layer, row, at)
+    if st != TV_OK:
+        raise TvError(st, "tv_cache_read_fp4")
+    return out
 
 
 def workspace_tensor(batch: int, num_nodes: int, vocab: int, device):

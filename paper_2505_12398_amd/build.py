@@ -3,6 +3,8 @@
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -11,7 +13,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libtv.so")
 
 SOURCES = ["tv_abi.cpp", "tv_ops_abi.cpp", "tv_kernels.hip", "tv_commit.hip", "tv_lmhead.hip",
-           "tv_logits.hip", "tv_cache.hip", "tv_attention.hip"]
+           "tv_logits.hip", "tv_cache.hip", "tv_fp4.hip", "tv_attention.hip",
+           "tv_attention_fp4.hip", "tv_prompt.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
@@ -26,11 +29,20 @@ FLAGS = [
 def build(verbose: bool = False) -> str:
     """Compile every source into paper_2505_12398_amd/libtv.so; returns its path."""
     tmp = LIB + ".tmp"
-    cmd = [HIPCC, *FLAGS, "-I", INCLUDE, "-I", CSRC,
-           *[os.path.join(CSRC, s) for s in SOURCES], "-o", tmp]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    compile_flags = [f for f in FLAGS if f != "-shared"]
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True)
+
+    with tempfile.TemporaryDirectory() as out:
+        objects = [os.path.join(out, s + ".o") for s in SOURCES]
+        with ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+            list(pool.map(lambda so: run([HIPCC, *compile_flags, "-I", INCLUDE, "-I", CSRC, "-c",
+                                          os.path.join(CSRC, so[0]), "-o", so[1]]),
+                          zip(SOURCES, objects)))
+        run([HIPCC, "--offload-arch=gfx950", "-shared", *objects, "-o", tmp])
     os.replace(tmp, LIB)
     return LIB
 

@@ -174,7 +174,7 @@ struct AttentionArgs {
   int64_t kv_stride;
   const void* k_cache;
   const void* v_cache;
-  int64_t page_stride;          // elements
+  int64_t page_stride;          // elements (a cache of 4 bits: bytes)
   int32_t num_pages, page_size;
   const int32_t* block_table;
   int32_t table_width;
@@ -189,8 +189,10 @@ struct AttentionArgs {
 size_t attention_workspace(int32_t batch, int32_t num_nodes, int32_t heads, int32_t kv_heads,
                            int32_t head_dim, int32_t prefix_len);
 
-// Enqueue the attention on `stream` (arguments validated).
+// Enqueue the attention on `stream` (arguments validated), over a cache of 16-bit keys
+// and values or of 4 bits.
 int launch_attention(const AttentionArgs& a, void* workspace, hipStream_t stream);
+int launch_attention_fp4(const AttentionArgs& a, void* workspace, hipStream_t stream);
 
 // Penalties, biases and masks on logits (tv_process_logits).
 struct LogitsArgs {
@@ -279,6 +281,70 @@ struct CacheCommitArgs {
 
 // Enqueue the writes on `stream` (arguments validated).
 int launch_cache_commit(const CacheCommitArgs& a, hipStream_t stream);
+
+// Committed keys and values into a cache of 4 bits (tv_cache_commit_fp4). New ones' strides
+// in elements, the cache's in bytes.
+struct Fp4CommitArgs {
+  int32_t layers, batch, num_nodes, kv_heads, head_dim;
+  int32_t dtype;                // TV_DTYPE_BF16 or TV_DTYPE_F16
+  const void* k_new;
+  const void* v_new;
+  int64_t new_layer_stride, node_stride;
+  void* k_cache;
+  void* v_cache;
+  int64_t cache_layer_stride, page_stride;
+  int32_t num_pages, page_size;
+  const int32_t* new_len;
+  int32_t max_new;
+  const int32_t* slots;
+  const int32_t* path_nodes;
+  int32_t path_width;
+};
+
+// Positions out of a cache of 4 bits (tv_cache_read_fp4).
+struct Fp4ReadArgs {
+  int32_t layers, batch, kv_heads, head_dim;
+  int32_t dtype;                // TV_DTYPE_BF16 or TV_DTYPE_F16
+  const void* k_cache;
+  const void* v_cache;
+  int64_t cache_layer_stride, page_stride;   // bytes
+  int32_t num_pages, page_size;
+  const int32_t* block_table;
+  int32_t table_width;
+  const int32_t* first;
+  const int32_t* length;
+  const int32_t* row_start;
+  int32_t num_rows;
+  void* k_out;
+  void* v_out;
+  int64_t out_layer_stride, row_stride;      // elements
+};
+
+// Enqueue the writes, and the reads, on `stream` (arguments validated).
+int launch_cache_commit_fp4(const Fp4CommitArgs& a, hipStream_t stream);
+int launch_cache_read_fp4(const Fp4ReadArgs& a, hipStream_t stream);
+
+// Causal attention of packed prompts (tv_prompt_attention).
+struct PromptArgs {
+  int32_t batch, num_queries, num_keys, heads, kv_heads, head_dim;
+  int32_t dtype;                // TV_DTYPE_BF16 or TV_DTYPE_F16
+  const void* q;
+  int64_t q_stride;             // elements between rows
+  const void* k;
+  const void* v;
+  int64_t kv_stride;
+  const int32_t* q_start;
+  const int32_t* k_start;
+  float scale;
+  void* out;
+};
+
+// Bytes of workspace of a call (sizes validated).
+size_t prompt_workspace(int32_t batch, int32_t num_queries, int32_t num_keys, int32_t heads,
+                        int32_t kv_heads, int32_t head_dim);
+
+// Enqueue the attention on `stream` (arguments validated).
+int launch_prompt(const PromptArgs& a, void* workspace, hipStream_t stream);
 
 // Enqueue the verification on `stream` (an initialisation kernel, then the
 // verifier). Arguments already validated. Returns a tv_status_t.

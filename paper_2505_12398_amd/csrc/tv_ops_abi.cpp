@@ -1,6 +1,6 @@
 // C-ABI entry points of the operators around a verification (attention over the
-// paged cache, logits processing, growth and commit of the cache; declared in
-// include/tv.h): argument validation on the host, then the launches on the
+// paged cache and of prompts, logits processing, growth and commit of the cache, the
+// cache of 4 bits; declared in include/tv.h): argument validation on the host, then the launches on the
 // caller's stream. Nothing here touches the GPU before the arguments are known
 // to be valid.
 #include <math.h>
@@ -34,7 +34,17 @@ int attention_sizes(int32_t batch, int32_t num_nodes, int32_t heads, int32_t kv_
   return TV_OK;
 }
 
-int validate(const tv::AttentionArgs& a, void* workspace, size_t workspace_bytes) {
+// Bytes of a head of a page of 4 bits; 0 for sizes that are not taken.
+int64_t fp4_page_bytes(int32_t page_size, int32_t head_dim) {
+  if (!page_size_ok(page_size) || head_dim < 1 || head_dim > TV_MAX_HEAD_DIM ||
+      head_dim % TV_FP4_BLOCK)
+    return 0;
+  return static_cast<int64_t>(page_size) * (head_dim / TV_FP4_BLOCK) * TV_FP4_BLOCK_BYTES;
+}
+
+// fp4: the cache is of 4 bits, its page_stride in bytes.
+int validate(const tv::AttentionArgs& a, void* workspace, size_t workspace_bytes,
+             bool fp4 = false) {
   const int st =
       attention_sizes(a.batch, a.num_nodes, a.heads, a.kv_heads, a.head_dim, a.prefix_len);
   if (st != TV_OK) return st;
@@ -47,10 +57,13 @@ int validate(const tv::AttentionArgs& a, void* workspace, size_t workspace_bytes
   const int64_t kv_row = static_cast<int64_t>(a.kv_heads) * a.head_dim;
   if (a.q_stride < static_cast<int64_t>(a.heads) * a.head_dim || a.kv_stride < kv_row)
     return TV_ERR_INVALID_ARG;
-  if (a.num_pages > 0 && a.page_stride < kv_row * a.page_size) return TV_ERR_INVALID_ARG;
-  if (a.q_stride % 8 || a.kv_stride % 8 || a.page_stride % 8) return TV_ERR_UNSUPPORTED;
+  const int64_t head = fp4 ? fp4_page_bytes(a.page_size, a.head_dim) : 0;
+  if (fp4 && !head) return TV_ERR_UNSUPPORTED;
+  if (a.num_pages > 0 && a.page_stride < (fp4 ? a.kv_heads * head : kv_row * a.page_size))
+    return TV_ERR_INVALID_ARG;
+  if (a.q_stride % 8 || a.kv_stride % 8 || a.page_stride % (fp4 ? 16 : 8)) return TV_ERR_UNSUPPORTED;
   if (a.q_stride > kMaxBytes / 2 / a.num_nodes || a.kv_stride > kMaxBytes / 2 / a.num_nodes ||
-      a.page_stride > kMaxBytes / 2)
+      a.page_stride > (fp4 ? kMaxBytes : kMaxBytes / 2))
     return TV_ERR_UNSUPPORTED;
   if (a.batch == 0) return TV_OK;
   if (!a.q || !a.k_new || !a.v_new || !a.ctx_len || !a.out || (a.num_nodes > 1 && !a.parents))
@@ -134,7 +147,8 @@ int validate(const tv::ExtendArgs& a) {
 
 // Whether pages of two layers share bytes: layers begin cache_layer_stride apart, and a
 // layer's pages of `size` bytes page_stride (no less).
-bool layers_overlap(const tv::CacheCommitArgs& a, int64_t size) {
+template <class Args>
+bool layers_overlap(const Args& a, int64_t size) {
   using Wide = __int128;
   const Wide apart = a.cache_layer_stride < 0 ? -static_cast<Wide>(a.cache_layer_stride)
                                               : static_cast<Wide>(a.cache_layer_stride);
@@ -171,6 +185,100 @@ int validate(const tv::CacheCommitArgs& a) {
     if (bits(p) % 16) return TV_ERR_INVALID_ARG;
   for (const int32_t* p : {a.new_len, a.slots, a.path_nodes})
     if (bits(p) % 4) return TV_ERR_INVALID_ARG;
+  return TV_OK;
+}
+
+// What a commit into a cache of 4 bits and a read from it have in common; the bytes of a head of
+// a page in `head`.
+template <class Args>
+int fp4_sizes(const Args& a, int64_t* head) {
+  if (a.layers < 0 || a.batch < 0 || a.kv_heads < 1 || a.head_dim < 1 || a.num_pages < 0 ||
+      a.page_size < 1)
+    return TV_ERR_INVALID_ARG;
+  if (a.dtype != TV_DTYPE_BF16 && a.dtype != TV_DTYPE_F16) return TV_ERR_INVALID_ARG;
+  *head = fp4_page_bytes(a.page_size, a.head_dim);
+  if (!*head || a.layers > TV_MAX_LAYERS || a.batch > TV_MAX_BATCH ||
+      static_cast<int64_t>(a.kv_heads) * a.head_dim > TV_MAX_HIDDEN ||
+      a.num_pages > INT32_MAX / a.page_size)
+    return TV_ERR_UNSUPPORTED;
+  if (a.num_pages > 0 && a.page_stride < a.kv_heads * *head) return TV_ERR_INVALID_ARG;
+  if (a.cache_layer_stride % 16 || a.page_stride % 16) return TV_ERR_UNSUPPORTED;
+  return TV_OK;
+}
+
+int validate(const tv::Fp4CommitArgs& a) {
+  if (a.num_nodes < 1 || a.max_new < 0 || a.path_width < 0) return TV_ERR_INVALID_ARG;
+  int64_t head = 0;
+  const int st = fp4_sizes(a, &head);
+  if (st != TV_OK) return st;
+  if (a.max_new > TV_MAX_NEW) return TV_ERR_UNSUPPORTED;
+  if (a.node_stride < static_cast<int64_t>(a.kv_heads) * a.head_dim) return TV_ERR_INVALID_ARG;
+  if (a.num_pages > 0 && layers_overlap(a, a.kv_heads * head)) return TV_ERR_INVALID_ARG;
+  if (a.new_layer_stride % 8 || a.node_stride % 8) return TV_ERR_UNSUPPORTED;
+  if (a.layers == 0 || a.batch == 0 || a.max_new == 0 || a.num_pages == 0) return TV_OK;
+  if (!a.k_new || !a.v_new || !a.k_cache || !a.v_cache || !a.new_len || !a.slots)
+    return TV_ERR_INVALID_ARG;
+  for (const void* p : {a.k_new, a.v_new, (const void*)a.k_cache, (const void*)a.v_cache})
+    if (bits(p) % 16) return TV_ERR_INVALID_ARG;
+  for (const int32_t* p : {a.new_len, a.slots, a.path_nodes})
+    if (bits(p) % 4) return TV_ERR_INVALID_ARG;
+  return TV_OK;
+}
+
+int validate(const tv::Fp4ReadArgs& a) {
+  if (a.table_width < 0 || a.num_rows < 0) return TV_ERR_INVALID_ARG;
+  int64_t head = 0;
+  const int st = fp4_sizes(a, &head);
+  if (st != TV_OK) return st;
+  if (a.table_width > INT32_MAX / a.page_size) return TV_ERR_UNSUPPORTED;
+  if (a.row_stride < static_cast<int64_t>(a.kv_heads) * a.head_dim) return TV_ERR_INVALID_ARG;
+  if (a.out_layer_stride % 8 || a.row_stride % 8) return TV_ERR_UNSUPPORTED;
+  if (a.layers == 0 || a.batch == 0 || a.num_rows == 0) return TV_OK;
+  if (!a.length || !a.row_start || !a.k_out || !a.v_out || (a.table_width > 0 && !a.block_table) ||
+      (a.num_pages > 0 && (!a.k_cache || !a.v_cache)))
+    return TV_ERR_INVALID_ARG;
+  for (const void* p : {a.k_cache, a.v_cache, (const void*)a.k_out, (const void*)a.v_out})
+    if (bits(p) % 16) return TV_ERR_INVALID_ARG;
+  for (const int32_t* p : {a.block_table, a.first, a.length, a.row_start})
+    if (bits(p) % 4) return TV_ERR_INVALID_ARG;
+  return TV_OK;
+}
+
+// TV_OK if a prompt attention of these sizes is taken
+int prompt_sizes(int32_t batch, int32_t num_queries, int32_t num_keys, int32_t heads,
+                 int32_t kv_heads, int32_t head_dim) {
+  if (batch < 0 || num_queries < 0 || num_keys < 0 || heads < 1 || kv_heads < 1 || head_dim < 1)
+    return TV_ERR_INVALID_ARG;
+  if (heads % kv_heads) return TV_ERR_INVALID_ARG;
+  if (batch > TV_MAX_BATCH || head_dim > TV_MAX_HEAD_DIM || head_dim % 8 ||
+      static_cast<int64_t>(heads) * head_dim > TV_MAX_HIDDEN ||
+      static_cast<int64_t>(num_queries) * heads >= int64_t{1} << 29 ||
+      static_cast<int64_t>(batch) * kv_heads >= int64_t{1} << 22)
+    return TV_ERR_UNSUPPORTED;
+  return TV_OK;
+}
+
+int validate(const tv::PromptArgs& a, void* workspace, size_t workspace_bytes) {
+  const int st =
+      prompt_sizes(a.batch, a.num_queries, a.num_keys, a.heads, a.kv_heads, a.head_dim);
+  if (st != TV_OK) return st;
+  if (a.dtype != TV_DTYPE_BF16 && a.dtype != TV_DTYPE_F16) return TV_ERR_INVALID_ARG;
+  if (!(a.scale > 0.0f) || !isfinite(a.scale)) return TV_ERR_INVALID_ARG;
+  if (a.scale > kMaxScale) return TV_ERR_UNSUPPORTED;
+  if (a.q_stride < static_cast<int64_t>(a.heads) * a.head_dim ||
+      a.kv_stride < static_cast<int64_t>(a.kv_heads) * a.head_dim)
+    return TV_ERR_INVALID_ARG;
+  if (a.q_stride % 8 || a.kv_stride % 8 || a.kv_stride > int64_t{1} << 24) return TV_ERR_UNSUPPORTED;
+  if (a.batch == 0 || a.num_queries == 0) return TV_OK;
+  if (!a.q || (a.num_keys > 0 && (!a.k || !a.v)) || !a.q_start || !a.out) return TV_ERR_INVALID_ARG;
+  for (const void* p : {a.q, a.k, a.v, (const void*)a.out})
+    if (bits(p) % 16) return TV_ERR_INVALID_ARG;
+  for (const int32_t* p : {a.q_start, a.k_start})
+    if (bits(p) % 4) return TV_ERR_INVALID_ARG;
+  if (!workspace || bits(workspace) % 256 ||
+      workspace_bytes < tv::prompt_workspace(a.batch, a.num_queries, a.num_keys, a.heads,
+                                             a.kv_heads, a.head_dim))
+    return TV_ERR_WORKSPACE;
   return TV_OK;
 }
 
@@ -259,6 +367,82 @@ int tv_cache_commit(int32_t layers, int32_t batch, int32_t num_nodes, int32_t kv
   const int st = validate(a);
   if (st != TV_OK || layers == 0 || batch == 0 || max_new == 0 || num_pages == 0) return st;
   return tv::launch_cache_commit(a, stream);
+}
+
+size_t tv_prompt_attention_workspace_size(int32_t batch, int32_t num_queries, int32_t num_keys,
+                                          int32_t heads, int32_t kv_heads, int32_t head_dim) {
+  if (batch < 1 || num_queries < 1 ||
+      prompt_sizes(batch, num_queries, num_keys, heads, kv_heads, head_dim) != TV_OK)
+    return 0;
+  return tv::prompt_workspace(batch, num_queries, num_keys, heads, kv_heads, head_dim);
+}
+
+int tv_prompt_attention(int32_t batch, int32_t num_queries, int32_t num_keys, int32_t heads,
+                        int32_t kv_heads, int32_t head_dim, int32_t dtype, const void* q,
+                        int64_t q_stride, const void* k, const void* v, int64_t kv_stride,
+                        const int32_t* q_start, const int32_t* k_start, float scale, void* out,
+                        void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  const tv::PromptArgs a{batch, num_queries, num_keys, heads,     kv_heads, head_dim,
+                         dtype, q,           q_stride, k,         v,        kv_stride,
+                         q_start, k_start,   scale,    out};
+  const int st = validate(a, workspace, workspace_bytes);
+  if (st != TV_OK || batch == 0 || num_queries == 0) return st;
+  return tv::launch_prompt(a, workspace, stream);
+}
+
+size_t tv_fp4_page_bytes(int32_t page_size, int32_t head_dim) {
+  return static_cast<size_t>(fp4_page_bytes(page_size, head_dim));
+}
+
+int tv_cache_commit_fp4(int32_t layers, int32_t batch, int32_t num_nodes, int32_t kv_heads,
+                        int32_t head_dim, int32_t dtype, const void* k_new, const void* v_new,
+                        int64_t new_layer_stride, int64_t node_stride, void* k_cache, void* v_cache,
+                        int64_t cache_layer_stride, int64_t page_stride, int32_t num_pages,
+                        int32_t page_size, const int32_t* new_len, int32_t max_new,
+                        const int32_t* slots, const int32_t* path_nodes, int32_t path_width,
+                        hipStream_t stream) {
+  const tv::Fp4CommitArgs a{layers,  batch,   num_nodes, kv_heads,    head_dim,
+                            dtype,   k_new,   v_new,     new_layer_stride, node_stride,
+                            k_cache, v_cache, cache_layer_stride, page_stride, num_pages,
+                            page_size, new_len, max_new, slots,       path_nodes,
+                            path_width};
+  const int st = validate(a);
+  if (st != TV_OK || layers == 0 || batch == 0 || max_new == 0 || num_pages == 0) return st;
+  return tv::launch_cache_commit_fp4(a, stream);
+}
+
+int tv_cache_read_fp4(int32_t layers, int32_t batch, int32_t kv_heads, int32_t head_dim, int32_t dtype,
+                      const void* k_cache, const void* v_cache, int64_t cache_layer_stride,
+                      int64_t page_stride, int32_t num_pages, int32_t page_size,
+                      const int32_t* block_table, int32_t table_width, const int32_t* first,
+                      const int32_t* length, const int32_t* row_start, int32_t num_rows, void* k_out,
+                      void* v_out, int64_t out_layer_stride, int64_t row_stride, hipStream_t stream) {
+  const tv::Fp4ReadArgs a{layers,    batch,     kv_heads, head_dim,    dtype,
+                          k_cache,   v_cache,   cache_layer_stride, page_stride, num_pages,
+                          page_size, block_table, table_width, first,  length,
+                          row_start, num_rows,  k_out,    v_out,       out_layer_stride,
+                          row_stride};
+  const int st = validate(a);
+  if (st != TV_OK || layers == 0 || batch == 0 || num_rows == 0) return st;
+  return tv::launch_cache_read_fp4(a, stream);
+}
+
+int tv_tree_attention_fp4(int32_t batch, int32_t num_nodes, int32_t heads, int32_t kv_heads,
+                          int32_t head_dim, int32_t dtype, const int32_t* parents, const void* q,
+                          int64_t q_stride, const void* k_new, const void* v_new, int64_t kv_stride,
+                          const void* k_cache, const void* v_cache, int64_t page_stride,
+                          int32_t num_pages, int32_t page_size, const int32_t* block_table,
+                          int32_t table_width, const int32_t* ctx_len, const int32_t* prefix_pages,
+                          int32_t prefix_len, float scale, void* out, void* workspace,
+                          size_t workspace_bytes, hipStream_t stream) {
+  const tv::AttentionArgs a{batch,     num_nodes,   heads,       kv_heads,  head_dim,
+                            dtype,     parents,     q,           q_stride,  k_new,
+                            v_new,     kv_stride,   k_cache,     v_cache,   page_stride,
+                            num_pages, page_size,   block_table, table_width, ctx_len,
+                            prefix_pages, prefix_len, scale,     out};
+  const int st = validate(a, workspace, workspace_bytes, true);
+  if (st != TV_OK || batch == 0) return st;
+  return tv::launch_attention_fp4(a, workspace, stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,583 @@
+// Causal attention of packed prompts for gfx950 (tv_prompt_attention).
+//
+// The query rows of a sequence and key head, (position, head of the group) in that order, are
+// the columns of a product with the keys: per 32 keys a wavefront forms S^T = K Q^T for its 64
+// rows (32x32x16 products), takes 2^(s k - m k) with k = scale log2(e) in the frame of a running
+// maximum m, and adds V^T P^T to its accumulators (out = sum p v / sum p). A lane holds four
+// consecutive keys of one row at a time, which is how the second product wants its operand, the
+// keys taken in the order in which the lanes hold them; values are read transposed from LDS.
+// Frames and the rounding of weights are those of tv_tree_attention.
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include <mutex>
+
+#include "tv.h"
+#include "tv_attention_common.h"
+#include "tv_launch.h"
+
+namespace {
+
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+
+constexpr int kKeys = 32;                 // keys of a tile
+constexpr int kWaveRows = 64, kWaves = 4, kThreads = 64 * kWaves;
+
+struct Item {                             // rows tile * BM .. of a sequence's query rows
+  int q0, nq, k0, nk, tile, pad[3];
+};
+
+struct Pass {
+  const uint16_t* q;
+  const uint16_t* k;
+  const uint16_t* v;
+  uint16_t* out;
+  int64_t q_stride, kv_stride;            // elements
+  const int32_t* q_start;
+  const int32_t* k_start;
+  int batch, num_queries, num_keys, heads, kv_heads, head_dim, group;
+  float k2;                               // scale log2(e)
+  float slack;                            // how far a score may exceed its frame
+  Item* items;                            // in the order in which they begin (NULL: one sequence)
+  int* count;                             // of items
+};
+
+template <class T>
+__device__ __forceinline__ f32x16 mfma32(s16x8 a, s16x8 b, f32x16 c) {
+  if constexpr (std::is_same<T, Bf16>::value)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// RW row groups of 64 rows, KW key groups that take the tiles in turn and are merged at the end.
+template <int DP_, int RW_>
+struct Shape {
+  static constexpr int DP = DP_, RW = RW_, KW = kWaves / RW_;
+  static constexpr int BM = kWaveRows * RW;
+  static constexpr int MT = 2;                       // blocks of 32 rows of a wavefront
+  static constexpr int KK = DP / 16, DB = DP / 32;   // steps of the first product, blocks of the second
+  static constexpr int CH = DP / 8, ROW = DP * 2;    // 16-byte chunks and bytes of a row
+  static constexpr int MAT = kKeys * ROW, STAGE = 2 * MAT;
+  static constexpr int LOADS = MAT / 1024 / RW;      // of a wavefront, for a tile's keys (or values)
+  static constexpr int S = RW == 1 ? 2 : 4;          // tiles in LDS per key group
+  static constexpr int RING = KW * S * STAGE;
+  static constexpr int ACC = (KW - 1) * RW * MT * DB * 4096;
+  static constexpr int MERGE = ACC + (KW - 1) * RW * MT * 64 * 8;
+  static constexpr int MAIN = RING > MERGE ? RING : MERGE;
+  static constexpr int FLAGS = MAIN, BYTES = FLAGS + 4 * kWaves;
+  static_assert(BYTES <= 160 * 1024, "LDS of a CU");
+  static_assert(S * 2 * LOADS < 64, "the count of loads in flight");
+};
+
+// Sequence b's rows, its starts kept within the tensors.
+__device__ __forceinline__ int clamped(int x, int lo, int hi) { return min(max(x, lo), hi); }
+
+template <class T, class SH>
+__global__ void __launch_bounds__(kThreads, 1) prompt_kernel(Pass P) {
+  constexpr int MT = SH::MT, RW = SH::RW, KW = SH::KW, KK = SH::KK, DB = SH::DB;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[SH::BYTES];
+  lds_byte* const lds = (lds_byte*)smem;
+  const int lds0 = static_cast<int>(reinterpret_cast<uintptr_t>(lds));
+  const int lane = threadIdx.x & 63, wave = uniform(static_cast<int>(threadIdx.x >> 6));
+  const int rg = wave % RW, kg = wave / RW;
+  const int n = lane & 31, h = lane >> 5;
+
+  // the item: consecutive workgroups, and so the XCDs in turn, take its key heads
+  const int rank = blockIdx.x / P.kv_heads, kh = blockIdx.x - rank * P.kv_heads;
+  Item I;
+  if (P.items) {
+    if (rank >= *P.count) return;
+    I = P.items[rank];
+  } else {
+    I.q0 = clamped(P.q_start[0], 0, P.num_queries);
+    I.nq = clamped(P.q_start[1], I.q0, P.num_queries) - I.q0;
+    const int32_t* const ks = P.k_start ? P.k_start : P.q_start;
+    I.k0 = clamped(ks[0], 0, P.num_keys);
+    I.nk = clamped(ks[1], I.k0, P.num_keys) - I.k0;
+    const int tiles = (I.nq * P.group + SH::BM - 1) / SH::BM;
+    if (rank >= tiles) return;
+    I.tile = tiles - 1 - rank;            // the one with the most keys first
+  }
+  const int rows = I.nq * P.group;        // (of all sequences below 2^30)
+  const int r0 = I.tile * SH::BM, rbase = r0 + rg * kWaveRows;
+  const int ctx = I.nk - I.nq;            // row position x sees keys up to x + ctx
+  auto position = [&](int r) { return min(r, rows - 1) / P.group; };
+  const int need = max(0, position(r0 + SH::BM - 1) + ctx + 1);
+  const int tiles = (need + kKeys - 1) / kKeys;
+  // tiles that some rows of this wavefront see, and those that all see whole
+  const int nsome = rbase < rows
+                        ? (max(0, uniform(position(rbase + kWaveRows - 1)) + ctx + 1) + kKeys - 1) / kKeys
+                        : 0;
+  const int nfull = min(nsome, max(0, uniform(position(rbase)) + ctx + 1) / kKeys);
+
+  // queries
+  s16x8 q[MT][KK];
+  int limit[MT];                          // the last key that a row sees
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int r = min(rbase + 32 * mt + n, rows - 1);
+    const int x = r / P.group, g = r - x * P.group;
+    limit[mt] = x + ctx;
+    const uint16_t* const src = P.q + static_cast<int64_t>(I.q0 + x) * P.q_stride +
+                                (kh * P.group + g) * P.head_dim;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      const int d = 16 * kk + 8 * h;
+      q[mt][kk] = d < P.head_dim ? *reinterpret_cast<const s16x8*>(src + d) : s16x8{};
+    }
+  }
+
+  // Loads: instruction i fills 1024 bytes, this lane the chunk at position lane % CH of row
+  // i * 1024 / ROW + lane / CH. Swizzle: a chunk of sixteen rows, and four chunks of four rows,
+  // touch all banks once.
+  auto swizzle = [](int r) {
+    return SH::DP == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
+  };
+  const int stride = static_cast<int>(P.kv_stride) * 2;
+  int kv_off[SH::LOADS];
+#pragma unroll
+  for (int i = 0; i < SH::LOADS; ++i) {
+    const int r = (rg * SH::LOADS + i) * (1024 / SH::ROW) + lane / SH::CH;
+    const int c = (lane % SH::CH) ^ swizzle(r);
+    kv_off[i] = 8 * c < P.head_dim ? r * stride + 16 * c : kPastRange;
+  }
+  const int64_t first = static_cast<int64_t>(I.k0) * P.kv_stride + kh * P.head_dim;
+  const uint64_t k_base = reinterpret_cast<uint64_t>(P.k + first);
+  const uint64_t to_v = reinterpret_cast<uint64_t>(P.v) - reinterpret_cast<uint64_t>(P.k);
+  auto issue = [&](int t, int stage, bool values) {
+    // rows behind the sequence's last key are zeros, so are tiles that are none
+    const int left = t < tiles ? min(kKeys, I.nk - t * kKeys) : 0;
+    const uint64_t a = k_base + static_cast<uint64_t>(min(t, tiles)) * kKeys * stride + (values ? to_v : 0);
+    const i32x4 rs = {static_cast<int>(a), static_cast<int>(a >> 32) & 0xffff, left * stride, 0x00020000};
+    const int to = lds0 + stage + (values ? SH::MAT : 0) + rg * SH::LOADS * 1024;
+#pragma unroll
+    for (int i = 0; i < SH::LOADS; ++i) {
+      const int voff[1] = {kv_off[i]};
+      load_to_lds<1>(rs, voff, to + i * 1024);
+    }
+  };
+  // Reads: keys, row n and chunk 2 kk + h; values, keys 4 h .. 4 h + 3 of 16 by sixteen of the
+  // head, lane i of sixteen the eight bytes i % 4 at key i / 4, transposed by the read.
+  const int k_at = n * SH::ROW + (h ^ swizzle(n & 15)) * 16;
+  const int vrow = 4 * h + ((lane & 15) >> 2);
+  const int v_at = vrow * SH::ROW + ((2 * (lane >> 4 & 1) + ((lane & 3) >> 1)) ^ swizzle(vrow)) * 16 +
+                   (lane & 1) * 8;
+  const int v_hi = (vrow + 8) * SH::ROW +
+                   ((2 * (lane >> 4 & 1) + ((lane & 3) >> 1)) ^ swizzle(vrow + 8)) * 16 + (lane & 1) * 8;
+
+  float m[MT], l[MT], c[MT];
+  f32x16 acc[DB][MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    m[mt] = -INFINITY;
+    l[mt] = c[mt] = 0.0f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) acc[db][mt] = f32x16{};
+  }
+  bool odd = false;                       // a value in a masked tile that is not finite
+
+  auto compute = [&](auto full, int stage, int t) {
+    f32x16 s[MT] = {};
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      const s16x8 a = *(const LDS(s16x8)*)(lds + stage + (k_at ^ (32 * kk)));
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) s[mt] = mfma32<T>(a, q[mt][kk], s[mt]);
+    }
+    if constexpr (!full.value) {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        const int last = limit[mt] - t * kKeys - 4 * h;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          s[mt][r] = 8 * (r >> 2) + (r & 3) <= last ? s[mt][r] : -INFINITY;
+      }
+    }
+    float top[MT];
+    bool moves = false;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      top[mt] = max3(s[mt][0], s[mt][1], s[mt][2]);
+#pragma unroll
+      for (int r = 3; r < 15; r += 2) top[mt] = max3(top[mt], s[mt][r], s[mt][r + 1]);
+      top[mt] = __builtin_elementwise_maximum(top[mt], s[mt][15]);
+      moves |= top[mt] > m[mt] + P.slack;
+    }
+    if (__builtin_amdgcn_ballot_w64(moves)) {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        float u = fmaxf(m[mt], top[mt]);
+        u = fmaxf(u, __shfl_xor(u, 32, 64));
+        u = u > m[mt] + P.slack ? u : m[mt];
+        const float f = to_frame<T>(m[mt], u, P.k2);
+        m[mt] = u;
+        c[mt] = frame<T>(u, P.k2);
+        l[mt] *= f;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) acc[db][mt] *= f;
+      }
+    }
+    s16x8 p[MT][2];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+      for (int sl = 0; sl < 2; ++sl) {
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float e0 = __builtin_amdgcn_exp2f(fmaf(s[mt][8 * sl + 2 * i], P.k2, c[mt]));
+          const float e1 = __builtin_amdgcn_exp2f(fmaf(s[mt][8 * sl + 2 * i + 1], P.k2, c[mt]));
+          w[i] = T::pack(e0, e1);
+          l[mt] = T::plus(l[mt], w[i]);
+        }
+        p[mt][sl] = __builtin_bit_cast(s16x8, w);
+      }
+    }
+    s16x8 v[DB][2];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int sl = 0; sl < 2; ++sl) {
+        const int at = stage + SH::MAT + 16 * sl * SH::ROW;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS(s16x4)*)(lds + at + (v_at ^ (64 * db))));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS(s16x4)*)(lds + at + (v_hi ^ (64 * db))));
+        v[db][sl] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+    if constexpr (!full.value) {
+      // Keys that a row does not see may hold anything: weight 0 times NaN or infinity must not
+      // reach the row. Such values are taken as 0 here and added to the rows that see them when
+      // these are written. (A half word's exponent of ones, plus one, carries into its sign.)
+      constexpr uint32_t kExp = T::kExponent * 0x10001u, kOne = (0x8000u - T::kExponent) * 0x10001u;
+      uint32_t ones = 0;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int sl = 0; sl < 2; ++sl) {
+          const u32x4 w = __builtin_bit_cast(u32x4, v[db][sl]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) ones |= (w[j] & kExp) + kOne;
+        }
+      if (__builtin_amdgcn_ballot_w64((ones & 0x80008000u) != 0)) {
+        odd = true;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int sl = 0; sl < 2; ++sl) {
+            u32x4 w = __builtin_bit_cast(u32x4, v[db][sl]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              w[j] = ((w[j] & T::kExponent) == T::kExponent ? 0 : w[j] & 0xffffu) |
+                     ((w[j] >> 16 & T::kExponent) == T::kExponent ? 0 : w[j] & 0xffff0000u);
+            v[db][sl] = __builtin_bit_cast(s16x8, w);
+          }
+      }
+    }
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int sl = 0; sl < 2; ++sl)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) acc[db][mt] = mfma32<T>(v[db][sl], p[mt][sl], acc[db][mt]);
+  };
+
+  // (left to the compiler, the queries' wait would be one for all loads in flight)
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(q[mt][kk]));
+  const int ring = kg * SH::S * SH::STAGE;
+  const int rounds = (tiles + KW - 1) / KW;
+#pragma unroll
+  for (int j = 0; j < SH::S; ++j) {
+    issue(kg + j * KW, ring + j * SH::STAGE, false);
+    issue(kg + j * KW, ring + j * SH::STAGE, true);
+  }
+  int stage = ring;
+#pragma unroll 1
+  for (int i = 0; i < rounds; ++i) {
+    const int t = i * KW + kg;
+    wait_loads<(SH::S - 1) * 2 * SH::LOADS>();
+    if constexpr (RW > 1) barrier();
+    if (t < nfull) compute(std::true_type{}, stage, t);
+    else if (t < nsome) compute(std::false_type{}, stage, t);
+    if constexpr (RW > 1) barrier();
+    else wait_reads();
+    issue(t + SH::S * KW, stage, false);
+    issue(t + SH::S * KW, stage, true);
+    stage = stage == ring + (SH::S - 1) * SH::STAGE ? ring : stage + SH::STAGE;
+  }
+  wait_loads<0>();                        // (zeros for tiles that are none)
+
+  // the key groups' parts, merged by group 0
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) l[mt] += __shfl_xor(l[mt], 32, 64);
+  LDS(int)* const flags = (LDS(int)*)(lds + SH::FLAGS);
+  if constexpr (KW > 1) {
+    barrier();                            // all have read their last tile
+    if (lane == 0) flags[wave] = odd;
+    if (kg > 0) {
+      const int w = (kg - 1) * RW + rg;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            *(LDS(f32x4)*)(lds + ((w * MT + mt) * DB + db) * 4096 + r * 1024 + lane * 16) =
+                f32x4{acc[db][mt][4 * r], acc[db][mt][4 * r + 1], acc[db][mt][4 * r + 2], acc[db][mt][4 * r + 3]};
+        *(LDS(f32x2)*)(lds + SH::ACC + (w * MT + mt) * 512 + lane * 8) = f32x2{m[mt], l[mt]};
+      }
+    }
+    barrier();
+    if (kg > 0) return;
+#pragma unroll
+    for (int j = 1; j < KW; ++j) odd |= flags[j * RW + rg] != 0;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      f32x2 o[KW];
+      float top = m[mt];
+#pragma unroll
+      for (int j = 1; j < KW; ++j) {
+        o[j] = *(const LDS(f32x2)*)(lds + SH::ACC + (((j - 1) * RW + rg) * MT + mt) * 512 + lane * 8);
+        top = fmaxf(top, o[j][0]);
+      }
+      const float f = to_frame<T>(m[mt], top, P.k2);
+      m[mt] = top;
+      l[mt] *= f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) acc[db][mt] *= f;
+#pragma unroll
+      for (int j = 1; j < KW; ++j) {
+        const float fj = to_frame<T>(o[j][0], top, P.k2);
+        l[mt] += o[j][1] * fj;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const f32x4 x = *(const LDS(f32x4)*)(
+                lds + ((((j - 1) * RW + rg) * MT + mt) * DB + db) * 4096 + r * 1024 + lane * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[db][mt][4 * r + e] += fj * x[e];
+          }
+      }
+    }
+  }
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int r = rbase + 32 * mt + n;
+    if (r >= rows) continue;
+    const int x = r / P.group, g = r - x * P.group;
+    uint16_t* const to = P.out + (static_cast<int64_t>(I.q0 + x) * P.heads + kh * P.group + g) * P.head_dim;
+    const float inv = limit[mt] >= 0 ? 1.0f / l[mt] : 0.0f;   // (a row that sees nothing is 0)
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int d = 32 * db + 8 * i + 4 * h;
+        if (d >= P.head_dim) continue;
+        float o[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = acc[db][mt][4 * i + e] * inv;
+        if (odd) {
+#pragma unroll 1
+          for (int j = nfull * kKeys; j <= limit[mt]; ++j) {
+            const u32x2 w = *reinterpret_cast<const u32x2*>(
+                P.v + first + static_cast<int64_t>(j) * P.kv_stride + d);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t u = w[e >> 1] >> (16 * (e & 1)) & 0xffffu;
+              if ((u & T::kExponent) == T::kExponent) o[e] += T::value(static_cast<uint16_t>(u));
+            }
+          }
+        }
+        *reinterpret_cast<u32x2*>(to + d) = u32x2{T::pack(o[0], o[1]), T::pack(o[2], o[3])};
+      }
+  }
+}
+
+// The items of all sequences, those with the most keys first, so that none begins late and
+// long. One workgroup: it counts the items of 1024 classes of keys, and puts them behind those
+// of the classes above. (The order within a class is that of its atomics: no result depends
+// on it.)
+constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64, kClasses = 1024;
+
+template <class F>
+__device__ __forceinline__ int block_scan(int x, F&& join, int zero, LDS(int)* part, int& all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int s = x;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int o = __shfl_up(s, off, 64);
+    if (lane >= off) s = join(s, o);
+  }
+  __syncthreads();
+  if (lane == 63) part[wave] = s;
+  __syncthreads();
+  int before = zero;
+  all = zero;
+#pragma unroll
+  for (int w = 0; w < kPlanWaves; ++w) {
+    if (w < wave) before = join(before, part[w]);
+    all = join(all, part[w]);
+  }
+  return join(before, s);                 // up to and with this thread's
+}
+
+__global__ void __launch_bounds__(kPlanThreads) plan_kernel(Pass P, int bm) {
+  __shared__ int part_[kPlanWaves], classes_[kClasses];
+  __shared__ int upto_[kPlanThreads], q0_[kPlanThreads + 1], k0_[kPlanThreads + 1], most_;
+  LDS(int)* const part = (LDS(int)*)part_;
+  const int tid = threadIdx.x;
+  const int32_t* const ks = P.k_start ? P.k_start : P.q_start;
+  auto larger = [](int a, int b) { return a > b ? a : b; };
+  auto plus = [](int a, int b) { return a + b; };
+  classes_[tid] = 0;
+  if (tid == 0) most_ = 1;
+  __syncthreads();
+  // the most keys of a sequence, which the classes divide
+  int most = 0;
+  for (int b = tid; b < P.batch; b += kPlanThreads)
+    most = max(most, clamped(ks[b + 1], 0, P.num_keys) - clamped(ks[b], 0, P.num_keys));
+  atomicMax(&most_, most);
+  // Twice over all sequences: count, then place.
+  for (int pass = 0; pass < 2; ++pass) {
+    int q_from = 0, k_from = 0;           // starts that decrease count as the largest before them
+    for (int b0 = 0; b0 < P.batch; b0 += kPlanThreads) {
+      const int b = min(b0 + tid, P.batch);   // (start b; the last one's twice or more)
+      int all;
+      int q = larger(q_from, block_scan(clamped(P.q_start[b], 0, P.num_queries), larger, 0, part, all));
+      int k = larger(k_from, block_scan(clamped(ks[b], 0, P.num_keys), larger, 0, part, all));
+      __syncthreads();
+      q0_[tid] = q;
+      k0_[tid] = k;
+      if (tid == kPlanThreads - 1) {
+        const int e = min(b0 + kPlanThreads, P.batch);
+        q0_[kPlanThreads] = larger(q, clamped(P.q_start[e], 0, P.num_queries));
+        k0_[kPlanThreads] = larger(k, clamped(ks[e], 0, P.num_keys));
+      }
+      __syncthreads();
+      q_from = q0_[kPlanThreads];
+      k_from = k0_[kPlanThreads];
+      const int rows = (q0_[tid + 1] - q) * P.group;
+      const int mine = b0 + tid < P.batch ? (rows + bm - 1) / bm : 0;
+      int total;
+      upto_[tid] = block_scan(mine, plus, 0, part, total);
+      __syncthreads();
+      for (int i = tid; i < total; i += kPlanThreads) {
+        int lo = 0, hi = kPlanThreads - 1;   // the sequence of item i: the first with upto > i
+        while (lo < hi) {
+          const int mid = (lo + hi) >> 1;
+          if (upto_[mid] > i) hi = mid;
+          else lo = mid + 1;
+        }
+        Item I{};
+        I.q0 = q0_[lo];
+        I.nq = q0_[lo + 1] - I.q0;
+        I.k0 = k0_[lo];
+        I.nk = k0_[lo + 1] - I.k0;
+        I.tile = i - (lo ? upto_[lo - 1] : 0);
+        const int last = min((I.tile + 1) * bm, I.nq * P.group) - 1;
+        const int keys = clamped(last / P.group + 1 + I.nk - I.nq, 0, most_);
+        const int cls = kClasses - 1 - static_cast<int>(static_cast<int64_t>(keys) * (kClasses - 1) / most_);
+        const int at = atomicAdd(&classes_[cls], 1);
+        if (pass) P.items[at] = I;
+      }
+      __syncthreads();
+    }
+    if (pass == 0) {
+      int total;
+      const int own = classes_[tid];
+      const int upto = block_scan(own, plus, 0, part, total);
+      __syncthreads();
+      classes_[tid] = upto - own;
+      if (tid == 0) *P.count = total;
+      __syncthreads();
+    }
+  }
+}
+
+int block_rows(int64_t rows, int64_t kv_heads, int cus) {
+  if (rows / 256 * kv_heads >= 2 * cus) return 256;
+  return rows / 128 * kv_heads >= cus ? 128 : 64;
+}
+
+int64_t most_items(int64_t rows, int64_t batch, int bm) { return rows / bm + batch; }
+
+int device_cus() {
+  constexpr int kMaxDevices = 64;
+  static int cus[kMaxDevices];
+  static std::mutex mu;
+  int dev = 0, n = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0) return 0;
+  std::lock_guard<std::mutex> lock(mu);
+  if (dev < kMaxDevices && cus[dev]) return cus[dev];
+  if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return 0;
+  if (dev < kMaxDevices) cus[dev] = n;
+  return n;
+}
+
+template <class T, int DP>
+hipError_t run(const Pass& P, int bm, unsigned wgs, hipStream_t stream) {
+  const dim3 grid(wgs), block(kThreads);
+  if (bm == 256) hipLaunchKernelGGL((prompt_kernel<T, Shape<DP, 4>>), grid, block, 0, stream, P);
+  else if (bm == 128) hipLaunchKernelGGL((prompt_kernel<T, Shape<DP, 2>>), grid, block, 0, stream, P);
+  else hipLaunchKernelGGL((prompt_kernel<T, Shape<DP, 1>>), grid, block, 0, stream, P);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+namespace tv {
+
+size_t prompt_workspace(int32_t batch, int32_t num_queries, int32_t num_keys, int32_t heads,
+                        int32_t kv_heads, int32_t head_dim) {
+  (void)num_keys;
+  (void)head_dim;
+  const int64_t rows = static_cast<int64_t>(num_queries) * (heads / kv_heads);
+  return align256(256 + static_cast<size_t>(most_items(rows, batch, kWaveRows)) * sizeof(Item));
+}
+
+int launch_prompt(const PromptArgs& a, void* workspace, hipStream_t stream) {
+  const int cus = device_cus();
+  if (!cus) return TV_ERR_HIP;
+  Pass P{};
+  P.q = static_cast<const uint16_t*>(a.q);
+  P.k = static_cast<const uint16_t*>(a.k);
+  P.v = static_cast<const uint16_t*>(a.v);
+  P.out = static_cast<uint16_t*>(a.out);
+  P.q_stride = a.q_stride;
+  P.kv_stride = a.kv_stride;
+  P.q_start = a.q_start;
+  P.k_start = a.k_start;
+  P.batch = a.batch;
+  P.num_queries = a.num_queries;
+  P.num_keys = a.num_keys;
+  P.heads = a.heads;
+  P.kv_heads = a.kv_heads;
+  P.head_dim = a.head_dim;
+  P.group = a.heads / a.kv_heads;
+  P.k2 = static_cast<float>(static_cast<double>(a.scale) * 1.4426950408889634);
+  const double slack = 8.0 / static_cast<double>(P.k2);
+  P.slack = slack < 3.0e38 ? static_cast<float>(slack) : 3.0e38f;
+  const int64_t rows = static_cast<int64_t>(a.num_queries) * P.group;
+  const int bm = block_rows(rows, a.kv_heads, cus);
+  const int64_t wgs = most_items(rows, a.batch, bm) * a.kv_heads;
+  if (a.batch > 1) {
+    P.count = static_cast<int*>(workspace);
+    P.items = reinterpret_cast<Item*>(static_cast<uint8_t*>(workspace) + 256);
+    hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, P, bm);
+    if (hipGetLastError() != hipSuccess) return TV_ERR_HIP;
+  }
+  const unsigned grid = static_cast<unsigned>(wgs);
+  hipError_t e;
+  if (a.dtype == TV_DTYPE_BF16)
+    e = a.head_dim <= 64 ? run<Bf16, 64>(P, bm, grid, stream) : run<Bf16, 128>(P, bm, grid, stream);
+  else
+    e = a.head_dim <= 64 ? run<F16, 64>(P, bm, grid, stream) : run<F16, 128>(P, bm, grid, stream);
+  return e == hipSuccess ? TV_OK : TV_ERR_HIP;
+}
+
+}  // namespace tv
