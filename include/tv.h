@@ -579,8 +579,8 @@ size_t tv_fp4_page_bytes(int32_t page_size, int32_t head_dim);
 
 /*
  * tv_cache_commit into a cache of 4 bits: the same rows to the same slots. The exponent of a block is
- * the least with amax <= 7 * 2^(e - 127), amax its largest magnitude, and at least 1 (from fp16 at most
- * 140, so that it reads back as finite numbers); elements are rounded to the nearest of the values
+ * the least with amax <= 7 * 2^(e - 127), amax its largest magnitude, and at least 1 and at most 252 (from
+ * fp16 140), so that it reads back as finite numbers; elements are rounded to the nearest of the values
  * above, ties to the even code, beyond 6 to 6. A block with an element that is not finite is NaN.
  * dtype (TV_DTYPE_BF16 or TV_DTYPE_F16) is that of k_new and v_new, whose strides are in elements and
  * multiples of 8; the caches' strides are in bytes and multiples of 16, pages page_stride apart, each

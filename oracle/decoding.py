@@ -175,7 +175,7 @@ def prompt_attention(q, k, v, scale):
 FP4_VALUES = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
 
 
-def fp4_encode(x, largest=254):
+def fp4_encode(x, largest=252):
     """Codes and exponent of a block of 32 numbers: the least e of 1 .. largest with
     max |x| <= 7 * 2^(e - 127), each number to the nearest value, of two as near the even code."""
     a = [abs(float(y)) for y in x]
@@ -211,7 +211,7 @@ def fp4_row(page, ps, dim, row):
     return np.concatenate(got)
 
 
-def fp4_put(page, ps, dim, row, x, largest=254):
+def fp4_put(page, ps, dim, row, x, largest=252):
     """Writes a row of numbers into a head's page of bytes."""
     for b in range(dim // 32):
         codes, e = fp4_encode(x[32 * b:32 * b + 32], largest)
@@ -232,7 +232,7 @@ def fp4_cache(cache, ps, dim):
     return out
 
 
-def cache_commit_fp4(k_new, cache, ps, new_len, slots, path_nodes, largest=254):
+def cache_commit_fp4(k_new, cache, ps, new_len, slots, path_nodes, largest=252):
     """The cache of bytes [layers, pages, kv_heads, bytes] after a call (keys or values)."""
     L, B, n1, KH, dim = k_new.shape
     cache = cache.copy()

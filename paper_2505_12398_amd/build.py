@@ -25,6 +25,11 @@ FLAGS = [
     "-Wall", "-Wno-unused-result",
 ]
 
+# The prompts' kernel holds 336 registers of a wavefront's 512: its products' results that the vector
+# unit reads in those that it can read, the rest in the others (by itself the compiler puts all results
+# into those, and copies 60 a step).
+SOURCE_FLAGS = {"tv_prompt.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+
 
 def build(verbose: bool = False) -> str:
     """Compile every source into paper_2505_12398_amd/libtv.so; returns its path."""
@@ -39,7 +44,8 @@ def build(verbose: bool = False) -> str:
     with tempfile.TemporaryDirectory() as out:
         objects = [os.path.join(out, s + ".o") for s in SOURCES]
         with ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
-            list(pool.map(lambda so: run([HIPCC, *compile_flags, "-I", INCLUDE, "-I", CSRC, "-c",
+            list(pool.map(lambda so: run([HIPCC, *compile_flags, *SOURCE_FLAGS.get(so[0], []),
+                                          "-I", INCLUDE, "-I", CSRC, "-c",
                                           os.path.join(CSRC, so[0]), "-o", so[1]]),
                           zip(SOURCES, objects)))
         run([HIPCC, "--offload-arch=gfx950", "-shared", *objects, "-o", tmp])

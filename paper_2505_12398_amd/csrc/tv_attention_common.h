@@ -47,6 +47,9 @@ struct Bf16 {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, f, SEL));
   }
   static __device__ __forceinline__ float value(uint16_t x) { return __uint_as_float(uint32_t{x} << 16); }
+  static __device__ __forceinline__ s16x8 ones() {
+    return s16x8{0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80};
+  }
   static constexpr uint32_t kExponent = 0x7f80;
   static constexpr float kLift = 0.0f;
 };
@@ -69,6 +72,9 @@ struct F16 {
   }
   static __device__ __forceinline__ float value(uint16_t x) {
     return static_cast<float>(__builtin_bit_cast(_Float16, x));
+  }
+  static __device__ __forceinline__ s16x8 ones() {
+    return s16x8{0x3c00, 0x3c00, 0x3c00, 0x3c00, 0x3c00, 0x3c00, 0x3c00, 0x3c00};
   }
   static constexpr uint32_t kExponent = 0x7c00;
   // Weights of up to 2^15 (the largest fp16 is below 2^16): those below 2^-21 of the largest

@@ -31,13 +31,13 @@ __device__ __forceinline__ uint32_t magnitudes(const u32x4& w, float (&x)[8]) {
 }
 
 // The exponent's byte of a block whose largest magnitude has these bits; 255 if it is not
-// finite. (fp16 is kept from exponents whose elements it could not hold: beyond 7 2^13 they
-// are rounded to 6 2^13.)
+// finite. (At most one whose elements the type holds: beyond 7 2^125, or 7 2^13 in fp16, they
+// are rounded to 6 of that power.)
 template <class T>
 __device__ __forceinline__ int exponent_of(uint32_t top) {
   if (top >= 0x7f800000u) return 255;
   const int e = static_cast<int>(top >> 23) - 2 + ((top & 0x7fffffu) > 0x600000u);
-  return min(max(e, 1), T::kExponent == 0x7c00 ? 127 + 13 : 254);
+  return min(max(e, 1), T::kExponent == 0x7c00 ? 127 + 13 : 127 + 125);
 }
 
 // Four lanes a block, eight elements a lane, so that reads are 16 bytes a lane and the four

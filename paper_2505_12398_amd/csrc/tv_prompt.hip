@@ -52,6 +52,25 @@ __device__ __forceinline__ f32x16 mfma32(s16x8 a, s16x8 b, f32x16 c) {
                                                   __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
+// The same onto an accumulator in the registers that the vector unit does not compute in, which
+// leaves the others to scores and weights. (In assembly: the compiler has one kind of register for
+// all products. It does not see that the result is late: settle() stands before the vector unit
+// reads or writes accumulators; products among themselves wait for each other.)
+template <class T>
+__device__ __forceinline__ void accumulate(s16x8 a, s16x8 b, f32x16& c) {
+  if constexpr (std::is_same<T, Bf16>::value)
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+  else
+    asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+}
+template <int DB, int MT>
+__device__ __forceinline__ void settle(f32x16 (&c)[DB][MT]) {
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) asm volatile("s_nop 7\n\ts_nop 3" : "+a"(c[db][mt]));
+}
+
 // RW row groups of 64 rows, KW key groups that take the tiles in turn and are merged at the end.
 template <int DP_, int RW_>
 struct Shape {
@@ -62,21 +81,41 @@ struct Shape {
   static constexpr int CH = DP / 8, ROW = DP * 2;    // 16-byte chunks and bytes of a row
   static constexpr int MAT = kKeys * ROW, STAGE = 2 * MAT;
   static constexpr int LOADS = MAT / 1024 / RW;      // of a wavefront, for a tile's keys (or values)
-  static constexpr int S = RW == 1 ? 2 : 4;          // tiles in LDS per key group
+  static constexpr int S = DP == 128 && RW == 1 ? 2 : 4;   // tiles in LDS per key group
+  // Operands of a step: values of the tile before, keys of the one behind, each for MT products.
+  static constexpr int NV = 2 * DB, NK = KK, OPS = NV + NK;
+  static constexpr int AHEAD = 3;                    // operands read before they are multiplied
+  static constexpr bool LOOK = S > 2;                // the next step's first ones among them
+  static constexpr int WAIT = 2 * LOADS * (S - 2 - LOOK);
+  static_assert(OPS % (AHEAD + 1) == 0, "places of operands are the same in every step");
   static constexpr int RING = KW * S * STAGE;
   static constexpr int ACC = (KW - 1) * RW * MT * DB * 4096;
   static constexpr int MERGE = ACC + (KW - 1) * RW * MT * 64 * 8;
   static constexpr int MAIN = RING > MERGE ? RING : MERGE;
   static constexpr int FLAGS = MAIN, BYTES = FLAGS + 4 * kWaves;
+  static constexpr int PER_CU = 1;        // workgroups
   static_assert(BYTES <= 160 * 1024, "LDS of a CU");
-  static_assert(S * 2 * LOADS < 64, "the count of loads in flight");
+  static_assert(WAIT < 64, "the count of loads in flight");
 };
 
-// Sequence b's rows, its starts kept within the tensors.
+// A wavefront's part of a tile's keys, or values, into LDS.
+template <int N>
+__device__ __forceinline__ void load_tile(const i32x4& rs, const int (&voff)[N], int dst) {
+  if constexpr (N <= 4) {
+    load_to_lds<N>(rs, voff, dst);
+  } else {
+    static_assert(N == 8, "eight loads at most");
+    const int lo[4] = {voff[0], voff[1], voff[2], voff[3]}, hi[4] = {voff[4], voff[5], voff[6], voff[7]};
+    load_to_lds<4>(rs, lo, dst);
+    load_to_lds<4>(rs, hi, dst + 4096);
+  }
+}
+
+// Starts are kept within the tensors.
 __device__ __forceinline__ int clamped(int x, int lo, int hi) { return min(max(x, lo), hi); }
 
 template <class T, class SH>
-__global__ void __launch_bounds__(kThreads, 1) prompt_kernel(Pass P) {
+__global__ void __launch_bounds__(kThreads, SH::PER_CU) prompt_kernel(Pass P) {
   constexpr int MT = SH::MT, RW = SH::RW, KW = SH::KW, KK = SH::KK, DB = SH::DB;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[SH::BYTES];
   lds_byte* const lds = (lds_byte*)smem;
@@ -137,6 +176,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(Pass P) {
     return SH::DP == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
   };
   const int stride = static_cast<int>(P.kv_stride) * 2;
+  const uint64_t step_bytes = static_cast<uint64_t>(KW) * kKeys * stride;
   int kv_off[SH::LOADS];
 #pragma unroll
   for (int i = 0; i < SH::LOADS; ++i) {
@@ -144,20 +184,15 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(Pass P) {
     const int c = (lane % SH::CH) ^ swizzle(r);
     kv_off[i] = 8 * c < P.head_dim ? r * stride + 16 * c : kPastRange;
   }
+  const int lds_own = lds0 + kg * SH::S * SH::STAGE + rg * SH::LOADS * 1024;
   const int64_t first = static_cast<int64_t>(I.k0) * P.kv_stride + kh * P.head_dim;
-  const uint64_t k_base = reinterpret_cast<uint64_t>(P.k + first);
-  const uint64_t to_v = reinterpret_cast<uint64_t>(P.v) - reinterpret_cast<uint64_t>(P.k);
+  const uint64_t k_base = reinterpret_cast<uint64_t>(P.k + first), v_base = reinterpret_cast<uint64_t>(P.v + first);
   auto issue = [&](int t, int stage, bool values) {
     // rows behind the sequence's last key are zeros, so are tiles that are none
-    const int left = t < tiles ? min(kKeys, I.nk - t * kKeys) : 0;
-    const uint64_t a = k_base + static_cast<uint64_t>(min(t, tiles)) * kKeys * stride + (values ? to_v : 0);
-    const i32x4 rs = {static_cast<int>(a), static_cast<int>(a >> 32) & 0xffff, left * stride, 0x00020000};
-    const int to = lds0 + stage + (values ? SH::MAT : 0) + rg * SH::LOADS * 1024;
-#pragma unroll
-    for (int i = 0; i < SH::LOADS; ++i) {
-      const int voff[1] = {kv_off[i]};
-      load_to_lds<1>(rs, voff, to + i * 1024);
-    }
+    const int left = t >= 0 && t < tiles ? min(kKeys, I.nk - t * kKeys) : 0;
+    const uint64_t a = (values ? v_base : k_base) + static_cast<uint64_t>(max(0, min(t, tiles))) * kKeys * stride;
+    const i32x4 rs = {static_cast<int>(a), static_cast<int>(a >> 32), left * stride, 0x00020000};
+    load_tile<SH::LOADS>(rs, kv_off, lds_own + stage + (values ? SH::MAT : 0));
   };
   // Reads: keys, row n and chunk 2 kk + h; values, keys 4 h .. 4 h + 3 of 16 by sixteen of the
   // head, lane i of sixteen the eight bytes i % 4 at key i / 4, transposed by the read.
@@ -168,152 +203,291 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(Pass P) {
   const int v_hi = (vrow + 8) * SH::ROW +
                    ((2 * (lane >> 4 & 1) + ((lane & 3) >> 1)) ^ swizzle(vrow + 8)) * 16 + (lane & 1) * 8;
 
-  float m[MT], l[MT], c[MT];
-  f32x16 acc[DB][MT];
+  float m[MT], c[MT], above[MT];          // above: what a score moves the frame from
+  // The last block is that of the sums: the weights times ones. (The vector unit would take 64
+  // instructions a step for them, of 250; a dot product of two weights waits for the matrix unit.)
+  f32x16 acc[DB + 1][MT];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
-    m[mt] = -INFINITY;
-    l[mt] = c[mt] = 0.0f;
+    m[mt] = above[mt] = -INFINITY;
+    c[mt] = 0.0f;
 #pragma unroll
-    for (int db = 0; db < DB; ++db) acc[db][mt] = f32x16{};
+    for (int db = 0; db <= DB; ++db) acc[db][mt] = f32x16{};
   }
   bool odd = false;                       // a value in a masked tile that is not finite
 
-  auto compute = [&](auto full, int stage, int t) {
-    f32x16 s[MT] = {};
+  const int ring = kg * SH::S * SH::STAGE;
+  int k_from[KK], v_from[DB][2];          // where operands lie in a key group's first place
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) k_from[kk] = here(ring + (k_at ^ (32 * kk)));
+#pragma unroll
+  for (int db = 0; db < DB; ++db) {
+    v_from[db][0] = here(ring + SH::MAT + (v_at ^ (64 * db)));
+    v_from[db][1] = here(ring + SH::MAT + (v_hi ^ (64 * db)));
+  }
+  // (the place is a constant in the steps that count, an offset in their reads)
+  auto key_operand = [&](int place, int kk) {
+    return *(const LDS(s16x8)*)(lds + k_from[kk] + place);
+  };
+  auto value_operand = [&](int place, int i) {
+    const int at = place + 16 * (i & 1) * SH::ROW, db = i >> 1;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS(s16x4)*)(lds + v_from[db][0] + at));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS(s16x4)*)(lds + v_from[db][1] + at));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  auto scores = [&](int stage, f32x16 (&s)[MT]) {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) s[mt] = f32x16{};
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
-      const s16x8 a = *(const LDS(s16x8)*)(lds + stage + (k_at ^ (32 * kk)));
+      const s16x8 a = key_operand(stage, kk);
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) s[mt] = mfma32<T>(a, q[mt][kk], s[mt]);
     }
-    if constexpr (!full.value) {
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        const int last = limit[mt] - t * kKeys - 4 * h;
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          s[mt][r] = 8 * (r >> 2) + (r & 3) <= last ? s[mt][r] : -INFINITY;
-      }
-    }
-    float top[MT];
-    bool moves = false;
+  };
+  // Where some score exceeds its row's frame: the new frames; what the sums so far are multiplied
+  // with (the accumulators once they hold all weights of the old frames).
+  auto move = [&](const float (&top)[MT], float (&f)[MT]) {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      top[mt] = max3(s[mt][0], s[mt][1], s[mt][2]);
-#pragma unroll
-      for (int r = 3; r < 15; r += 2) top[mt] = max3(top[mt], s[mt][r], s[mt][r + 1]);
-      top[mt] = __builtin_elementwise_maximum(top[mt], s[mt][15]);
-      moves |= top[mt] > m[mt] + P.slack;
+      float u = fmaxf(m[mt], top[mt]);
+      u = fmaxf(u, __shfl_xor(u, 32, 64));
+      u = u > above[mt] ? u : m[mt];
+      f[mt] = to_frame<T>(m[mt], u, P.k2);
+      m[mt] = u;
+      above[mt] = u + P.slack;
+      c[mt] = frame<T>(u, P.k2);
     }
-    if (__builtin_amdgcn_ballot_w64(moves)) {
+  };
+  auto rescale = [&](const float (&f)[MT]) {
+    settle(acc);
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        float u = fmaxf(m[mt], top[mt]);
-        u = fmaxf(u, __shfl_xor(u, 32, 64));
-        u = u > m[mt] + P.slack ? u : m[mt];
-        const float f = to_frame<T>(m[mt], u, P.k2);
-        m[mt] = u;
-        c[mt] = frame<T>(u, P.k2);
-        l[mt] *= f;
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int db = 0; db < DB; ++db) acc[db][mt] *= f;
-      }
+      for (int db = 0; db <= DB; ++db) acc[db][mt] *= f[mt];
+    settle(acc);
+  };
+  auto weight = [&](const f32x16 (&s)[MT], int mt, int r) {
+    return __builtin_amdgcn_exp2f(fmaf(s[mt][r], P.k2, c[mt]));
+  };
+  auto largest = [&](const f32x16& s, int i, float top) {   // of two more
+    return i == 0 ? __builtin_elementwise_maximum(s[0], s[1]) : max3(top, s[2 * i], s[2 * i + 1]);
+  };
+
+  // A tile's values times its weights, where some rows do not see it whole: keys that a row does not
+  // see may hold anything, and weight 0 times NaN or infinity must not reach the row. Such values are
+  // taken as 0 here and added to the rows that see them when these are written. (A half word's
+  // exponent of ones, plus one, carries into its sign.)
+  const s16x8 ones8 = T::ones();
+  auto add_values = [&](int stage, const u32x4 (&p)[MT][2], bool whole) {
+    s16x8 v[SH::NV];
+    uint32_t ones = 0;
+    constexpr uint32_t kExp = T::kExponent * 0x10001u, kOne = (0x8000u - T::kExponent) * 0x10001u;
+#pragma unroll
+    for (int i = 0; i < SH::NV; ++i) {
+      v[i] = value_operand(stage, i);
+      const u32x4 w = __builtin_bit_cast(u32x4, v[i]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) ones |= (w[j] & kExp) + kOne;
     }
-    s16x8 p[MT][2];
+    if (!whole && __builtin_amdgcn_ballot_w64((ones & 0x80008000u) != 0)) {
+      odd = true;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
+      for (int i = 0; i < SH::NV; ++i) {
+        u32x4 w = __builtin_bit_cast(u32x4, v[i]);
 #pragma unroll
-      for (int sl = 0; sl < 2; ++sl) {
-        u32x4 w;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float e0 = __builtin_amdgcn_exp2f(fmaf(s[mt][8 * sl + 2 * i], P.k2, c[mt]));
-          const float e1 = __builtin_amdgcn_exp2f(fmaf(s[mt][8 * sl + 2 * i + 1], P.k2, c[mt]));
-          w[i] = T::pack(e0, e1);
-          l[mt] = T::plus(l[mt], w[i]);
-        }
-        p[mt][sl] = __builtin_bit_cast(s16x8, w);
-      }
-    }
-    s16x8 v[DB][2];
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int sl = 0; sl < 2; ++sl) {
-        const int at = stage + SH::MAT + 16 * sl * SH::ROW;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS(s16x4)*)(lds + at + (v_at ^ (64 * db))));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS(s16x4)*)(lds + at + (v_hi ^ (64 * db))));
-        v[db][sl] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      }
-    if constexpr (!full.value) {
-      // Keys that a row does not see may hold anything: weight 0 times NaN or infinity must not
-      // reach the row. Such values are taken as 0 here and added to the rows that see them when
-      // these are written. (A half word's exponent of ones, plus one, carries into its sign.)
-      constexpr uint32_t kExp = T::kExponent * 0x10001u, kOne = (0x8000u - T::kExponent) * 0x10001u;
-      uint32_t ones = 0;
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int sl = 0; sl < 2; ++sl) {
-          const u32x4 w = __builtin_bit_cast(u32x4, v[db][sl]);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) ones |= (w[j] & kExp) + kOne;
-        }
-      if (__builtin_amdgcn_ballot_w64((ones & 0x80008000u) != 0)) {
-        odd = true;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int sl = 0; sl < 2; ++sl) {
-            u32x4 w = __builtin_bit_cast(u32x4, v[db][sl]);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              w[j] = ((w[j] & T::kExponent) == T::kExponent ? 0 : w[j] & 0xffffu) |
-                     ((w[j] >> 16 & T::kExponent) == T::kExponent ? 0 : w[j] & 0xffff0000u);
-            v[db][sl] = __builtin_bit_cast(s16x8, w);
-          }
+        for (int j = 0; j < 4; ++j)
+          w[j] = ((w[j] & T::kExponent) == T::kExponent ? 0 : w[j] & 0xffffu) |
+                 ((w[j] >> 16 & T::kExponent) == T::kExponent ? 0 : w[j] & 0xffff0000u);
+        v[i] = __builtin_bit_cast(s16x8, w);
       }
     }
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+    for (int i = 0; i < SH::NV; ++i)
 #pragma unroll
-      for (int sl = 0; sl < 2; ++sl)
+      for (int mt = 0; mt < MT; ++mt)
+        accumulate<T>(v[i], __builtin_bit_cast(s16x8, p[mt][i & 1]), acc[i >> 1][mt]);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) acc[db][mt] = mfma32<T>(v[db][sl], p[mt][sl], acc[db][mt]);
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+        accumulate<T>(ones8, __builtin_bit_cast(s16x8, p[mt][i]), acc[DB][mt]);
   };
 
   // (left to the compiler, the queries' wait would be one for all loads in flight)
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(q[mt][kk]));
-  const int ring = kg * SH::S * SH::STAGE;
+    for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+a"(q[mt][kk]));
+
+  // Step j of a key group, whose tiles are kg, kg + KW, ..: the weights of its tile j, the values of
+  // tile j - 1 times theirs, and the scores of tile j + 1, so that the matrix units have products that
+  // wait for nothing while the vector units form weights. Once all have passed step j's barrier, the
+  // places of K_j and V_{j-2} are free: K_{j+S} and V_{j+S-2} go there. All but the WAIT newest loads
+  // have landed by then, so K_{j+1} and V_{j-1} are there (and V_j, whose first operands the end of
+  // the step reads).
   const int rounds = (tiles + KW - 1) / KW;
+  const int mine = (nsome - kg + KW - 1) / KW, whole = (nfull - kg + KW - 1) / KW;   // (0 or less: none)
+  auto place = [](int j) { return (j & (SH::S - 1)) * SH::STAGE; };
+  static_assert((SH::S & (SH::S - 1)) == 0, "places of tiles");
+  auto issue_keys = [&](int j) { issue(kg + (j + SH::S) * KW, place(j), false); };
+  auto issue_values = [&](int j) {
+    const int x = j + SH::S - 2;
+    issue(x < 0 ? -1 : kg + x * KW, place(x), true);
+  };
 #pragma unroll
-  for (int j = 0; j < SH::S; ++j) {
-    issue(kg + j * KW, ring + j * SH::STAGE, false);
-    issue(kg + j * KW, ring + j * SH::STAGE, true);
+  for (int j = -SH::S; j < 0; ++j) {
+    issue_keys(j);
+    if (j >= 1 - SH::S) issue_values(j);  // (V_-1 is zeros)
   }
-  int stage = ring;
+  f32x16 s0[MT], s1[MT];
+  u32x4 p0[MT][2] = {}, p1[MT][2];        // weights, two of a row in a word
+  wait_loads<SH::WAIT>();
+  if constexpr (RW > 1) barrier();
+  scores(place(0), s0);
+  s16x8 op[SH::AHEAD + 1];                // operand i at i % (AHEAD + 1)
+  if constexpr (SH::LOOK) unrolled<SH::AHEAD>([&](auto i) { op[i.value] = value_operand(place(-1), i.value); });
+
+  // A step all of whose rows see tiles j - 1 and j whole (or tile j - 1 is none), J = j modulo 4: one
+  // product a slot, the vector instructions spread over the slots. kFull: the tiles it loads are full
+  // and lie one step behind those loaded before.
+  uint64_t k_next = 0, v_next = 0;
+  auto step = [&](auto Jc, auto full, int j, f32x16 (&s)[MT], f32x16 (&next)[MT], const u32x4 (&p)[MT][2],
+                  u32x4 (&pn)[MT][2]) {
+    constexpr int J = Jc.value;
+    constexpr int kFirst = SH::OPS / 8;   // operands whose products go with the search for maxima
+    wait_loads<SH::WAIT>();
+    if constexpr (RW > 1) barrier();
+    auto read = [&](auto ic) {
+      constexpr int i = ic.value;
+      if constexpr (i < SH::NV) op[i % (SH::AHEAD + 1)] = value_operand(place(J - 1), i);
+      else if constexpr (i < SH::OPS) op[i % (SH::AHEAD + 1)] = key_operand(place(J + 1), i - SH::NV);
+      else if constexpr (SH::LOOK) op[i % (SH::AHEAD + 1)] = value_operand(place(J), i - SH::OPS);
+    };
+    if constexpr (!SH::LOOK) unrolled<SH::AHEAD>(read);
+    auto product = [&](auto ic, auto mtc) {
+      constexpr int i = ic.value, mt = mtc.value;
+      const s16x8 a = op[i % (SH::AHEAD + 1)];
+      if constexpr (i < SH::NV)
+        accumulate<T>(a, __builtin_bit_cast(s16x8, p[mt][i & 1]), acc[i >> 1][mt]);
+      else
+        next[mt] = mfma32<T>(a, q[mt][i - SH::NV], i == SH::NV ? f32x16{} : next[mt]);
+      if constexpr (i >= SH::NV - 2 && i < SH::NV)
+        accumulate<T>(ones8, __builtin_bit_cast(s16x8, p[mt][i & 1]), acc[DB][mt]);
+    };
+    auto load = [&](bool values) {
+      if constexpr (full.value) {
+        const uint64_t a = values ? v_next : k_next;
+        load_tile<SH::LOADS>(i32x4{static_cast<int>(a), static_cast<int>(a >> 32), kKeys * stride, 0x00020000},
+                               kv_off, lds_own + place(values ? J + SH::S - 2 : J) + (values ? SH::MAT : 0));
+        (values ? v_next : k_next) += step_bytes;
+      } else if (values) {
+        issue_values(j);
+      } else {
+        issue_keys(j);
+      }
+    };
+    float top[MT];
+    unrolled<kFirst * MT>([&](auto uc) {
+      constexpr int u = uc.value, i = u / MT, mt = u % MT;
+      if constexpr (mt == 0) read(std::integral_constant<int, i + SH::AHEAD>{});
+      product(std::integral_constant<int, i>{}, std::integral_constant<int, mt>{});
+      constexpr int kN = 8 * MT / (kFirst * MT);   // pairs of scores a slot
+#pragma unroll
+      for (int x = u * kN; x < (u + 1) * kN; ++x) top[x / 8] = largest(s[x / 8], x % 8, top[x / 8]);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    bool moves = false;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) moves |= top[mt] > above[mt];
+    const bool moved = __builtin_amdgcn_ballot_w64(moves) != 0;
+    float f[MT];
+    if (moved) move(top, f);
+    // two weights in a word, a pair after they are formed (their result is late)
+    float e[3];
+    auto pack_pair = [&](int x) {
+      uint32_t w = T::pack(e[x % 3], e[(x + 1) % 3]);
+      asm volatile("" : "+v"(w));         // (here, and not where it is used)
+      pn[x / 16][x % 16 / 8][x % 8 / 2] = w;
+    };
+    unrolled<(SH::OPS - kFirst) * MT>([&](auto uc) {
+      constexpr int u = uc.value, i = kFirst + u / MT, mt = u % MT, kAll = (SH::OPS - kFirst) * MT;
+      if constexpr (mt == 0) read(std::integral_constant<int, i + SH::AHEAD>{});
+      product(std::integral_constant<int, i>{}, std::integral_constant<int, mt>{});
+      if constexpr (u == 0) load(false);
+      if constexpr (u == kAll / 4) load(true);
+      constexpr int kWeights = 16 * MT;
+#pragma unroll
+      for (int x = u * kWeights / kAll; x < (u + 1) * kWeights / kAll; ++x) {
+        e[x % 3] = weight(s, x / 16, x % 16);
+        if (x % 2 == 0 && x > 0) pack_pair(x - 2);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    pack_pair(16 * MT - 2);
+    if (moved) rescale(f);
+  };
+  auto four = [&](auto full, int j) {
+    step(std::integral_constant<int, 0>{}, full, j, s0, s1, p0, p1);
+    step(std::integral_constant<int, 1>{}, full, j + 1, s1, s0, p1, p0);
+    step(std::integral_constant<int, 2>{}, full, j + 2, s0, s1, p0, p1);
+    step(std::integral_constant<int, 3>{}, full, j + 3, s1, s0, p1, p0);
+  };
+  int j = 0;
+  k_next = k_base + static_cast<uint64_t>(kg + SH::S * KW) * kKeys * stride;
+  v_next = v_base + static_cast<uint64_t>(kg + (SH::S - 2) * KW) * kKeys * stride;
+  // tiles of this key group that are full
+  const int loads_whole = (min(tiles, I.nk / kKeys) - kg + KW - 1) / KW;
 #pragma unroll 1
-  for (int i = 0; i < rounds; ++i) {
-    const int t = i * KW + kg;
-    wait_loads<(SH::S - 1) * 2 * SH::LOADS>();
+  for (; j + 3 < whole && j + 3 + SH::S < loads_whole; j += 4) four(std::true_type{}, j);
+#pragma unroll 1
+  for (; j + 3 < whole; j += 4) four(std::false_type{}, j);
+  // The others: tiles that some rows see in part, and steps of other wavefronts' tiles.
+#pragma unroll 1
+  for (; j < rounds; ++j) {
+    wait_loads<SH::WAIT>();
     if constexpr (RW > 1) barrier();
-    if (t < nfull) compute(std::true_type{}, stage, t);
-    else if (t < nsome) compute(std::false_type{}, stage, t);
-    if constexpr (RW > 1) barrier();
-    else wait_reads();
-    issue(t + SH::S * KW, stage, false);
-    issue(t + SH::S * KW, stage, true);
-    stage = stage == ring + (SH::S - 1) * SH::STAGE ? ring : stage + SH::STAGE;
+    issue_keys(j);
+    issue_values(j);
+    if (j > mine) continue;
+    if (j > 0) add_values(place(j - 1), p0, j - 1 < whole);
+    if (j == mine) continue;
+    const int t = kg + j * KW;
+    float top[MT];
+    bool moves = false;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      const int last = limit[mt] - t * kKeys - 4 * h;
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        s0[mt][r] = 8 * (r >> 2) + (r & 3) <= last ? s0[mt][r] : -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top[mt] = largest(s0[mt], i, top[mt]);
+      moves |= top[mt] > above[mt];
+    }
+    if (__builtin_amdgcn_ballot_w64(moves)) {
+      float f[MT];
+      move(top, f);
+      rescale(f);
+    }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) {
+        p0[mt][r / 8][r % 8 / 2] = T::pack(weight(s0, mt, r), weight(s0, mt, r + 1));
+      }
+    if (j + 1 < mine) scores(place(j + 1), s0);
   }
   wait_loads<0>();                        // (zeros for tiles that are none)
+  if constexpr (RW > 1) barrier();
+  if (mine == rounds && mine > 0) add_values(place(mine - 1), p0, mine - 1 < whole);
+
+  settle(acc);
 
   // the key groups' parts, merged by group 0
+  float l[MT];
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt) l[mt] += __shfl_xor(l[mt], 32, 64);
+  for (int mt = 0; mt < MT; ++mt) l[mt] = acc[DB][mt][0];
   LDS(int)* const flags = (LDS(int)*)(lds + SH::FLAGS);
   if constexpr (KW > 1) {
     barrier();                            // all have read their last tile

@@ -346,9 +346,9 @@ def test_offsets_beyond_32_bits():
     near = torch.randn((n, wide, 64), generator=g, device=DEV).to(torch.bfloat16)
     kv[rows - n:] = near
     at = torch.tensor([rows - n, rows], dtype=torch.int32, device=DEV)
-    far = tv.prompt_attention(kv[:, :8], kv[:, 8:10], kv[:, 1022:], at, 0.125)
-    want = tv.prompt_attention(near[:, :8], near[:, 8:10], near[:, 1022:], at - (rows - n), 0.125)
-    assert torch.equal(far[rows - n:], want)
-    far = tv.prompt_attention(kv, kv[:, :256], kv[:, 256:512], at, 0.125)
-    want = tv.prompt_attention(near, near[:, :256], near[:, 256:512], at - (rows - n), 0.125)
-    assert torch.equal(far[rows - n:], want) and bool(want.isfinite().all())
+    # (another count of queries may sum in another order: to the bounds, not to the bit)
+    for q, k, v in ((slice(0, 8), slice(8, 10), slice(1022, 1024)),
+                    (slice(0, 1024), slice(0, 256), slice(256, 512))):
+        far = tv.prompt_attention(kv[:, q], kv[:, k], kv[:, v], at, 0.125)
+        check(dict(q=near[:, q], k=near[:, k], v=near[:, v], q_start=at - (rows - n), scale=0.125),
+              out=far[rows - n:])
