@@ -63,6 +63,15 @@ __device__ __forceinline__ void accumulate(s16x8 a, s16x8 b, f32x16& c) {
   else
     asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
 }
+// The sums: ones from a register that is theirs for good. (A constant is put into one right before
+// the product, which reads it two instructions later at the earliest.)
+template <class T>
+__device__ __forceinline__ void accumulate_ones(s16x8 ones, s16x8 b, f32x16& c) {
+  if constexpr (std::is_same<T, Bf16>::value)
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(c) : "a"(ones), "v"(b));
+  else
+    asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+a"(c) : "a"(ones), "v"(b));
+}
 template <int DB, int MT>
 __device__ __forceinline__ void settle(f32x16 (&c)[DB][MT]) {
 #pragma unroll
@@ -82,11 +91,11 @@ struct Shape {
   static constexpr int MAT = kKeys * ROW, STAGE = 2 * MAT;
   static constexpr int LOADS = MAT / 1024 / RW;      // of a wavefront, for a tile's keys (or values)
   static constexpr int S = DP == 128 && RW == 1 ? 2 : 4;   // tiles in LDS per key group
-  // Operands of a step: values of the tile before, keys of the one behind, each for MT products.
-  static constexpr int NV = 2 * DB, NK = KK, OPS = NV + NK;
+  // Operands of a step: keys of the tile behind, values of the one before, each for MT products.
+  static constexpr int NK = KK, NV = 2 * DB, OPS = NK + NV;
   static constexpr int AHEAD = 3;                    // operands read before they are multiplied
   static constexpr bool LOOK = S > 2;                // the next step's first ones among them
-  static constexpr int WAIT = 2 * LOADS * (S - 2 - LOOK);
+  static constexpr int WAIT = LOADS * (LOOK ? 2 * (S - 3) + 1 : 2 * (S - 2));
   static_assert(OPS % (AHEAD + 1) == 0, "places of operands are the same in every step");
   static constexpr int RING = KW * S * STAGE;
   static constexpr int ACC = (KW - 1) * RW * MT * DB * 4096;
@@ -278,7 +287,8 @@ __global__ void __launch_bounds__(kThreads, SH::PER_CU) prompt_kernel(Pass P) {
   // see may hold anything, and weight 0 times NaN or infinity must not reach the row. Such values are
   // taken as 0 here and added to the rows that see them when these are written. (A half word's
   // exponent of ones, plus one, carries into its sign.)
-  const s16x8 ones8 = T::ones();
+  s16x8 ones8 = T::ones();
+  asm volatile("" : "+a"(ones8));
   auto add_values = [&](int stage, const u32x4 (&p)[MT][2], bool whole) {
     s16x8 v[SH::NV];
     uint32_t ones = 0;
@@ -311,7 +321,7 @@ __global__ void __launch_bounds__(kThreads, SH::PER_CU) prompt_kernel(Pass P) {
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
-        accumulate<T>(ones8, __builtin_bit_cast(s16x8, p[mt][i]), acc[DB][mt]);
+        accumulate_ones<T>(ones8, __builtin_bit_cast(s16x8, p[mt][i]), acc[DB][mt]);
   };
 
   // (left to the compiler, the queries' wait would be one for all loads in flight)
@@ -320,12 +330,12 @@ __global__ void __launch_bounds__(kThreads, SH::PER_CU) prompt_kernel(Pass P) {
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+a"(q[mt][kk]));
 
-  // Step j of a key group, whose tiles are kg, kg + KW, ..: the weights of its tile j, the values of
-  // tile j - 1 times theirs, and the scores of tile j + 1, so that the matrix units have products that
+  // Step j of a key group, whose tiles are kg, kg + KW, ..: the weights of its tile j, the scores of
+  // tile j + 1, and the values of tile j - 1 times theirs, so that the matrix units have products that
   // wait for nothing while the vector units form weights. Once all have passed step j's barrier, the
   // places of K_j and V_{j-2} are free: K_{j+S} and V_{j+S-2} go there. All but the WAIT newest loads
-  // have landed by then, so K_{j+1} and V_{j-1} are there (and V_j, whose first operands the end of
-  // the step reads).
+  // have landed by then, so K_{j+1} and V_{j-1} are there (and K_{j+2}, whose first operands the end
+  // of the step reads).
   const int rounds = (tiles + KW - 1) / KW;
   const int mine = (nsome - kg + KW - 1) / KW, whole = (nfull - kg + KW - 1) / KW;   // (0 or less: none)
   auto place = [](int j) { return (j & (SH::S - 1)) * SH::STAGE; };
@@ -346,34 +356,54 @@ __global__ void __launch_bounds__(kThreads, SH::PER_CU) prompt_kernel(Pass P) {
   if constexpr (RW > 1) barrier();
   scores(place(0), s0);
   s16x8 op[SH::AHEAD + 1];                // operand i at i % (AHEAD + 1)
-  if constexpr (SH::LOOK) unrolled<SH::AHEAD>([&](auto i) { op[i.value] = value_operand(place(-1), i.value); });
+  if constexpr (SH::LOOK) unrolled<SH::AHEAD>([&](auto i) { op[i.value] = key_operand(place(1), i.value); });
+  // Whether the frames moved for a tile's scores, and what the accumulators are multiplied with for
+  // it once the weights before it are in them.
+  bool moved = false;
+  float f[MT];
+  auto look = [&](const float (&top)[MT]) {
+    bool moves = false;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) moves |= top[mt] > above[mt];
+    moved = __builtin_amdgcn_ballot_w64(moves) != 0;
+    if (moved) move(top, f);
+  };
+  auto look_all = [&](const f32x16 (&s)[MT]) {
+    float top[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top[mt] = largest(s[mt], i, top[mt]);
+    look(top);
+  };
+  int j = 0;
+  if (whole > 4) look_all(s0);            // (else the steps below do)
 
-  // A step all of whose rows see tiles j - 1 and j whole (or tile j - 1 is none), J = j modulo 4: one
-  // product a slot, the vector instructions spread over the slots. kFull: the tiles it loads are full
-  // and lie one step behind those loaded before.
+  // A step all of whose rows see tiles j - 1 (or it is none), j and j + 1 whole, J = j modulo 4; the
+  // frames are those of tile j. One product a slot, the vector instructions spread over the slots.
+  // kFull: the tiles it loads are full and lie one step behind those loaded before.
   uint64_t k_next = 0, v_next = 0;
   auto step = [&](auto Jc, auto full, int j, f32x16 (&s)[MT], f32x16 (&next)[MT], const u32x4 (&p)[MT][2],
                   u32x4 (&pn)[MT][2]) {
     constexpr int J = Jc.value;
-    constexpr int kFirst = SH::OPS / 8;   // operands whose products go with the search for maxima
     wait_loads<SH::WAIT>();
     if constexpr (RW > 1) barrier();
     auto read = [&](auto ic) {
       constexpr int i = ic.value;
-      if constexpr (i < SH::NV) op[i % (SH::AHEAD + 1)] = value_operand(place(J - 1), i);
-      else if constexpr (i < SH::OPS) op[i % (SH::AHEAD + 1)] = key_operand(place(J + 1), i - SH::NV);
-      else if constexpr (SH::LOOK) op[i % (SH::AHEAD + 1)] = value_operand(place(J), i - SH::OPS);
+      if constexpr (i < SH::NK) op[i % (SH::AHEAD + 1)] = key_operand(place(J + 1), i);
+      else if constexpr (i < SH::OPS) op[i % (SH::AHEAD + 1)] = value_operand(place(J - 1), i - SH::NK);
+      else if constexpr (SH::LOOK) op[i % (SH::AHEAD + 1)] = key_operand(place(J + 2), i - SH::OPS);
     };
     if constexpr (!SH::LOOK) unrolled<SH::AHEAD>(read);
     auto product = [&](auto ic, auto mtc) {
-      constexpr int i = ic.value, mt = mtc.value;
+      constexpr int i = ic.value, mt = mtc.value, v = i - SH::NK;
       const s16x8 a = op[i % (SH::AHEAD + 1)];
-      if constexpr (i < SH::NV)
-        accumulate<T>(a, __builtin_bit_cast(s16x8, p[mt][i & 1]), acc[i >> 1][mt]);
+      if constexpr (i < SH::NK)
+        next[mt] = mfma32<T>(a, q[mt][i], i == 0 ? f32x16{} : next[mt]);
       else
-        next[mt] = mfma32<T>(a, q[mt][i - SH::NV], i == SH::NV ? f32x16{} : next[mt]);
-      if constexpr (i >= SH::NV - 2 && i < SH::NV)
-        accumulate<T>(ones8, __builtin_bit_cast(s16x8, p[mt][i & 1]), acc[DB][mt]);
+        accumulate<T>(a, __builtin_bit_cast(s16x8, p[mt][v & 1]), acc[v >> 1][mt]);
+      if constexpr (i >= SH::OPS - 2)
+        accumulate_ones<T>(ones8, __builtin_bit_cast(s16x8, p[mt][v & 1]), acc[DB][mt]);
     };
     auto load = [&](bool values) {
       if constexpr (full.value) {
@@ -387,34 +417,18 @@ __global__ void __launch_bounds__(kThreads, SH::PER_CU) prompt_kernel(Pass P) {
         issue_keys(j);
       }
     };
-    float top[MT];
-    unrolled<kFirst * MT>([&](auto uc) {
-      constexpr int u = uc.value, i = u / MT, mt = u % MT;
-      if constexpr (mt == 0) read(std::integral_constant<int, i + SH::AHEAD>{});
-      product(std::integral_constant<int, i>{}, std::integral_constant<int, mt>{});
-      constexpr int kN = 8 * MT / (kFirst * MT);   // pairs of scores a slot
-#pragma unroll
-      for (int x = u * kN; x < (u + 1) * kN; ++x) top[x / 8] = largest(s[x / 8], x % 8, top[x / 8]);
-      __builtin_amdgcn_sched_barrier(0);
-    });
-    bool moves = false;
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) moves |= top[mt] > above[mt];
-    const bool moved = __builtin_amdgcn_ballot_w64(moves) != 0;
-    float f[MT];
-    if (moved) move(top, f);
     // two weights in a word, a pair after they are formed (their result is late)
-    float e[3];
+    float e[3], top[MT];
     auto pack_pair = [&](int x) {
       uint32_t w = T::pack(e[x % 3], e[(x + 1) % 3]);
       asm volatile("" : "+v"(w));         // (here, and not where it is used)
       pn[x / 16][x % 16 / 8][x % 8 / 2] = w;
     };
-    unrolled<(SH::OPS - kFirst) * MT>([&](auto uc) {
-      constexpr int u = uc.value, i = kFirst + u / MT, mt = u % MT, kAll = (SH::OPS - kFirst) * MT;
+    unrolled<SH::OPS * MT>([&](auto uc) {
+      constexpr int u = uc.value, i = u / MT, mt = u % MT, kAll = SH::OPS * MT;
       if constexpr (mt == 0) read(std::integral_constant<int, i + SH::AHEAD>{});
       product(std::integral_constant<int, i>{}, std::integral_constant<int, mt>{});
-      if constexpr (u == 0) load(false);
+      if constexpr (u == 1) load(false);
       if constexpr (u == kAll / 4) load(true);
       constexpr int kWeights = 16 * MT;
 #pragma unroll
@@ -422,10 +436,20 @@ __global__ void __launch_bounds__(kThreads, SH::PER_CU) prompt_kernel(Pass P) {
         e[x % 3] = weight(s, x / 16, x % 16);
         if (x % 2 == 0 && x > 0) pack_pair(x - 2);
       }
+      // the next tile's scores are there a few products after their last one
+      constexpr int kFrom = SH::NK * MT + 4, kPairs = 8 * MT;
+      if constexpr (u >= kFrom) {
+#pragma unroll
+        for (int x = (u - kFrom) * kPairs / (kAll - kFrom); x < (u + 1 - kFrom) * kPairs / (kAll - kFrom); ++x) {
+          top[x / 8] = largest(next[x / 8], x % 8, top[x / 8]);
+          asm volatile("" : "+v"(top[x / 8]));
+        }
+      }
       __builtin_amdgcn_sched_barrier(0);
     });
     pack_pair(16 * MT - 2);
     if (moved) rescale(f);
+    look(top);
   };
   auto four = [&](auto full, int j) {
     step(std::integral_constant<int, 0>{}, full, j, s0, s1, p0, p1);
@@ -433,15 +457,14 @@ __global__ void __launch_bounds__(kThreads, SH::PER_CU) prompt_kernel(Pass P) {
     step(std::integral_constant<int, 2>{}, full, j + 2, s0, s1, p0, p1);
     step(std::integral_constant<int, 3>{}, full, j + 3, s1, s0, p1, p0);
   };
-  int j = 0;
   k_next = k_base + static_cast<uint64_t>(kg + SH::S * KW) * kKeys * stride;
   v_next = v_base + static_cast<uint64_t>(kg + (SH::S - 2) * KW) * kKeys * stride;
   // tiles of this key group that are full
   const int loads_whole = (min(tiles, I.nk / kKeys) - kg + KW - 1) / KW;
 #pragma unroll 1
-  for (; j + 3 < whole && j + 3 + SH::S < loads_whole; j += 4) four(std::true_type{}, j);
+  for (; j + 4 < whole && j + 3 + SH::S < loads_whole; j += 4) four(std::true_type{}, j);
 #pragma unroll 1
-  for (; j + 3 < whole; j += 4) four(std::false_type{}, j);
+  for (; j + 4 < whole; j += 4) four(std::false_type{}, j);
   // The others: tiles that some rows see in part, and steps of other wavefronts' tiles.
 #pragma unroll 1
   for (; j < rounds; ++j) {
@@ -451,31 +474,25 @@ __global__ void __launch_bounds__(kThreads, SH::PER_CU) prompt_kernel(Pass P) {
     issue_values(j);
     if (j > mine) continue;
     if (j > 0) add_values(place(j - 1), p0, j - 1 < whole);
+    if (moved) rescale(f);
+    moved = false;
     if (j == mine) continue;
     const int t = kg + j * KW;
-    float top[MT];
-    bool moves = false;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       const int last = limit[mt] - t * kKeys - 4 * h;
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         s0[mt][r] = 8 * (r >> 2) + (r & 3) <= last ? s0[mt][r] : -INFINITY;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top[mt] = largest(s0[mt], i, top[mt]);
-      moves |= top[mt] > above[mt];
     }
-    if (__builtin_amdgcn_ballot_w64(moves)) {
-      float f[MT];
-      move(top, f);
-      rescale(f);
-    }
+    look_all(s0);
+    if (moved) rescale(f);
+    moved = false;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int r = 0; r < 16; r += 2) {
+      for (int r = 0; r < 16; r += 2)
         p0[mt][r / 8][r % 8 / 2] = T::pack(weight(s0, mt, r), weight(s0, mt, r + 1));
-      }
     if (j + 1 < mine) scores(place(j + 1), s0);
   }
   wait_loads<0>();                        // (zeros for tiles that are none)
