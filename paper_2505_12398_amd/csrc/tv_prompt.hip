@@ -90,12 +90,12 @@ struct Shape {
   static constexpr int CH = DP / 8, ROW = DP * 2;    // 16-byte chunks and bytes of a row
   static constexpr int MAT = kKeys * ROW, STAGE = 2 * MAT;
   static constexpr int LOADS = MAT / 1024 / RW;      // of a wavefront, for a tile's keys (or values)
-  static constexpr int S = DP == 128 && RW == 1 ? 2 : 4;   // tiles in LDS per key group
+  static constexpr int S = 4;                        // tiles in LDS per key group
   // Operands of a step: keys of the tile behind, values of the one before, each for MT products.
   static constexpr int NK = KK, NV = 2 * DB, OPS = NK + NV;
   static constexpr int AHEAD = 3;                    // operands read before they are multiplied
-  static constexpr bool LOOK = S > 2;                // the next step's first ones among them
-  static constexpr int WAIT = LOADS * (LOOK ? 2 * (S - 3) + 1 : 2 * (S - 2));
+  // (the next step's first ones among them)
+  static constexpr int WAIT = LOADS * (2 * (S - 3) + 1);
   static_assert(OPS % (AHEAD + 1) == 0, "places of operands are the same in every step");
   static constexpr int RING = KW * S * STAGE;
   static constexpr int ACC = (KW - 1) * RW * MT * DB * 4096;
@@ -107,21 +107,248 @@ struct Shape {
   static_assert(WAIT < 64, "the count of loads in flight");
 };
 
-// A wavefront's part of a tile's keys, or values, into LDS.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+// A wavefront's part of a tile's keys, or values, into LDS: 1024 bytes at dst, and so on. (Without the
+// wait states of load_to_lds: the scalars come from the scalar unit, which the generated code is
+// tested for.)
 template <int N>
 __device__ __forceinline__ void load_tile(const i32x4& rs, const int (&voff)[N], int dst) {
-  if constexpr (N <= 4) {
-    load_to_lds<N>(rs, voff, dst);
-  } else {
-    static_assert(N == 8, "eight loads at most");
-    const int lo[4] = {voff[0], voff[1], voff[2], voff[3]}, hi[4] = {voff[4], voff[5], voff[6], voff[7]};
-    load_to_lds<4>(rs, lo, dst);
-    load_to_lds<4>(rs, hi, dst + 4096);
-  }
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :: "s"(dst), "v"(voff[i]), "s"(rs), "n"(i * 1024) : "memory", "m0", "scc");
 }
+#pragma clang diagnostic pop
 
 // Starts are kept within the tensors.
 __device__ __forceinline__ int clamped(int x, int lo, int hi) { return min(max(x, lo), hi); }
+
+// Swizzle of a tile's rows in LDS: a chunk of sixteen rows, and four chunks of four rows, touch all
+// banks once.
+template <int DP>
+__device__ __forceinline__ int swizzle(int r) {
+  return DP == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
+}
+
+// The end of an item: the key groups' parts merged by group 0, and its rows written; odd: with what is
+// not finite of the values v (those of the item's first key and key head) from key `from` on.
+template <class T, class SH>
+__device__ __forceinline__ void finish(lds_byte* lds, f32x16 (&acc)[SH::DB + 1][SH::MT], float (&m)[SH::MT],
+                                       const int (&limit)[SH::MT], bool odd, const uint16_t* v, int64_t kv_stride,
+                                       uint16_t* out, int heads, int head_dim, int group, float k2, int kh, int q0,
+                                       int rows, int rbase, int from) {
+  constexpr int MT = SH::MT, RW = SH::RW, KW = SH::KW, DB = SH::DB;
+  const int lane = threadIdx.x & 63, wave = uniform(static_cast<int>(threadIdx.x >> 6));
+  const int rg = wave % RW, kg = wave / RW, n = lane & 31, h = lane >> 5;
+  LDS(int)* const flags = (LDS(int)*)(lds + SH::FLAGS);
+  float l[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) l[mt] = acc[DB][mt][0];
+  if constexpr (KW > 1) {
+    barrier();                            // (all have read the flags)
+    if (lane == 0) flags[wave] = odd;
+    if (kg > 0) {
+      const int w = (kg - 1) * RW + rg;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            *(LDS(f32x4)*)(lds + ((w * MT + mt) * DB + db) * 4096 + r * 1024 + lane * 16) =
+                f32x4{acc[db][mt][4 * r], acc[db][mt][4 * r + 1], acc[db][mt][4 * r + 2], acc[db][mt][4 * r + 3]};
+        *(LDS(f32x2)*)(lds + SH::ACC + (w * MT + mt) * 512 + lane * 8) = f32x2{m[mt], l[mt]};
+      }
+    }
+    barrier();
+    if (kg > 0) return;
+#pragma unroll
+    for (int j = 1; j < KW; ++j) odd |= flags[j * RW + rg] != 0;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      f32x2 o[KW];
+      float top = m[mt];
+#pragma unroll
+      for (int j = 1; j < KW; ++j) {
+        o[j] = *(const LDS(f32x2)*)(lds + SH::ACC + (((j - 1) * RW + rg) * MT + mt) * 512 + lane * 8);
+        top = fmaxf(top, o[j][0]);
+      }
+      const float f = to_frame<T>(m[mt], top, k2);
+      l[mt] *= f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) acc[db][mt] *= f;
+#pragma unroll
+      for (int j = 1; j < KW; ++j) {
+        const float fj = to_frame<T>(o[j][0], top, k2);
+        l[mt] += o[j][1] * fj;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const f32x4 x = *(const LDS(f32x4)*)(
+                lds + ((((j - 1) * RW + rg) * MT + mt) * DB + db) * 4096 + r * 1024 + lane * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[db][mt][4 * r + e] += fj * x[e];
+          }
+      }
+    }
+  }
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int r = rbase + 32 * mt + n;
+    if (r >= rows) continue;
+    const int x = r / group, g = r - x * group;
+    uint16_t* const to = out + (static_cast<int64_t>(q0 + x) * heads + kh * group + g) * head_dim;
+    const float inv = limit[mt] >= 0 ? 1.0f / l[mt] : 0.0f;   // (a row that sees nothing is 0)
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int d = 32 * db + 8 * i + 4 * h;
+        if (d >= head_dim) continue;
+        float o[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = acc[db][mt][4 * i + e] * inv;
+        if (odd) {
+#pragma unroll 1
+          for (int j = from; j <= limit[mt]; ++j) {
+            const u32x2 w = *reinterpret_cast<const u32x2*>(v + static_cast<int64_t>(j) * kv_stride + d);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t u = w[e >> 1] >> (16 * (e & 1)) & 0xffffu;
+              if ((u & T::kExponent) == T::kExponent) o[e] += T::value(static_cast<uint16_t>(u));
+            }
+          }
+        }
+        *reinterpret_cast<u32x2*>(to + d) = u32x2{T::pack(o[0], o[1]), T::pack(o[2], o[3])};
+      }
+  }
+}
+
+// An item whose keys or values hold what is not finite, a tile of each key group at a time: values in
+// tiles that some rows do not see whole are taken as 0 where they are not finite, and added to the rows
+// that see them when these are written. The same sums in the same order as in the kernel, so that the
+// rows that see none of it keep their bits. Not inlined: the registers of the kernel are laid out for
+// the other path.
+template <class T, class SH>
+__device__ __attribute__((noinline))
+void careful_item(lds_byte* lds, const uint16_t* pq, const uint16_t* pk, const uint16_t* pv, uint16_t* out,
+                  int64_t q_stride, int64_t kv_stride, int heads, int head_dim, int group, int kh, int q0, int nq,
+                  int k0, int nk, int tile, float k2, float slack) {
+  constexpr int MT = SH::MT, RW = SH::RW, KW = SH::KW, KK = SH::KK, DB = SH::DB;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int rg = wave % RW, kg = wave / RW, n = lane & 31, h = lane >> 5;
+  const int rows = nq * group, r0 = tile * SH::BM, rbase = r0 + rg * kWaveRows, ctx = nk - nq;
+  auto position = [&](int r) { return min(r, rows - 1) / group; };
+  const int tiles = uniform((max(0, position(r0 + SH::BM - 1) + ctx + 1) + kKeys - 1) / kKeys);
+  const int nfull = uniform(max(0, position(rbase) + ctx + 1) / kKeys);
+  s16x8 q[MT][KK];
+  int limit[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int r = min(rbase + 32 * mt + n, rows - 1), x = r / group, g = r - x * group;
+    limit[mt] = x + ctx;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      const int d = 16 * kk + 8 * h;
+      q[mt][kk] = d < head_dim ? *reinterpret_cast<const s16x8*>(
+                                     pq + static_cast<int64_t>(q0 + x) * q_stride + (kh * group + g) * head_dim + d)
+                               : s16x8{};
+    }
+  }
+  const int64_t first = static_cast<int64_t>(k0) * kv_stride + kh * head_dim;
+  const int at0 = kg * SH::STAGE;         // of this key group's tile
+  const int k_at = at0 + n * SH::ROW + (h ^ swizzle<SH::DP>(n & 15)) * 16;
+  const int vrow = 4 * h + ((lane & 15) >> 2), vchunk = 2 * (lane >> 4 & 1) + ((lane & 3) >> 1);
+  const s16x8 ones = T::ones();
+  float m[MT], c[MT];
+  f32x16 acc[DB + 1][MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    m[mt] = -INFINITY;
+    c[mt] = 0.0f;
+#pragma unroll
+    for (int db = 0; db <= DB; ++db) acc[db][mt] = f32x16{};
+  }
+  bool odd = false;
+#pragma unroll 1
+  for (int t0 = 0; t0 < tiles; t0 += KW) {
+    const int t = t0 + kg;
+    __syncthreads();
+    for (int i = rg * 64 + lane; i < 2 * kKeys * SH::CH; i += 64 * RW) {
+      const int ch = i % SH::CH, r = i / SH::CH % kKeys, values = i / (SH::CH * kKeys), j = t * kKeys + r;
+      u32x4 w = {0, 0, 0, 0};
+      if (j < nk && 8 * ch < head_dim)
+        w = *reinterpret_cast<const u32x4*>((values ? pv : pk) + first + static_cast<int64_t>(j) * kv_stride + 8 * ch);
+      *(LDS(u32x4)*)(lds + at0 + values * SH::MAT + r * SH::ROW + (ch ^ swizzle<SH::DP>(r & 15)) * 16) = w;
+    }
+    __syncthreads();
+    f32x16 s[MT] = {};
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      const s16x8 a = *(const LDS(s16x8)*)(lds + (k_at ^ (32 * kk)));
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) s[mt] = mfma32<T>(a, q[mt][kk], s[mt]);
+    }
+    u32x4 p[MT][2];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      const int last = limit[mt] - t * kKeys - 4 * h;
+      float top = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[mt][r] = 8 * (r >> 2) + (r & 3) <= last ? s[mt][r] : -INFINITY;
+        top = __builtin_elementwise_maximum(top, s[mt][r]);
+      }
+      const float above = m[mt] + slack;
+      float u = fmaxf(m[mt], top);
+      u = fmaxf(u, __shfl_xor(u, 32, 64));
+      u = u > above ? u : m[mt];
+      const float f = to_frame<T>(m[mt], u, k2);
+      if (u > m[mt]) {                    // (a frame that stays multiplies nothing: infinity stays)
+#pragma unroll
+        for (int db = 0; db <= DB; ++db) acc[db][mt] *= f;
+      }
+      m[mt] = u;
+      c[mt] = frame<T>(u, k2);
+#pragma unroll
+      for (int r = 0; r < 16; r += 2)
+        p[mt][r / 8][r % 8 / 2] = T::pack(__builtin_amdgcn_exp2f(fmaf(s[mt][r], k2, c[mt])),
+                                          __builtin_amdgcn_exp2f(fmaf(s[mt][r + 1], k2, c[mt])));
+    }
+#pragma unroll
+    for (int i = 0; i < SH::NV; ++i) {
+      const int at = at0 + SH::MAT + (16 * (i & 1) + vrow) * SH::ROW + 8 * (lane & 1), ch = 4 * (i >> 1);
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (LDS(s16x4)*)(lds + at + ((ch + vchunk) ^ swizzle<SH::DP>(vrow)) * 16));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (LDS(s16x4)*)(lds + at + 8 * SH::ROW + ((ch + vchunk) ^ swizzle<SH::DP>(vrow + 8)) * 16));
+      u32x4 w = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      if (t >= nfull) {
+        bool some = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool a = (w[e] & T::kExponent) == T::kExponent, b = (w[e] >> 16 & T::kExponent) == T::kExponent;
+          some |= a | b;
+          w[e] = (a ? 0 : w[e] & 0xffffu) | (b ? 0 : w[e] & 0xffff0000u);
+        }
+        odd |= __builtin_amdgcn_ballot_w64(some) != 0;
+      }
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+        acc[i >> 1][mt] = mfma32<T>(__builtin_bit_cast(s16x8, w), __builtin_bit_cast(s16x8, p[mt][i & 1]), acc[i >> 1][mt]);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+        acc[DB][mt] = mfma32<T>(ones, __builtin_bit_cast(s16x8, p[mt][i]), acc[DB][mt]);
+  }
+  __syncthreads();
+  finish<T, SH>(lds, acc, m, limit, odd, pv + first, kv_stride, out, heads, head_dim, group, k2, kh, q0, rows,
+                rbase, nfull * kKeys);
+}
 
 template <class T, class SH>
 __global__ void __launch_bounds__(kThreads, SH::PER_CU) prompt_kernel(Pass P) {
@@ -136,13 +363,20 @@ __global__ void __launch_bounds__(kThreads, SH::PER_CU) prompt_kernel(Pass P) {
   // the item: consecutive workgroups, and so the XCDs in turn, take its key heads
   const int rank = blockIdx.x / P.kv_heads, kh = blockIdx.x - rank * P.kv_heads;
   Item I;
+  // (read through the scalar cache: nothing of this launch writes them)
   if (P.items) {
-    if (rank >= *P.count) return;
-    I = P.items[rank];
+    CONSTANT(Item)* const items = (CONSTANT(Item)*)P.items;
+    if (rank >= *(CONSTANT(int)*)P.count) return;
+    I.q0 = items[rank].q0;
+    I.nq = items[rank].nq;
+    I.k0 = items[rank].k0;
+    I.nk = items[rank].nk;
+    I.tile = items[rank].tile;
   } else {
-    I.q0 = clamped(P.q_start[0], 0, P.num_queries);
-    I.nq = clamped(P.q_start[1], I.q0, P.num_queries) - I.q0;
-    const int32_t* const ks = P.k_start ? P.k_start : P.q_start;
+    CONSTANT(int)* const qs = (CONSTANT(int)*)P.q_start;
+    CONSTANT(int)* const ks = P.k_start ? (CONSTANT(int)*)P.k_start : qs;
+    I.q0 = clamped(qs[0], 0, P.num_queries);
+    I.nq = clamped(qs[1], I.q0, P.num_queries) - I.q0;
     I.k0 = clamped(ks[0], 0, P.num_keys);
     I.nk = clamped(ks[1], I.k0, P.num_keys) - I.k0;
     const int tiles = (I.nq * P.group + SH::BM - 1) / SH::BM;
@@ -155,11 +389,61 @@ __global__ void __launch_bounds__(kThreads, SH::PER_CU) prompt_kernel(Pass P) {
   auto position = [&](int r) { return min(r, rows - 1) / P.group; };
   const int need = max(0, position(r0 + SH::BM - 1) + ctx + 1);
   const int tiles = (need + kKeys - 1) / kKeys;
-  // tiles that some rows of this wavefront see, and those that all see whole
-  const int nsome = rbase < rows
-                        ? (max(0, uniform(position(rbase + kWaveRows - 1)) + ctx + 1) + kKeys - 1) / kKeys
-                        : 0;
-  const int nfull = min(nsome, max(0, uniform(position(rbase)) + ctx + 1) / kKeys);
+  // tiles that all rows of this wavefront see whole
+  const int nfull = max(0, uniform(position(rbase)) + ctx + 1) / kKeys;
+
+  // Loads: instruction i fills 1024 bytes, this lane the chunk at position lane % CH of row
+  // i * 1024 / ROW + lane / CH.
+  const int stride = static_cast<int>(P.kv_stride) * 2;
+  const uint64_t step_bytes = static_cast<uint64_t>(KW) * kKeys * stride;
+  int kv_off[SH::LOADS];
+#pragma unroll
+  for (int i = 0; i < SH::LOADS; ++i) {
+    const int r = (rg * SH::LOADS + i) * (1024 / SH::ROW) + lane / SH::CH;
+    const int c = (lane % SH::CH) ^ swizzle<SH::DP>(r);
+    kv_off[i] = 8 * c < P.head_dim ? r * stride + 16 * c : kPastRange;
+  }
+  const int lds_own = lds0 + kg * SH::S * SH::STAGE + rg * SH::LOADS * 1024;
+  const int64_t first = static_cast<int64_t>(I.k0) * P.kv_stride + kh * P.head_dim;
+  const uint64_t k_base = reinterpret_cast<uint64_t>(P.k + first), v_base = reinterpret_cast<uint64_t>(P.v + first);
+  // The key group's next tile to load, of keys and of values: where it is, and how many rows it and
+  // those behind it have.
+  struct Next {
+    uint64_t at;
+    int left;
+  };
+  Next keys = {k_base + static_cast<uint64_t>(kg) * kKeys * stride, I.nk - kg * kKeys};
+  Next values = {v_base + static_cast<uint64_t>(kg) * kKeys * stride, keys.left};
+  // (rows behind the sequence's last key are zeros, and so are tiles that are none)
+  auto issue = [&](Next& x, int place, bool values) {
+    int some = min(x.left, kKeys);
+    asm("" : "+s"(some));                 // (else one instruction of the vector unit)
+    const int range = max(some, 0) * stride;
+    load_tile<SH::LOADS>(i32x4{static_cast<int>(x.at), static_cast<int>(x.at >> 32), range, 0x00020000}, kv_off,
+                         lds_own + place + (values ? SH::MAT : 0));
+    x.at += step_bytes;
+    x.left -= KW * kKeys;
+  };
+  // Step j of a key group, whose tiles are kg, kg + KW, ..: the weights of its tile j, the scores of
+  // tile j + 1, and the values of tile j - 1 times theirs, so that the matrix units have products that
+  // wait for nothing while the vector units form weights. Once all have passed step j's barrier, the
+  // places of K_j and V_{j-2} are free: K_{j+S} and V_{j+S-2} go there. All but the WAIT newest loads
+  // have landed by then, so K_{j+1} and V_{j-1} are there (and K_{j+2}, whose first operands the end
+  // of the step reads).
+  const int rounds = (tiles + KW - 1) / KW;   // (of all wavefronts; without a tile of its own, one masks all)
+  const int whole = (nfull - kg + KW - 1) / KW;   // (0 or less: none)
+  auto place = [](int j) { return (j & (SH::S - 1)) * SH::STAGE; };
+  static_assert((SH::S & (SH::S - 1)) == 0, "places of tiles");
+#pragma unroll
+  for (int j = -SH::S; j < 0; ++j) {
+    issue(keys, place(j), false);
+    if (j == 1 - SH::S) {                 // (V_-1 is zeros)
+      Next none = {v_base, 0};
+      issue(none, place(-1), true);
+    } else if (j > 1 - SH::S) {
+      issue(values, place(j + SH::S - 2), true);
+    }
+  }
 
   // queries
   s16x8 q[MT][KK];
@@ -178,52 +462,19 @@ __global__ void __launch_bounds__(kThreads, SH::PER_CU) prompt_kernel(Pass P) {
     }
   }
 
-  // Loads: instruction i fills 1024 bytes, this lane the chunk at position lane % CH of row
-  // i * 1024 / ROW + lane / CH. Swizzle: a chunk of sixteen rows, and four chunks of four rows,
-  // touch all banks once.
-  auto swizzle = [](int r) {
-    return SH::DP == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
-  };
-  const int stride = static_cast<int>(P.kv_stride) * 2;
-  const uint64_t step_bytes = static_cast<uint64_t>(KW) * kKeys * stride;
-  int kv_off[SH::LOADS];
-#pragma unroll
-  for (int i = 0; i < SH::LOADS; ++i) {
-    const int r = (rg * SH::LOADS + i) * (1024 / SH::ROW) + lane / SH::CH;
-    const int c = (lane % SH::CH) ^ swizzle(r);
-    kv_off[i] = 8 * c < P.head_dim ? r * stride + 16 * c : kPastRange;
-  }
-  const int lds_own = lds0 + kg * SH::S * SH::STAGE + rg * SH::LOADS * 1024;
-  const int64_t first = static_cast<int64_t>(I.k0) * P.kv_stride + kh * P.head_dim;
-  const uint64_t k_base = reinterpret_cast<uint64_t>(P.k + first), v_base = reinterpret_cast<uint64_t>(P.v + first);
-  auto issue = [&](int t, int stage, bool values) {
-    // rows behind the sequence's last key are zeros, so are tiles that are none
-    const int left = t >= 0 && t < tiles ? min(kKeys, I.nk - t * kKeys) : 0;
-    const uint64_t a = (values ? v_base : k_base) + static_cast<uint64_t>(max(0, min(t, tiles))) * kKeys * stride;
-    const i32x4 rs = {static_cast<int>(a), static_cast<int>(a >> 32), left * stride, 0x00020000};
-    load_tile<SH::LOADS>(rs, kv_off, lds_own + stage + (values ? SH::MAT : 0));
-  };
   // Reads: keys, row n and chunk 2 kk + h; values, keys 4 h .. 4 h + 3 of 16 by sixteen of the
   // head, lane i of sixteen the eight bytes i % 4 at key i / 4, transposed by the read.
-  const int k_at = n * SH::ROW + (h ^ swizzle(n & 15)) * 16;
+  const int k_at = n * SH::ROW + (h ^ swizzle<SH::DP>(n & 15)) * 16;
   const int vrow = 4 * h + ((lane & 15) >> 2);
-  const int v_at = vrow * SH::ROW + ((2 * (lane >> 4 & 1) + ((lane & 3) >> 1)) ^ swizzle(vrow)) * 16 +
+  const int v_at = vrow * SH::ROW + ((2 * (lane >> 4 & 1) + ((lane & 3) >> 1)) ^ swizzle<SH::DP>(vrow)) * 16 +
                    (lane & 1) * 8;
   const int v_hi = (vrow + 8) * SH::ROW +
-                   ((2 * (lane >> 4 & 1) + ((lane & 3) >> 1)) ^ swizzle(vrow + 8)) * 16 + (lane & 1) * 8;
+                   ((2 * (lane >> 4 & 1) + ((lane & 3) >> 1)) ^ swizzle<SH::DP>(vrow + 8)) * 16 + (lane & 1) * 8;
 
   float m[MT], c[MT], above[MT];          // above: what a score moves the frame from
   // The last block is that of the sums: the weights times ones. (The vector unit would take 64
   // instructions a step for them, of 250; a dot product of two weights waits for the matrix unit.)
   f32x16 acc[DB + 1][MT];
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    m[mt] = above[mt] = -INFINITY;
-    c[mt] = 0.0f;
-#pragma unroll
-    for (int db = 0; db <= DB; ++db) acc[db][mt] = f32x16{};
-  }
-  bool odd = false;                       // a value in a masked tile that is not finite
 
   const int ring = kg * SH::S * SH::STAGE;
   int k_from[KK], v_from[DB][2];          // where operands lie in a key group's first place
@@ -283,46 +534,8 @@ __global__ void __launch_bounds__(kThreads, SH::PER_CU) prompt_kernel(Pass P) {
     return i == 0 ? __builtin_elementwise_maximum(s[0], s[1]) : max3(top, s[2 * i], s[2 * i + 1]);
   };
 
-  // A tile's values times its weights, where some rows do not see it whole: keys that a row does not
-  // see may hold anything, and weight 0 times NaN or infinity must not reach the row. Such values are
-  // taken as 0 here and added to the rows that see them when these are written. (A half word's
-  // exponent of ones, plus one, carries into its sign.)
   s16x8 ones8 = T::ones();
   asm volatile("" : "+a"(ones8));
-  auto add_values = [&](int stage, const u32x4 (&p)[MT][2], bool whole) {
-    s16x8 v[SH::NV];
-    uint32_t ones = 0;
-    constexpr uint32_t kExp = T::kExponent * 0x10001u, kOne = (0x8000u - T::kExponent) * 0x10001u;
-#pragma unroll
-    for (int i = 0; i < SH::NV; ++i) {
-      v[i] = value_operand(stage, i);
-      const u32x4 w = __builtin_bit_cast(u32x4, v[i]);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) ones |= (w[j] & kExp) + kOne;
-    }
-    if (!whole && __builtin_amdgcn_ballot_w64((ones & 0x80008000u) != 0)) {
-      odd = true;
-#pragma unroll
-      for (int i = 0; i < SH::NV; ++i) {
-        u32x4 w = __builtin_bit_cast(u32x4, v[i]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          w[j] = ((w[j] & T::kExponent) == T::kExponent ? 0 : w[j] & 0xffffu) |
-                 ((w[j] >> 16 & T::kExponent) == T::kExponent ? 0 : w[j] & 0xffff0000u);
-        v[i] = __builtin_bit_cast(s16x8, w);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < SH::NV; ++i)
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-        accumulate<T>(v[i], __builtin_bit_cast(s16x8, p[mt][i & 1]), acc[i >> 1][mt]);
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-        accumulate_ones<T>(ones8, __builtin_bit_cast(s16x8, p[mt][i]), acc[DB][mt]);
-  };
 
   // (left to the compiler, the queries' wait would be one for all loads in flight)
 #pragma unroll
@@ -330,33 +543,9 @@ __global__ void __launch_bounds__(kThreads, SH::PER_CU) prompt_kernel(Pass P) {
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+a"(q[mt][kk]));
 
-  // Step j of a key group, whose tiles are kg, kg + KW, ..: the weights of its tile j, the scores of
-  // tile j + 1, and the values of tile j - 1 times theirs, so that the matrix units have products that
-  // wait for nothing while the vector units form weights. Once all have passed step j's barrier, the
-  // places of K_j and V_{j-2} are free: K_{j+S} and V_{j+S-2} go there. All but the WAIT newest loads
-  // have landed by then, so K_{j+1} and V_{j-1} are there (and K_{j+2}, whose first operands the end
-  // of the step reads).
-  const int rounds = (tiles + KW - 1) / KW;
-  const int mine = (nsome - kg + KW - 1) / KW, whole = (nfull - kg + KW - 1) / KW;   // (0 or less: none)
-  auto place = [](int j) { return (j & (SH::S - 1)) * SH::STAGE; };
-  static_assert((SH::S & (SH::S - 1)) == 0, "places of tiles");
-  auto issue_keys = [&](int j) { issue(kg + (j + SH::S) * KW, place(j), false); };
-  auto issue_values = [&](int j) {
-    const int x = j + SH::S - 2;
-    issue(x < 0 ? -1 : kg + x * KW, place(x), true);
-  };
-#pragma unroll
-  for (int j = -SH::S; j < 0; ++j) {
-    issue_keys(j);
-    if (j >= 1 - SH::S) issue_values(j);  // (V_-1 is zeros)
-  }
   f32x16 s0[MT], s1[MT];
-  u32x4 p0[MT][2] = {}, p1[MT][2];        // weights, two of a row in a word
-  wait_loads<SH::WAIT>();
-  if constexpr (RW > 1) barrier();
-  scores(place(0), s0);
+  u32x4 p0[MT][2], p1[MT][2];             // weights, two of a row in a word
   s16x8 op[SH::AHEAD + 1];                // operand i at i % (AHEAD + 1)
-  if constexpr (SH::LOOK) unrolled<SH::AHEAD>([&](auto i) { op[i.value] = key_operand(place(1), i.value); });
   // Whether the frames moved for a tile's scores, and what the accumulators are multiplied with for
   // it once the weights before it are in them.
   bool moved = false;
@@ -376,25 +565,29 @@ __global__ void __launch_bounds__(kThreads, SH::PER_CU) prompt_kernel(Pass P) {
       for (int i = 0; i < 8; ++i) top[mt] = largest(s[mt], i, top[mt]);
     look(top);
   };
-  int j = 0;
-  if (whole > 4) look_all(s0);            // (else the steps below do)
+  // Keys of tile j that a row does not see.
+  auto mask = [&](int j, f32x16 (&s)[MT]) {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      const int last = limit[mt] - (kg + j * KW) * kKeys - 4 * h;
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        s[mt][r] = 8 * (r >> 2) + (r & 3) <= last ? s[mt][r] : -INFINITY;
+    }
+  };
 
-  // A step all of whose rows see tiles j - 1 (or it is none), j and j + 1 whole, J = j modulo 4; the
-  // frames are those of tile j. One product a slot, the vector instructions spread over the slots.
-  // kFull: the tiles it loads are full and lie one step behind those loaded before.
-  uint64_t k_next = 0, v_next = 0;
-  auto step = [&](auto Jc, auto full, int j, f32x16 (&s)[MT], f32x16 (&next)[MT], const u32x4 (&p)[MT][2],
+  // Step j, J = j modulo 4; the frames are those of tile j. One product a slot, the vector
+  // instructions spread over the slots. masked: some row may not see tile j + 1 whole.
+  auto step = [&](auto J, auto masked, int j, f32x16 (&s)[MT], f32x16 (&next)[MT], const u32x4 (&p)[MT][2],
                   u32x4 (&pn)[MT][2]) {
-    constexpr int J = Jc.value;
     wait_loads<SH::WAIT>();
-    if constexpr (RW > 1) barrier();
+    barrier();
     auto read = [&](auto ic) {
       constexpr int i = ic.value;
       if constexpr (i < SH::NK) op[i % (SH::AHEAD + 1)] = key_operand(place(J + 1), i);
       else if constexpr (i < SH::OPS) op[i % (SH::AHEAD + 1)] = value_operand(place(J - 1), i - SH::NK);
-      else if constexpr (SH::LOOK) op[i % (SH::AHEAD + 1)] = key_operand(place(J + 2), i - SH::OPS);
+      else op[i % (SH::AHEAD + 1)] = key_operand(place(J + 2), i - SH::OPS);
     };
-    if constexpr (!SH::LOOK) unrolled<SH::AHEAD>(read);
     auto product = [&](auto ic, auto mtc) {
       constexpr int i = ic.value, mt = mtc.value, v = i - SH::NK;
       const s16x8 a = op[i % (SH::AHEAD + 1)];
@@ -404,18 +597,6 @@ __global__ void __launch_bounds__(kThreads, SH::PER_CU) prompt_kernel(Pass P) {
         accumulate<T>(a, __builtin_bit_cast(s16x8, p[mt][v & 1]), acc[v >> 1][mt]);
       if constexpr (i >= SH::OPS - 2)
         accumulate_ones<T>(ones8, __builtin_bit_cast(s16x8, p[mt][v & 1]), acc[DB][mt]);
-    };
-    auto load = [&](bool values) {
-      if constexpr (full.value) {
-        const uint64_t a = values ? v_next : k_next;
-        load_tile<SH::LOADS>(i32x4{static_cast<int>(a), static_cast<int>(a >> 32), kKeys * stride, 0x00020000},
-                               kv_off, lds_own + place(values ? J + SH::S - 2 : J) + (values ? SH::MAT : 0));
-        (values ? v_next : k_next) += step_bytes;
-      } else if (values) {
-        issue_values(j);
-      } else {
-        issue_keys(j);
-      }
     };
     // two weights in a word, a pair after they are formed (their result is late)
     float e[3], top[MT];
@@ -428,8 +609,8 @@ __global__ void __launch_bounds__(kThreads, SH::PER_CU) prompt_kernel(Pass P) {
       constexpr int u = uc.value, i = u / MT, mt = u % MT, kAll = SH::OPS * MT;
       if constexpr (mt == 0) read(std::integral_constant<int, i + SH::AHEAD>{});
       product(std::integral_constant<int, i>{}, std::integral_constant<int, mt>{});
-      if constexpr (u == 1) load(false);
-      if constexpr (u == kAll / 4) load(true);
+      if constexpr (u == 1) issue(keys, place(J), false);
+      if constexpr (u == kAll / 4) issue(values, place(J + SH::S - 2), true);
       constexpr int kWeights = 16 * MT;
 #pragma unroll
       for (int x = u * kWeights / kAll; x < (u + 1) * kWeights / kAll; ++x) {
@@ -438,6 +619,8 @@ __global__ void __launch_bounds__(kThreads, SH::PER_CU) prompt_kernel(Pass P) {
       }
       // the next tile's scores are there a few products after their last one
       constexpr int kFrom = SH::NK * MT + 4, kPairs = 8 * MT;
+      if constexpr (masked.value && u == kFrom)
+        if (j + 1 >= whole) mask(j + 1, next);
       if constexpr (u >= kFrom) {
 #pragma unroll
         for (int x = (u - kFrom) * kPairs / (kAll - kFrom); x < (u + 1 - kFrom) * kPairs / (kAll - kFrom); ++x) {
@@ -451,142 +634,87 @@ __global__ void __launch_bounds__(kThreads, SH::PER_CU) prompt_kernel(Pass P) {
     if (moved) rescale(f);
     look(top);
   };
-  auto four = [&](auto full, int j) {
-    step(std::integral_constant<int, 0>{}, full, j, s0, s1, p0, p1);
-    step(std::integral_constant<int, 1>{}, full, j + 1, s1, s0, p1, p0);
-    step(std::integral_constant<int, 2>{}, full, j + 2, s0, s1, p0, p1);
-    step(std::integral_constant<int, 3>{}, full, j + 3, s1, s0, p1, p0);
+  // The last tile's values.
+  auto add_last = [&](int place, const u32x4 (&p)[MT][2]) {
+#pragma unroll
+    for (int i = 0; i < SH::NV; ++i) {
+      const s16x8 v = value_operand(place, i);
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+        accumulate<T>(v, __builtin_bit_cast(s16x8, p[mt][i & 1]), acc[i >> 1][mt]);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+        accumulate_ones<T>(ones8, __builtin_bit_cast(s16x8, p[mt][i]), acc[DB][mt]);
   };
-  k_next = k_base + static_cast<uint64_t>(kg + SH::S * KW) * kKeys * stride;
-  v_next = v_base + static_cast<uint64_t>(kg + (SH::S - 2) * KW) * kKeys * stride;
-  // tiles of this key group that are full
-  const int loads_whole = (min(tiles, I.nk / kKeys) - kg + KW - 1) / KW;
-#pragma unroll 1
-  for (; j + 4 < whole && j + 3 + SH::S < loads_whole; j += 4) four(std::true_type{}, j);
-#pragma unroll 1
-  for (; j + 4 < whole; j += 4) four(std::false_type{}, j);
-  // The others: tiles that some rows see in part, and steps of other wavefronts' tiles.
-#pragma unroll 1
-  for (; j < rounds; ++j) {
-    wait_loads<SH::WAIT>();
-    if constexpr (RW > 1) barrier();
-    issue_keys(j);
-    issue_values(j);
-    if (j > mine) continue;
-    if (j > 0) add_values(place(j - 1), p0, j - 1 < whole);
-    if (moved) rescale(f);
-    moved = false;
-    if (j == mine) continue;
-    const int t = kg + j * KW;
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      const int last = limit[mt] - t * kKeys - 4 * h;
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        s0[mt][r] = 8 * (r >> 2) + (r & 3) <= last ? s0[mt][r] : -INFINITY;
-    }
-    look_all(s0);
-    if (moved) rescale(f);
-    moved = false;
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int r = 0; r < 16; r += 2)
-        p0[mt][r / 8][r % 8 / 2] = T::pack(weight(s0, mt, r), weight(s0, mt, r + 1));
-    if (j + 1 < mine) scores(place(j + 1), s0);
-  }
-  wait_loads<0>();                        // (zeros for tiles that are none)
-  if constexpr (RW > 1) barrier();
-  if (mine == rounds && mine > 0) add_values(place(mine - 1), p0, mine - 1 < whole);
-
-  settle(acc);
-
-  // the key groups' parts, merged by group 0
-  float l[MT];
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt) l[mt] = acc[DB][mt][0];
-  LDS(int)* const flags = (LDS(int)*)(lds + SH::FLAGS);
-  if constexpr (KW > 1) {
-    barrier();                            // all have read their last tile
-    if (lane == 0) flags[wave] = odd;
-    if (kg > 0) {
-      const int w = (kg - 1) * RW + rg;
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            *(LDS(f32x4)*)(lds + ((w * MT + mt) * DB + db) * 4096 + r * 1024 + lane * 16) =
-                f32x4{acc[db][mt][4 * r], acc[db][mt][4 * r + 1], acc[db][mt][4 * r + 2], acc[db][mt][4 * r + 3]};
-        *(LDS(f32x2)*)(lds + SH::ACC + (w * MT + mt) * 512 + lane * 8) = f32x2{m[mt], l[mt]};
-      }
-    }
-    barrier();
-    if (kg > 0) return;
-#pragma unroll
-    for (int j = 1; j < KW; ++j) odd |= flags[j * RW + rg] != 0;
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      f32x2 o[KW];
-      float top = m[mt];
-#pragma unroll
-      for (int j = 1; j < KW; ++j) {
-        o[j] = *(const LDS(f32x2)*)(lds + SH::ACC + (((j - 1) * RW + rg) * MT + mt) * 512 + lane * 8);
-        top = fmaxf(top, o[j][0]);
-      }
-      const float f = to_frame<T>(m[mt], top, P.k2);
-      m[mt] = top;
-      l[mt] *= f;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) acc[db][mt] *= f;
-#pragma unroll
-      for (int j = 1; j < KW; ++j) {
-        const float fj = to_frame<T>(o[j][0], top, P.k2);
-        l[mt] += o[j][1] * fj;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const f32x4 x = *(const LDS(f32x4)*)(
-                lds + ((((j - 1) * RW + rg) * MT + mt) * DB + db) * 4096 + r * 1024 + lane * 16);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[db][mt][4 * r + e] += fj * x[e];
-          }
-      }
-    }
-  }
+  constexpr std::integral_constant<int, 0> j0{};
+  constexpr std::integral_constant<int, 1> j1{};
+  constexpr std::integral_constant<int, 2> j2{};
+  constexpr std::integral_constant<int, 3> j3{};
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
-    const int r = rbase + 32 * mt + n;
-    if (r >= rows) continue;
-    const int x = r / P.group, g = r - x * P.group;
-    uint16_t* const to = P.out + (static_cast<int64_t>(I.q0 + x) * P.heads + kh * P.group + g) * P.head_dim;
-    const float inv = limit[mt] >= 0 ? 1.0f / l[mt] : 0.0f;   // (a row that sees nothing is 0)
+    m[mt] = above[mt] = -INFINITY;
+    c[mt] = f[mt] = 0.0f;
+    p0[mt][0] = p0[mt][1] = u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int db = 0; db <= DB; ++db) acc[db][mt] = f32x16{};
+  }
+  settle(acc);
+  wait_loads<SH::WAIT>();
+  barrier();
+  scores(place(0), s0);
+  unrolled<SH::AHEAD>([&](auto i) { op[i.value] = key_operand(place(1), i.value); });
+  if (whole < 1) mask(0, s0);
+  look_all(s0);
+  int j = 0;
+#pragma unroll 1
+  for (; j + 4 < whole; j += 4) {
+    step(j0, std::false_type{}, j, s0, s1, p0, p1);
+    step(j1, std::false_type{}, j + 1, s1, s0, p1, p0);
+    step(j2, std::false_type{}, j + 2, s0, s1, p0, p1);
+    step(j3, std::false_type{}, j + 3, s1, s0, p1, p0);
+  }
+#pragma unroll 1
+  for (; j < rounds; ++j) {
+    step(j, std::true_type{}, j, s0, s1, p0, p1);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      s0[mt] = s1[mt];
+      p0[mt][0] = p1[mt][0];
+      p0[mt][1] = p1[mt][1];
+    }
+  }
+  wait_loads<0>();                        // (zeros for tiles that are none)
+  barrier();
+  add_last(place(rounds - 1), p0);
+  settle(acc);
+
+  // Weight 0 times a value that is not finite is NaN, and a row must not see the values behind it:
+  // an item with a sum that is not finite is computed again, a tile at a time.
+  float zero = 0.0f;                      // NaN if some sum is not finite
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int d = 32 * db + 8 * i + 4 * h;
-        if (d >= P.head_dim) continue;
-        float o[4];
+      for (int r = 0; r < 16; ++r) zero = fmaf(acc[db][mt][r], 0.0f, zero);
+  LDS(int)* const flags = (LDS(int)*)(lds + SH::FLAGS);
+  const uint64_t bad = __builtin_amdgcn_ballot_w64(zero != zero);
+  if (lane == 0) flags[wave] = bad != 0;
+  barrier();                              // (all have read their last tile, too)
+  int any = 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = acc[db][mt][4 * i + e] * inv;
-        if (odd) {
-#pragma unroll 1
-          for (int j = nfull * kKeys; j <= limit[mt]; ++j) {
-            const u32x2 w = *reinterpret_cast<const u32x2*>(
-                P.v + first + static_cast<int64_t>(j) * P.kv_stride + d);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t u = w[e >> 1] >> (16 * (e & 1)) & 0xffffu;
-              if ((u & T::kExponent) == T::kExponent) o[e] += T::value(static_cast<uint16_t>(u));
-            }
-          }
-        }
-        *reinterpret_cast<u32x2*>(to + d) = u32x2{T::pack(o[0], o[1]), T::pack(o[2], o[3])};
-      }
+  for (int w = 0; w < kWaves; ++w) any |= flags[w];
+  if (__builtin_expect(uniform(any), 0)) {
+    careful_item<T, SH>(lds, P.q, P.k, P.v, P.out, P.q_stride, P.kv_stride, P.heads, P.head_dim, P.group,
+                        kh, I.q0, I.nq, I.k0, I.nk, I.tile, P.k2, P.slack);
+    return;
   }
+
+  finish<T, SH>(lds, acc, m, limit, false, nullptr, 0, P.out, P.heads, P.head_dim, P.group, P.k2, kh, I.q0, rows,
+                rbase, 0);
 }
 
 // The items of all sequences, those with the most keys first, so that none begins late and
@@ -690,9 +818,12 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(Pass P, int bm) {
   }
 }
 
+// Rows of a workgroup, of which a CU holds one: 256 of them where they give every CU one, else 128 (two
+// key groups). One prompt, 32 heads over 8 of 128, by 64 / 128 / 256 rows: 100 tokens 14.7 / 13.2 /
+// 13.5 us, 700 31 / 21 / 28, 2000 (250 workgroups of 256) 90 / 58 / 61, 3000 (375) 155 / 114 / 98, 6000
+// 430 / 327 / 301.
 int block_rows(int64_t rows, int64_t kv_heads, int cus) {
-  if (rows / 256 * kv_heads >= 2 * cus) return 256;
-  return rows / 128 * kv_heads >= cus ? 128 : 64;
+  return rows / 256 * kv_heads > cus ? 256 : 128;
 }
 
 int64_t most_items(int64_t rows, int64_t batch, int bm) { return rows / bm + batch; }
@@ -714,8 +845,7 @@ template <class T, int DP>
 hipError_t run(const Pass& P, int bm, unsigned wgs, hipStream_t stream) {
   const dim3 grid(wgs), block(kThreads);
   if (bm == 256) hipLaunchKernelGGL((prompt_kernel<T, Shape<DP, 4>>), grid, block, 0, stream, P);
-  else if (bm == 128) hipLaunchKernelGGL((prompt_kernel<T, Shape<DP, 2>>), grid, block, 0, stream, P);
-  else hipLaunchKernelGGL((prompt_kernel<T, Shape<DP, 1>>), grid, block, 0, stream, P);
+  else hipLaunchKernelGGL((prompt_kernel<T, Shape<DP, 2>>), grid, block, 0, stream, P);
   return hipGetLastError();
 }
 
@@ -728,7 +858,7 @@ size_t prompt_workspace(int32_t batch, int32_t num_queries, int32_t num_keys, in
   (void)num_keys;
   (void)head_dim;
   const int64_t rows = static_cast<int64_t>(num_queries) * (heads / kv_heads);
-  return align256(256 + static_cast<size_t>(most_items(rows, batch, kWaveRows)) * sizeof(Item));
+  return align256(256 + static_cast<size_t>(most_items(rows, batch, 2 * kWaveRows)) * sizeof(Item));
 }
 
 int launch_prompt(const PromptArgs& a, void* workspace, hipStream_t stream) {
