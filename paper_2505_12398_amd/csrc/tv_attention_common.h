@@ -46,6 +46,12 @@ struct Bf16 {
   static __device__ __forceinline__ uint32_t widen(uint32_t x, float f) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, f, SEL));
   }
+  // two elements divided by f, a power of two, as 4 bits each into byte SEL: to the nearest, ties to
+  // even, beyond 6 to 6
+  template <int SEL>
+  static __device__ __forceinline__ uint32_t narrow(uint32_t old, uint32_t two, float f) {
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(old, __builtin_bit_cast(bf16x2, two), f, SEL);
+  }
   static __device__ __forceinline__ float value(uint16_t x) { return __uint_as_float(uint32_t{x} << 16); }
   static __device__ __forceinline__ s16x8 ones() {
     return s16x8{0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80};
@@ -69,6 +75,10 @@ struct F16 {
   template <int SEL>
   static __device__ __forceinline__ uint32_t widen(uint32_t x, float f) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x, f, SEL));
+  }
+  template <int SEL>
+  static __device__ __forceinline__ uint32_t narrow(uint32_t old, uint32_t two, float f) {
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(old, __builtin_bit_cast(f16x2, two), f, SEL);
   }
   static __device__ __forceinline__ float value(uint16_t x) {
     return static_cast<float>(__builtin_bit_cast(_Float16, x));
