@@ -109,7 +109,8 @@ struct Shape {
   static constexpr int ROW = DP * 2;
   static constexpr int HALF = kHalf * ROW;        // bytes
   static constexpr int LOADS = HALF / 1024;       // load instructions of a half
-  static constexpr int MAT = 2 * HALF, STAGE = 2 * MAT;
+  // a tile's keys and, VALUES behind them, its values (in 4 bits: its values alone)
+  static constexpr int MAT = 2 * HALF, VALUES = Q4 ? 0 : MAT, STAGE = VALUES + MAT;
   // loads of a wavefront per tile, of keys (or values)
   static constexpr int MINE = 2 * LOADS / RW;
   // tiles in LDS per key group
@@ -372,7 +373,7 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
                             (kh * P.group + r - node * P.group) * P.head_dim;
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) {
-        const int d = 32 * kk + 8 * qg;
+        const int d = SH::Q4 ? 8 * (KK * qg + kk) : 32 * kk + 8 * qg;
         q[mt][kk] = d < P.head_dim ? *reinterpret_cast<const s16x8*>(src + d) : s16x8{};
       }
     }
@@ -605,7 +606,7 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
     constexpr int kAhead = DB / 2;
     auto read_values = [&](int stage, auto dbc, s16x8 (&a)[kAhead + 1]) {
       constexpr int db = dbc.value;
-      const int at = (stage + SH::MAT + v_at) ^ (32 * db);
+      const int at = (stage + SH::VALUES + v_at) ^ (32 * db);
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS(s16x4)*)(lds + at));
       const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS(s16x4)*)(lds + at + SH::HALF));
       a[db % (kAhead + 1)] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -614,7 +615,7 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
     // infinity must not reach the row. Such values enter the product as 0 and are
     // added to the rows that see them once these are written.
     auto clean = [&](int stage) {
-      const int mat = stage + SH::MAT;
+      const int mat = stage + SH::VALUES;
       // (a half word's exponent of ones, plus one, carries into its sign's place)
       constexpr uint32_t kExp = T::kExponent * 0x10001u, kOne = (0x8000u - T::kExponent) * 0x10001u;
       const int hl = here(lane);
@@ -664,67 +665,101 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
       add_values(stage, p, v);
     };
     if constexpr (SH::Q4) {
-      // A cached tile of 4 bits is read into registers a round ahead, 16 bytes (a block of 32
-      // elements) and their exponent a lane, and widened into the tile's place in LDS. It
-      // comes in units: heads of 128, a half's keys or values; of 64, a tile's. Wavefronts that
-      // share tiles share the units, and tiles take two places in turn: a place is written once
-      // all have passed the barrier behind the products of the tile before it.
-      constexpr int kUnits = SH::DP == 128 ? 4 : 2, kOwn = (kUnits + RW - 1) / RW;
-      constexpr int kBlocks = SH::DP / 32;
-      const int blk = lane % kBlocks, row = lane / kBlocks;  // (heads of 64: rows of both halves)
-      const bool in_head = blk < P.head_dim >> 5;            // (else the zeros behind a head)
-      u32x4 raw[kOwn] = {};
-      uint32_t exponent[kOwn] = {};
+      // A cached tile of 4 bits is read into registers kDeep rounds ahead and widened there.
+      // Keys need no LDS: the products take the head's elements in the order in which lanes hold
+      // them, lane (n, g) elements 8 KK g .. 8 KK (g + 1) - 1 of key n, eight of them each (the
+      // queries are loaded in that order), and wavefronts that share tiles each read all of their
+      // keys. Values are shared, kWords words and their exponent a lane, and widened into the
+      // tile's place in LDS. Tiles of wavefronts that share take two places in turn: a place is
+      // written once all have passed the barrier behind the products of the tile before it.
+      //
+      // Keys through LDS too: single tokens of 64 sequences 190 us, 256 trees of 65 nodes 870, four
+      // chains of 6 in heads of 64 with a prefix 89; so 173, 847 and 83. Rounds ahead 1 / 2 / 3 / 4:
+      // the first 173 / 175 / 176 / 178, the last, whose tiles are half as large, 87 / 83 / 83 / 84;
+      // rows of 48 in heads of 128 have registers for one. (Four wavefronts of 16 rows on a SIMD,
+      // in 128 registers each, spill: 254 us.)
+      constexpr int kDeep = SH::DP == 64 ? 2 : 1;
+      constexpr int kAll = kKeys * SH::DP / 8 / 64;          // a lane's words of the tile
+      constexpr int kWords = kAll >= 4 * RW ? 4 : 2;
+      constexpr int kUnits = kAll / kWords, kOwn = (kUnits + RW - 1) / RW;
+      constexpr int kPieces = SH::DP / 8 / kWords, kUnitRows = 64 / kPieces;
+      typedef __attribute__((ext_vector_type(KK))) uint32_t key_words;
+      typedef __attribute__((ext_vector_type(kWords))) uint32_t value_words;
+      const int blocks = P.head_dim >> 5;
+      const bool k_in = 8 * KK * g < P.head_dim;             // (else the zeros behind a head)
+      const int k_off = n * row_bytes + 4 * KK * g, ke_off = n * blocks + KK * g / 4;
+      const int piece = lane % kPieces, row = lane / kPieces;
+      const bool v_in = 8 * kWords * piece < P.head_dim;
+      const int v_off = (row & (kHalf - 1)) * row_bytes + 4 * kWords * piece;
+      const int ve_off = (row & (kHalf - 1)) * blocks + kWords * piece / 4;
+      key_words kw[kDeep][2] = {};
+      value_words vw[kDeep][kOwn] = {};
+      uint32_t ke[kDeep][2] = {}, ve[kDeep][kOwn] = {};
       int next[2] = {};                                      // pages of the tile to load next
+      uint64_t at[2] = {};                                   // its halves' first rows
+      uint32_t to_e[2] = {};                                 // from there to their exponents
       auto fetch4 = [&](int t) {
         if (t < min(nct, tile_end)) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) next[h] = pages[min(first_key(t, h), last_key) >> P.page_shift];
         }
       };
-      auto load4 = [&](int t) {
+      auto place4 = [&](int t) {
         if (t >= min(nct, tile_end)) return;
-        uint64_t at[2];                                      // the halves' keys
-        uint32_t off[2];                                     // the first row's place in its page
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int key = min(first_key(t, h), last_key) & ~(kHalf - 1);
-          at[h] = key_at(next[h], 0);
-          off[h] = key & in_page;
+          at[h] = key_at(next[h], key);
+          to_e[h] = (static_cast<uint32_t>(row_bytes) << P.page_shift) -
+                    static_cast<uint32_t>((key & in_page) * (row_bytes - blocks));
         }
+      };
+      auto load_keys = [&](auto to, int t) {
+        if (t >= min(nct, tile_end)) return;
 #pragma unroll
-        for (int j = 0; j < kOwn; ++j) {
-          const int u = rg + j * RW;
-          if (u >= kUnits) continue;
-          const int h = SH::DP == 128 ? u & 1 : row >> 4;
-          const uint64_t v = (SH::DP == 128 ? u >> 1 : u) ? v_base - k_base : 0;
-          const uint8_t* const from = reinterpret_cast<const uint8_t*>((h ? at[1] : at[0]) + v);
-          const uint32_t r = (h ? off[1] : off[0]) + (row & (kHalf - 1));
-          if (in_head) {
-            raw[j] = *reinterpret_cast<const u32x4*>(from + r * row_bytes + 16 * blk);
-            exponent[j] = from[(static_cast<uint32_t>(row_bytes) << P.page_shift) +
-                               r * (P.head_dim >> 5) + blk];
+        for (int h = 0; h < 2; ++h) {
+          const uint8_t* const from = reinterpret_cast<const uint8_t*>(at[h]);
+          if (k_in) {
+            kw[to.value][h] = *reinterpret_cast<const key_words*>(from + k_off);
+            ke[to.value][h] = (from + to_e[h])[ke_off];
           }
         }
       };
-      auto widen = [&](int stage, int t) {
+      auto load_values = [&](auto to, int t) {
+        if (t >= min(nct, tile_end)) return;
 #pragma unroll
         for (int j = 0; j < kOwn; ++j) {
           const int u = rg + j * RW;
           if (u >= kUnits) continue;
-          const int h = SH::DP == 128 ? u & 1 : row >> 4, r = row & (kHalf - 1);
-          u32x4 w = raw[j];
+          const int first = u * kUnitRows;
+          // (units of 32 rows: lanes of both halves)
+          const int h = kUnitRows == kKeys ? row >> 4 : first >> 4;
+          const uint32_t skip = first & (kHalf - 1);
+          const uint8_t* const from = reinterpret_cast<const uint8_t*>((h ? at[1] : at[0]) + (v_base - k_base));
+          if (v_in) {
+            vw[to.value][j] = *reinterpret_cast<const value_words*>(from + skip * row_bytes + v_off);
+            ve[to.value][j] = (from + (h ? to_e[1] : to_e[0]) + skip * blocks)[ve_off];
+          }
+        }
+      };
+      auto widen = [&](auto held, int stage, int t) {
+#pragma unroll
+        for (int j = 0; j < kOwn; ++j) {
+          const int u = rg + j * RW;
+          if (u >= kUnits) continue;
+          const int at_row = u * kUnitRows + row, r = at_row & (kHalf - 1);
+          value_words w = vw[held.value][j];
           // rows behind the last are zeros: their weight 0 must not meet a value that is not finite
-          uint32_t e = exponent[j];
-          if (t >= nfull && first_key(t, h) + r > last_key) {
-            w = u32x4{0, 0, 0, 0};
+          uint32_t e = ve[held.value][j];
+          if (t >= nfull && first_key(t, 0) + at_row > last_key) {
+            w = 0;
             e = 0;
           }
           const float f = __uint_as_float(e << 23);
-          const int to = stage + ((SH::DP == 128 ? u >> 1 : u) ? SH::MAT : 0) + h * SH::HALF + r * SH::ROW;
+          const int to = stage + (at_row >> 4) * SH::HALF + r * SH::ROW;
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            *(LDS(u32x4)*)(lds + to + ((4 * blk + i) ^ swizzle(r)) * 16) =
+          for (int i = 0; i < kWords; ++i)
+            *(LDS(u32x4)*)(lds + to + ((kWords * piece + i) ^ swizzle(r)) * 16) =
                 u32x4{T::template widen<0>(w[i], f), T::template widen<1>(w[i], f),
                       T::template widen<2>(w[i], f), T::template widen<3>(w[i], f)};
         }
@@ -733,44 +768,87 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
       auto put_nodes = [&](int stage, int t) {
         const int first = (R.tiles - 1 - t) * kKeys;
 #pragma unroll 4
-        for (int i = rg * 64 + lane; i < 2 * kKeys * SH::CH; i += 64 * RW) {
-          const int c = i % SH::CH, r = i / SH::CH % kKeys, values = i / (SH::CH * kKeys);
+        for (int i = rg * 64 + lane; i < kKeys * SH::CH; i += 64 * RW) {
+          const int c = i % SH::CH, r = i / SH::CH;
           const int x = first + r;
           u32x4 w = {0, 0, 0, 0};
           if (x < P.num_nodes && 8 * c < P.head_dim)
             w = *reinterpret_cast<const u32x4*>(
-                (values ? P.v_new : P.k_new) +
-                (static_cast<int64_t>(b) * P.num_nodes + x) * P.kv_stride + kh * P.head_dim + 8 * c);
-          *(LDS(u32x4)*)(lds + stage + (values ? SH::MAT : 0) + (r >> 4) * SH::HALF +
-                         (r & 15) * SH::ROW + (c ^ swizzle(r & 15)) * 16) = w;
+                P.v_new + (static_cast<int64_t>(b) * P.num_nodes + x) * P.kv_stride +
+                kh * P.head_dim + 8 * c);
+          *(LDS(u32x4)*)(lds + stage + (r >> 4) * SH::HALF + (r & 15) * SH::ROW +
+                         (c ^ swizzle(r & 15)) * 16) = w;
         }
       };
+      // Scores of a tile, operand (half, step) of `key`.
+      auto scores4 = [&](f32x4 (&s)[MT][2], auto key) {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+          s[mt][0] = s[mt][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        unrolled<2 * KK>([&](auto ic) {
+          constexpr int i = ic.value, kb = i % 2, kk = i / 2;
+          const s16x8 a = key(kb, kk);
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) s[mt][kb] = T::mfma(a, q[mt][kk], s[mt][kb]);
+        });
+      };
+      auto cached_scores = [&](auto held, f32x4 (&s)[MT][2]) {
+        const float f[2] = {__uint_as_float(ke[held.value][0] << 23),
+                            __uint_as_float(ke[held.value][1] << 23)};
+        scores4(s, [&](int kb, int kk) {
+          const uint32_t w = kw[held.value][kb][kk];
+          return __builtin_bit_cast(
+              s16x8, u32x4{T::template widen<0>(w, f[kb]), T::template widen<1>(w, f[kb]),
+                           T::template widen<2>(w, f[kb]), T::template widen<3>(w, f[kb])});
+        });
+      };
+      auto node_scores = [&](int t, f32x4 (&s)[MT][2]) {
+        const int first = (R.tiles - 1 - t) * kKeys + here(n);
+        const int hg = here(g);
+        scores4(s, [&](int kb, int kk) {
+          const int x = first + 16 * kb, d = 8 * (KK * hg + kk);
+          return x < P.num_nodes && d < P.head_dim
+                     ? *reinterpret_cast<const s16x8*>(
+                           P.k_new + (static_cast<int64_t>(b) * P.num_nodes + x) * P.kv_stride +
+                           kh * P.head_dim + d)
+                     : s16x8{};
+        });
+      };
       fetch4(tile0);
-      load4(tile0);
-      fetch4(tile0 + KW);
+      unrolled<kDeep>([&](auto j) {
+        place4(tile0 + j.value * KW);
+        load_values(j, tile0 + j.value * KW);
+        load_keys(j, tile0 + j.value * KW);
+        fetch4(tile0 + (j.value + 1) * KW);
+      });
       prepare();
       constexpr int kLast = (SH::S - 1) * SH::STAGE;
       int stage = ring;
-      auto round = [&](auto full, int i, int t) {
-        if (full.value || t < nct) widen(stage, t);
+      auto round = [&](auto full, auto held, int i, int t) {
+        f32x4 s[MT][2];
+        place4(t + kDeep * KW);
+        if (full.value || t < nct) widen(held, stage, t);
         else if (t < tile_end) put_nodes(stage, t);
-        load4(t + KW);
-        fetch4(t + 2 * KW);
+        load_values(held, t + kDeep * KW);
+        if (full.value || t < nct) cached_scores(held, s);
+        else if (t < tile_end) node_scores(t, s);
+        load_keys(held, t + kDeep * KW);
+        fetch4(t + (kDeep + 1) * KW);
         if constexpr (RW == 1) wait_reads();
         else barrier();
-        if (full.value || KW == 1 || i < mine) {
-          f32x4 s[MT][2];
-          scores(stage, s);
-          multiply(full, stage, t, s);
-        }
+        if (full.value || KW == 1 || i < mine) multiply(full, stage, t, s);
         if constexpr (RW == 1) wait_reads();
         stage = stage == ring + kLast ? ring : stage + SH::STAGE;
       };
       int i = 0, t = tile0;
 #pragma unroll 1
-      for (const int lim = min(nfull, tile_end); t < lim; ++i, t += KW) round(std::true_type{}, i, t);
+      for (const int lim = min(nfull, tile_end) - (kDeep - 1) * KW; t < lim; i += kDeep, t += kDeep * KW)
+        unrolled<kDeep>([&](auto j) { round(std::true_type{}, j, i + j.value, t + j.value * KW); });
 #pragma unroll 1
-      for (; i < rounds; ++i, t += KW) round(std::false_type{}, i, t);
+      for (; i < rounds; i += kDeep, t += kDeep * KW)
+        unrolled<kDeep>([&](auto j) {
+          if (j.value == 0 || i + j.value < rounds) round(std::false_type{}, j, i + j.value, t + j.value * KW);
+        });
     } else {
       // Round i multiplies tile i. Its keys' place is free after the first product and its
       // values' after the second, once all wavefronts that share them are there, and is
