@@ -7,6 +7,22 @@
 // consecutive keys of one row at a time, which is how the second product wants its operand, the
 // keys taken in the order in which the lanes hold them; values are read transposed from LDS.
 // Frames and the rounding of weights are those of tv_tree_attention.
+//
+// A wavefront has its SIMD to itself, and so all its registers: queries and accumulators in those
+// that the vector unit does not compute in, scores, weights and operands in the others. In step j
+// it multiplies tile j + 1's keys, takes tile j's weights and adds tile j - 1's values, in one
+// order of instructions in which the matrix unit always has a product to run beside the vector
+// unit's work (one after the other: 16384 tokens 4215 us, so 1905). 36 products of 32 cycles a
+// step of 32 keys, row sums among them, as products with ones (dot products in the vector unit
+// would hold up the matrix unit). Tiles come into LDS three steps ahead.
+//
+// What bounds it. One prompt of 16384 tokens, 32 heads over 8 of 128: 1905 us, 1155 TFLOP/s of the
+// 1612 that a large product reaches here: a step takes 1550 to 1650 cycles of which the matrix unit
+// is busy 1152 (the clock falls to 1.8 or 1.9 GHz meanwhile). An item costs 13 thousand cycles
+// before its first step, nine of them the queries' loads, and 6 behind its last: 32 prompts of
+// 20 to 2999 tokens 1042 us, 800 TFLOP/s. Few items are bound by the longest: four pieces behind
+// long contexts have 350 items for 256 CUs, 241 us. One short prompt: 13 us, of which the kernel
+// takes 8.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -819,14 +835,18 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(Pass P, int bm) {
 }
 
 // Rows of a workgroup, of which a CU holds one: 256 of them where they give every CU one, else 128 (two
-// key groups). One prompt, 32 heads over 8 of 128, by 64 / 128 / 256 rows: 100 tokens 14.7 / 13.2 /
-// 13.5 us, 700 31 / 21 / 28, 2000 (250 workgroups of 256) 90 / 58 / 61, 3000 (375) 155 / 114 / 98, 6000
-// 430 / 327 / 301.
-int block_rows(int64_t rows, int64_t kv_heads, int cus) {
-  return rows / 256 * kv_heads > cus ? 256 : 128;
-}
-
+// key groups), and in heads of 64 (whose four key groups' tiles LDS holds) 64 where no CU has two. One
+// prompt, 32 heads over 8 of 128, by 128 / 256 rows: 100 tokens 13.2 / 13.5 us, 700 21 / 28, 2000 (250
+// workgroups of 256) 58 / 61, 3000 (375) 114 / 98, 6000 327 / 301. Heads of 64, by 64 / 128 rows: 100
+// tokens 9.4 / 9.2, 500 (256 workgroups of 64) 12.5 / 13.2, 512 behind 7488 more 49 / 73, 1000 23.5 /
+// 18.2, two of 512 behind 7488 more 105 / 95.
 int64_t most_items(int64_t rows, int64_t batch, int bm) { return rows / bm + batch; }
+
+int block_rows(int64_t rows, int64_t batch, int64_t kv_heads, int head_dim, int cus) {
+  if (rows / 256 * kv_heads > cus) return 256;
+  const int64_t narrow = (rows + kWaveRows - 1) / kWaveRows + batch - 1;
+  return head_dim <= 64 && narrow * kv_heads <= cus ? 64 : 128;
+}
 
 int device_cus() {
   constexpr int kMaxDevices = 64;
@@ -845,7 +865,10 @@ template <class T, int DP>
 hipError_t run(const Pass& P, int bm, unsigned wgs, hipStream_t stream) {
   const dim3 grid(wgs), block(kThreads);
   if (bm == 256) hipLaunchKernelGGL((prompt_kernel<T, Shape<DP, 4>>), grid, block, 0, stream, P);
-  else hipLaunchKernelGGL((prompt_kernel<T, Shape<DP, 2>>), grid, block, 0, stream, P);
+  else if constexpr (DP == 64) {
+    if (bm == 64) hipLaunchKernelGGL((prompt_kernel<T, Shape<DP, 1>>), grid, block, 0, stream, P);
+    else hipLaunchKernelGGL((prompt_kernel<T, Shape<DP, 2>>), grid, block, 0, stream, P);
+  } else hipLaunchKernelGGL((prompt_kernel<T, Shape<DP, 2>>), grid, block, 0, stream, P);
   return hipGetLastError();
 }
 
@@ -856,9 +879,8 @@ namespace tv {
 size_t prompt_workspace(int32_t batch, int32_t num_queries, int32_t num_keys, int32_t heads,
                         int32_t kv_heads, int32_t head_dim) {
   (void)num_keys;
-  (void)head_dim;
   const int64_t rows = static_cast<int64_t>(num_queries) * (heads / kv_heads);
-  return align256(256 + static_cast<size_t>(most_items(rows, batch, 2 * kWaveRows)) * sizeof(Item));
+  return align256(256 + static_cast<size_t>(most_items(rows, batch, head_dim <= 64 ? 64 : 128)) * sizeof(Item));
 }
 
 int launch_prompt(const PromptArgs& a, void* workspace, hipStream_t stream) {
@@ -884,7 +906,7 @@ int launch_prompt(const PromptArgs& a, void* workspace, hipStream_t stream) {
   const double slack = 8.0 / static_cast<double>(P.k2);
   P.slack = slack < 3.0e38 ? static_cast<float>(slack) : 3.0e38f;
   const int64_t rows = static_cast<int64_t>(a.num_queries) * P.group;
-  const int bm = block_rows(rows, a.kv_heads, cus);
+  const int bm = block_rows(rows, a.batch, a.kv_heads, a.head_dim, cus);
   const int64_t wgs = most_items(rows, a.batch, bm) * a.kv_heads;
   if (a.batch > 1) {
     P.count = static_cast<int*>(workspace);

@@ -231,6 +231,25 @@ def test_infinite_values(nk):
         assert torch.equal(got[..., rest], clean[..., rest])
 
 
+@pytest.mark.parametrize("n,earlier", [(30, 3001), (500, 0), (512, 1490), (700, 333), (2500, 0)])
+def test_heights_of_heads_of_64(n, earlier):
+    """Workgroups of 64, 128 and 256 rows: an infinite value and keys that are not numbers reach the
+    queries that see them, and change no bit of the others."""
+    call = inputs([n], [n + earlier], 32, 8, 64, "f16", seed=n)
+    clean = check(call, "f16")
+    rest = [d for d in range(64) if d != 5]
+    for at in (earlier, earlier + n // 2, earlier + n - 1):
+        k, v = call["k"].clone(), call["v"].clone()
+        v[at, :, 5] = -float("inf")
+        sees = torch.arange(n, device=DEV) + earlier >= at
+        got = tv.prompt_attention(**dict(call, k=k, v=v))
+        assert (got[sees][..., 5] == -float("inf")).all() and torch.equal(got[..., rest], clean[..., rest])
+        assert torch.equal(got[~sees], clean[~sees])
+        k[at:] = float("nan")
+        got = tv.prompt_attention(**dict(call, k=k, v=v))
+        assert torch.isnan(got[sees]).all() and torch.equal(got[~sees], clean[~sees])
+
+
 def test_large_scores_and_growing_ones():
     """One key holds nearly all of a row's weight; every later key scores higher."""
     check(inputs([300, 20], None, 4, 2, 64, scale_q=40.0))

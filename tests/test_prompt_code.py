@@ -34,7 +34,7 @@ def test_prompt_wait_states(tmp_path):
                    capture_output=True)
     text = out.read_text()
     kernels = re.findall(r"^(_ZN\S*prompt_kernel\S*):\s*;.*?\n(.*?)^\.Lfunc_end", text, re.M | re.S)
-    assert len(kernels) == 8           # two types, two head sizes, two heights
+    assert len(kernels) == 10          # two types; heads of 64 in three heights, of 128 in two
     for name, body in kernels:
         assert re.search(r"v_mfma_f32_32x32x16_b?f16 a\[", body) and re.search(r"offen lds", body)
         assert [f for f in violations(body) if of_assembly(f)] == [], name
