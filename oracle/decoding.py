@@ -1,7 +1,7 @@
 """Plain 64-bit forms of the operators around a verification: attention of tree
 nodes over a paged cache and of prompts, penalties, biases and masks on logits, growth
-of block tables, commit of accepted keys and values, in 4 bits too. Written from their definitions, one
-tree, node and token at a time; no code of the library."""
+of block tables, commit of accepted keys and values, in 4 bits too. Written from their
+definitions, one tree, node and token at a time; no code of the library."""
 
 import numpy as np
 

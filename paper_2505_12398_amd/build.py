@@ -25,7 +25,7 @@ FLAGS = [
     "-Wall", "-Wno-unused-result",
 ]
 
-# The prompts' kernel holds 336 registers of a wavefront's 512: its products' results that the vector
+# The prompts' kernel holds 490 registers of a wavefront's 512: its products' results that the vector
 # unit reads in those that it can read, the rest in the others (by itself the compiler puts all results
 # into those, and copies 60 a step).
 SOURCE_FLAGS = {"tv_prompt.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
