@@ -21,8 +21,8 @@
 // is busy 1152 (the clock falls to 1.8 or 1.9 GHz meanwhile). An item costs 13 thousand cycles
 // before its first step, nine of them the queries' loads, and 6 behind its last: 32 prompts of
 // 20 to 2999 tokens 1042 us, 800 TFLOP/s. Few items are bound by the longest: four pieces behind
-// long contexts have 350 items for 256 CUs, 241 us. One short prompt: 13 us, of which the kernel
-// takes 8.
+// long contexts have 350 items for 256 CUs, 241 us. One prompt of 100 tokens: 13 us, waits for
+// queries, first keys and the other key group's part.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -777,61 +777,74 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(Pass P, int bm) {
   for (int b = tid; b < P.batch; b += kPlanThreads)
     most = max(most, clamped(ks[b + 1], 0, P.num_keys) - clamped(ks[b], 0, P.num_keys));
   atomicMax(&most_, most);
-  // Twice over all sequences: count, then place.
-  for (int pass = 0; pass < 2; ++pass) {
-    int q_from = 0, k_from = 0;           // starts that decrease count as the largest before them
+  // Over all sequences: the items' classes are counted; each item's count before it is its place
+  // in its class. Where a thread has one item at most it keeps that until the classes' places are
+  // known, else all is gone over once more (32 prompts 11.0 us, and twice 15.6; four 9.7
+  // and 12.5).
+  int total = 0, cls = 0, at = 0, q_from, k_from;
+  Item I{};
+  // the starts of sequence b0 and on, and how many items they have up to each
+  auto fetch = [&](int b0) {
+    const int b = min(b0 + tid, P.batch);   // (start b; the last one's twice or more)
+    int all;
+    const int q = larger(q_from, block_scan(clamped(P.q_start[b], 0, P.num_queries), larger, 0, part, all));
+    const int k = larger(k_from, block_scan(clamped(ks[b], 0, P.num_keys), larger, 0, part, all));
+    __syncthreads();
+    q0_[tid] = q;
+    k0_[tid] = k;
+    if (tid == kPlanThreads - 1) {
+      const int e = min(b0 + kPlanThreads, P.batch);
+      q0_[kPlanThreads] = larger(q, clamped(P.q_start[e], 0, P.num_queries));
+      k0_[kPlanThreads] = larger(k, clamped(ks[e], 0, P.num_keys));
+    }
+    __syncthreads();
+    q_from = q0_[kPlanThreads];
+    k_from = k0_[kPlanThreads];
+    const int rows = (q0_[tid + 1] - q) * P.group;
+    const int mine = b0 + tid < P.batch ? (rows + bm - 1) / bm : 0;
+    upto_[tid] = block_scan(mine, plus, 0, part, total);
+    __syncthreads();
+  };
+  auto take = [&](int i) {
+    int lo = 0, hi = kPlanThreads - 1;      // the sequence of item i: the first with upto > i
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (upto_[mid] > i) hi = mid;
+      else lo = mid + 1;
+    }
+    I.q0 = q0_[lo];
+    I.nq = q0_[lo + 1] - I.q0;
+    I.k0 = k0_[lo];
+    I.nk = k0_[lo + 1] - I.k0;
+    I.tile = i - (lo ? upto_[lo - 1] : 0);
+    const int last = min((I.tile + 1) * bm, I.nq * P.group) - 1;
+    const int keys = clamped(last / P.group + 1 + I.nk - I.nq, 0, most_);
+    cls = kClasses - 1 - static_cast<int>(static_cast<int64_t>(keys) * (kClasses - 1) / most_);
+    at = atomicAdd(&classes_[cls], 1);
+  };
+  bool once = false;
+  for (int pass = 0; pass < (once ? 1 : 2); ++pass) {
+    q_from = k_from = 0;                    // starts that decrease count as the largest before them
     for (int b0 = 0; b0 < P.batch; b0 += kPlanThreads) {
-      const int b = min(b0 + tid, P.batch);   // (start b; the last one's twice or more)
-      int all;
-      int q = larger(q_from, block_scan(clamped(P.q_start[b], 0, P.num_queries), larger, 0, part, all));
-      int k = larger(k_from, block_scan(clamped(ks[b], 0, P.num_keys), larger, 0, part, all));
-      __syncthreads();
-      q0_[tid] = q;
-      k0_[tid] = k;
-      if (tid == kPlanThreads - 1) {
-        const int e = min(b0 + kPlanThreads, P.batch);
-        q0_[kPlanThreads] = larger(q, clamped(P.q_start[e], 0, P.num_queries));
-        k0_[kPlanThreads] = larger(k, clamped(ks[e], 0, P.num_keys));
-      }
-      __syncthreads();
-      q_from = q0_[kPlanThreads];
-      k_from = k0_[kPlanThreads];
-      const int rows = (q0_[tid + 1] - q) * P.group;
-      const int mine = b0 + tid < P.batch ? (rows + bm - 1) / bm : 0;
-      int total;
-      upto_[tid] = block_scan(mine, plus, 0, part, total);
-      __syncthreads();
+      fetch(b0);
+      once = P.batch <= kPlanThreads && total <= kPlanThreads;
       for (int i = tid; i < total; i += kPlanThreads) {
-        int lo = 0, hi = kPlanThreads - 1;   // the sequence of item i: the first with upto > i
-        while (lo < hi) {
-          const int mid = (lo + hi) >> 1;
-          if (upto_[mid] > i) hi = mid;
-          else lo = mid + 1;
-        }
-        Item I{};
-        I.q0 = q0_[lo];
-        I.nq = q0_[lo + 1] - I.q0;
-        I.k0 = k0_[lo];
-        I.nk = k0_[lo + 1] - I.k0;
-        I.tile = i - (lo ? upto_[lo - 1] : 0);
-        const int last = min((I.tile + 1) * bm, I.nq * P.group) - 1;
-        const int keys = clamped(last / P.group + 1 + I.nk - I.nq, 0, most_);
-        const int cls = kClasses - 1 - static_cast<int>(static_cast<int64_t>(keys) * (kClasses - 1) / most_);
-        const int at = atomicAdd(&classes_[cls], 1);
+        take(i);
         if (pass) P.items[at] = I;
       }
       __syncthreads();
     }
     if (pass == 0) {
-      int total;
+      int count;
       const int own = classes_[tid];
-      const int upto = block_scan(own, plus, 0, part, total);
+      const int upto = block_scan(own, plus, 0, part, count);
       __syncthreads();
       classes_[tid] = upto - own;
-      if (tid == 0) *P.count = total;
+      if (tid == 0) *P.count = count;
       __syncthreads();
     }
   }
+  if (once && tid < total) P.items[classes_[cls] + at] = I;
 }
 
 // Rows of a workgroup, of which a CU holds one: 256 of them where they give every CU one, else 128 (two

@@ -188,6 +188,10 @@ def test_many_sequences():
     check(inputs(nq.tolist(), nk.tolist(), 4, 2, 32, "f16"), "f16")
 
 
+def test_more_items_than_the_plan_has_threads():
+    check(inputs([37, 3500, 700], None, 64, 1, 64))
+
+
 def test_rows_of_no_sequence():
     """Garbage before the first and behind the last sequence reaches none, and its outputs stay."""
     call = inputs([20, 75], None, 4, 2, 64, before=3, behind=40)
