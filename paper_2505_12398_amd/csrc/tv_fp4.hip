@@ -130,29 +130,30 @@ __global__ void __launch_bounds__(kThreads) commit_kernel(tv::Fp4CommitArgs a) {
 template <class T>
 __global__ void __launch_bounds__(kThreads) read_kernel(tv::Fp4ReadArgs a) {
   __shared__ int64_t froms[kRows];        // a row's page
-  __shared__ int rows[kRows];             // and which row of it, -1 for none, -2 for a row that is passed over
-  const int b = blockIdx.x, layer = blockIdx.y, all = a.length[b], tid = threadIdx.x;
+  __shared__ int rows[kRows];             // and which row of it, -1 for none
+  const int b = blockIdx.x, layer = blockIdx.y, tid = threadIdx.x;
   const int shift = 31 - __builtin_clz(a.page_size);
   const int per_head = a.head_dim / 8, per = per_head * a.kv_heads, row_bytes = a.head_dim / 2;
   const int blocks = a.head_dim / TV_FP4_BLOCK, exps = a.page_size * row_bytes;
   const int64_t head_bytes = exps + a.page_size * blocks;
   const int first = a.first ? a.first[b] : 0, start = a.row_start[b];
+  // the positions whose rows the outputs have (a length may be far beyond them)
+  const int64_t from = max(-static_cast<int64_t>(start), int64_t{0});
+  const int64_t all = min(static_cast<int64_t>(a.length[b]), static_cast<int64_t>(a.num_rows) - start);
   const uint8_t* src[2] = {static_cast<const uint8_t*>(a.k_cache), static_cast<const uint8_t*>(a.v_cache)};
   uint16_t* dst[2] = {static_cast<uint16_t*>(a.k_out), static_cast<uint16_t*>(a.v_out)};
   const Spread S = spread(per);
-  for (int64_t k0 = static_cast<int64_t>(blockIdx.z) * kRows; k0 < all;
+  for (int64_t k0 = from + static_cast<int64_t>(blockIdx.z) * kRows; k0 < all;
        k0 += static_cast<int64_t>(gridDim.z) * kRows) {
     const int n = static_cast<int>(min<int64_t>(all - k0, kRows));
     __syncthreads();                      // (the rows before are written)
     if (tid < n) {
-      const int64_t x = first + k0 + tid, to_row = start + k0 + tid;
+      const int64_t x = first + k0 + tid;
       int page = -1;
       if (x >= 0 && x >> shift < a.table_width)
         page = a.block_table[static_cast<size_t>(b) * a.table_width + (x >> shift)];
       froms[tid] = layer * a.cache_layer_stride + page * a.page_stride;
-      rows[tid] = to_row < 0 || to_row >= a.num_rows ? -2
-                  : page < 0 || page >= a.num_pages  ? -1
-                                                     : static_cast<int>(x & (a.page_size - 1));
+      rows[tid] = page < 0 || page >= a.num_pages ? -1 : static_cast<int>(x & (a.page_size - 1));
     }
     __syncthreads();
     for (int w = S.w; w < per; w += S.w_step) {
@@ -165,7 +166,7 @@ __global__ void __launch_bounds__(kThreads) read_kernel(tv::Fp4ReadArgs a) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
           const int r = r0 + u * S.r_step;
-          row[u] = r < n ? rows[r] : -2;
+          row[u] = r < n ? rows[r] : -1;
           q[u][0] = q[u][1] = 0;
           e[u][0] = e[u][1] = 255;
           if (row[u] < 0) continue;
@@ -178,7 +179,7 @@ __global__ void __launch_bounds__(kThreads) read_kernel(tv::Fp4ReadArgs a) {
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-          if (row[u] == -2) continue;
+          if (r0 + u * S.r_step >= n) continue;
           const int64_t t = to + (r0 + u * S.r_step) * a.row_stride;
 #pragma unroll
           for (int c = 0; c < 2; ++c) {

@@ -197,6 +197,28 @@ def test_many_rows_of_long_requests():
     assert torch.equal(k2, k) and torch.equal(v2, v)
 
 
+def test_lengths_far_beyond_the_outputs():
+    """Positions whose rows the outputs do not have cost nothing, however many: the rows there are hold
+    theirs, NaN behind the table."""
+    ps, KH, dim, rows, most = 16, 2, 64, 100, 2 ** 31 - 1
+    rng = np.random.default_rng(8)
+    cache = rng.integers(0, 255, (2, 2) + tv.fp4_cache_shape(5, KH, ps, dim)).astype(np.uint8)
+    kc, vc = (torch.as_tensor(c, device=DEV) for c in cache)
+    table = np.array([[3, 1, 4]])
+    # (and the call without what the outputs do not have)
+    for first, start, as_first, as_start in ((0, 0, 0, 0), (7, 40, 7, 40), (5, -20, 25, 0),
+                                             (0, -2 ** 30, 2 ** 30, 0), (-3, 99, -3, 99),
+                                             (most, 90, most, 90), (0, 100, 0, 100), (0, most, 0, 100),
+                                             (0, -2 ** 31, 0, 100)):
+        out = tuple(torch.full((2, rows, KH, dim), 5.0, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        tv.cache_read_fp4(kc, vc, ps, i32(table), i32([most]), i32([start]), rows, first=i32([first]), out=out)
+        for got, c in zip(out, cache):
+            want = D.cache_read_fp4(c, ps, dim, table, [as_first], [rows - as_start], [as_start],
+                                    np.full((2, rows, KH, dim), 5.0))
+            want = torch.tensor(want).to(torch.bfloat16).double().numpy()
+            np.testing.assert_array_equal(got.double().cpu().numpy(), want, err_msg=f"{first} {start}")
+
+
 def test_write_and_read_captured_and_replayed():
     ps, KH, dim = 16, 2, 64
     g = torch.Generator(device=DEV).manual_seed(4)
