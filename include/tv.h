@@ -552,8 +552,8 @@ int tv_cache_commit(int32_t layers, int32_t batch, int32_t num_nodes, int32_t kv
  * which depend on num_queries and batch; the same call gives the same bits.
  *
  * head_dim: a multiple of 8 up to TV_MAX_HEAD_DIM; heads a multiple of kv_heads; heads * head_dim at
- * most TV_MAX_HIDDEN; num_queries * heads below 2^29 and batch * kv_heads below 2^22; kv_stride at
- * most 2^24; scale as for tv_tree_attention; q, k, v and out 16-byte aligned, strides multiples of 8.
+ * most TV_MAX_HIDDEN; num_queries * heads below 2^29, num_keys at most 2^31 - 1024 and batch * kv_heads
+ * below 2^22; kv_stride at most 2^24; scale as for tv_tree_attention; q, k, v and out 16-byte aligned, strides multiples of 8.
  * out dtype [num_queries][heads][head_dim], apart from all inputs; rows of no sequence are left as
  * they were. workspace: tv_prompt_attention_workspace_size() bytes (0 for invalid sizes), 256-byte
  * aligned. Nothing is allocated. Returns a tv_status_t; argument errors launch nothing.

@@ -244,13 +244,17 @@ int validate(const tv::Fp4ReadArgs& a) {
   return TV_OK;
 }
 
+// Keys of a prompt attention: the kernel's tiles of 32 keys, rounded up and a few further ones
+// of idle key groups, end below 2^31.
+constexpr int32_t kMaxKeys = INT32_MAX - 1023;
+
 // TV_OK if a prompt attention of these sizes is taken
 int prompt_sizes(int32_t batch, int32_t num_queries, int32_t num_keys, int32_t heads,
                  int32_t kv_heads, int32_t head_dim) {
   if (batch < 0 || num_queries < 0 || num_keys < 0 || heads < 1 || kv_heads < 1 || head_dim < 1)
     return TV_ERR_INVALID_ARG;
   if (heads % kv_heads) return TV_ERR_INVALID_ARG;
-  if (batch > TV_MAX_BATCH || head_dim > TV_MAX_HEAD_DIM || head_dim % 8 ||
+  if (batch > TV_MAX_BATCH || head_dim > TV_MAX_HEAD_DIM || head_dim % 8 || num_keys > kMaxKeys ||
       static_cast<int64_t>(heads) * head_dim > TV_MAX_HIDDEN ||
       static_cast<int64_t>(num_queries) * heads >= int64_t{1} << 29 ||
       static_cast<int64_t>(batch) * kv_heads >= int64_t{1} << 22)

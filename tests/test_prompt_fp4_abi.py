@@ -53,6 +53,20 @@ def test_prompt_empty_calls_and_workspace_size():
     assert size(1, 5, 5, 8, 2, 64) > 0 and size(300, 100000, 100000, 32, 8, 128) % 256 == 0
 
 
+def test_prompt_keys_that_32_bits_cannot_count():
+    """The kernel rounds a sequence's keys up to whole tiles of 32, and counts on for the key groups
+    that have none: of 2^31 - 31 keys and more the count was negative, and the outputs NaN."""
+    size = tv.tv_prompt_attention_workspace_size
+    most = 2 ** 31 - 1024
+    for dim in (8, 64, 128):
+        assert size(2, 50, most, 8, 2, dim) == size(2, 50, 70, 8, 2, dim) > 0
+        for n in (most + 1, 2 ** 31 - 31, 2 ** 31 - 1):
+            assert size(2, 50, n, 8, 2, dim) == 0
+            assert call_prompt(num_keys=n, head_dim=dim, q_stride=8 * dim, kv_stride=2 * dim) == UNS
+    # the tiles counted of the most keys, of four key groups, and as many again that are loaded ahead
+    assert (-(-most // 32) + 4 + 4 * 5) * 32 + 64 <= 2 ** 31 - 1
+
+
 def call_commit(**kw):
     args = dict(layers=2, batch=2, num_nodes=5, kv_heads=2, head_dim=64, dtype=tv.TV_DTYPE_BF16,
                 k_new=A, v_new=A, new_layer_stride=1 << 16, node_stride=128, k_cache=A, v_cache=A,
