@@ -602,8 +602,9 @@ int tv_cache_commit_fp4(int32_t layers, int32_t batch, int32_t num_nodes, int32_
  * rows row_stride, each [kv_heads][head_dim], in elements and multiples of 8. Positions that the block
  * table int32 [batch][table_width] does not hold, and those on pages outside [0, num_pages), are NaN;
  * rows outside [0, num_rows) are passed over, and all other rows left as they were. The rows of a call
- * must differ. Caches as for tv_cache_commit_fp4. No workspace; nothing is allocated. Returns a
- * tv_status_t; argument errors launch nothing.
+ * must differ, and no two of the num_rows of all layers of k_out and v_out may share bytes (but for one
+ * buffer as both, where the caches are one, too). Caches as for tv_cache_commit_fp4. No workspace;
+ * nothing is allocated. Returns a tv_status_t; argument errors launch nothing.
  */
 int tv_cache_read_fp4(int32_t layers, int32_t batch, int32_t kv_heads, int32_t head_dim, int32_t dtype,
                       const void* k_cache, const void* v_cache, int64_t cache_layer_stride,

@@ -145,20 +145,43 @@ int validate(const tv::ExtendArgs& a) {
   return TV_OK;
 }
 
+using Wide = __int128;
+Wide magnitude(int64_t x) { return x < 0 ? -static_cast<Wide>(x) : static_cast<Wide>(x); }
+
+// Whether blocks of `size` that begin at multiples of `step` (no less) up to `last` share bytes with
+// as many that begin `at` (0 or more) further on.
+bool meets(Wide at, Wide step, Wide last, Wide size) {
+  // the first one of those: behind a block's end, and before the next one's start
+  const Wide block = at / step * step;
+  return (block <= last && at - block < size) || (block + step <= last && block + step - at < size);
+}
+
 // Whether pages of two layers share bytes: layers begin cache_layer_stride apart, and a
 // layer's pages of `size` bytes page_stride (no less).
 template <class Args>
 bool layers_overlap(const Args& a, int64_t size) {
-  using Wide = __int128;
-  const Wide apart = a.cache_layer_stride < 0 ? -static_cast<Wide>(a.cache_layer_stride)
-                                              : static_cast<Wide>(a.cache_layer_stride);
+  const Wide apart = magnitude(a.cache_layer_stride);
   const Wide step = a.page_stride, last = (a.num_pages - 1) * step;   // the last page
   if (a.layers < 2 || apart >= last + size) return false;
-  for (int l = 1; l < a.layers; ++l) {
-    // the first page of the layer l on: behind a page's end, and before the next one's start
-    const Wide at = l * apart, page = at / step * step;
-    if (page <= last && at - page < size) return true;
-    if (page + step <= last && page + step - at < size) return true;
+  for (int l = 1; l < a.layers; ++l)
+    if (meets(l * apart, step, last, size)) return true;
+  return false;
+}
+
+// The same of the rows that a read writes: of two layers, or of the keys and the values.
+bool outputs_overlap(const tv::Fp4ReadArgs& a) {
+  const Wide apart = magnitude(a.out_layer_stride) * 2, size = Wide{a.kv_heads} * a.head_dim * 2;
+  const Wide step = Wide{a.row_stride} * 2, last = (a.num_rows - 1) * step;
+  const bool one = a.layers < 2 || apart >= last + size;
+  for (int l = 1; l < a.layers && !one; ++l)
+    if (meets(l * apart, step, last, size)) return true;
+  // (both of the same cache to the same rows: the same bytes)
+  if (a.k_out == a.v_out) return a.k_cache != a.v_cache;
+  const Wide from = static_cast<Wide>(bits(a.v_out)) - static_cast<Wide>(bits(a.k_out));
+  if ((from < 0 ? -from : from) >= (a.layers - 1) * apart + last + size) return false;
+  for (int l = 1 - a.layers; l < a.layers; ++l) {
+    const Wide at = from + l * apart;
+    if (meets(at < 0 ? -at : at, step, last, size)) return true;
   }
   return false;
 }
@@ -241,7 +264,7 @@ int validate(const tv::Fp4ReadArgs& a) {
     if (bits(p) % 16) return TV_ERR_INVALID_ARG;
   for (const int32_t* p : {a.block_table, a.first, a.length, a.row_start})
     if (bits(p) % 4) return TV_ERR_INVALID_ARG;
-  return TV_OK;
+  return outputs_overlap(a) ? TV_ERR_INVALID_ARG : TV_OK;
 }
 
 // Keys of a prompt attention: the kernel's tiles of 32 keys, rounded up and a few further ones

@@ -197,6 +197,38 @@ def test_many_rows_of_long_requests():
     assert torch.equal(k2, k) and torch.equal(v2, v)
 
 
+@pytest.mark.parametrize("order", ["kv first", "layers in a row", "rows first, layers backwards", "one"])
+def test_outputs_between_each_other(order):
+    """Rows of all layers, of keys and values, in one buffer; one buffer as both for one cache as both."""
+    ps, KH, dim, L, rows = 16, 2, 64, 3, 21
+    rng = np.random.default_rng(6)
+    cache = rng.integers(0, 250, (2, L) + tv.fp4_cache_shape(3, KH, ps, dim)).astype(np.uint8)
+    kc, vc = (torch.as_tensor(c, device=DEV) for c in cache)
+    args = (ps, i32([[2, 0]]), i32([rows]), i32([0]), rows)
+    want = tv.cache_read_fp4(kc, vc, *args)
+    if order == "one":
+        got = tv.cache_read_fp4(kc, kc, *args, out=(want[1], want[1]))
+        assert torch.equal(got[0], want[0])
+        return
+    if order == "kv first":
+        k, v = torch.zeros((2, L, rows, KH, dim), dtype=torch.bfloat16, device=DEV)
+    elif order == "layers in a row":
+        buf = torch.zeros((rows, 2, L, KH, dim), dtype=torch.bfloat16, device=DEV)
+        k, v = buf[:, 0].transpose(0, 1), buf[:, 1].transpose(0, 1)
+    else:
+        buf = torch.zeros((L, rows, 2, KH, dim), dtype=torch.bfloat16, device=DEV)
+        k, v = buf[:, :, 1], buf[:, :, 0]
+    if "backwards" in order:                 # (torch has no negative strides: through the C-ABI)
+        st = tv.tv_cache_read_fp4(L, 1, KH, dim, tv.TV_DTYPE_BF16, kc, vc, kc.stride(0), kc.stride(1), 3, *args[:2],
+                                  2, None, args[2], args[3], rows, k[L - 1].data_ptr(), v[L - 1].data_ptr(),
+                                  -k.stride(0), k.stride(1), torch.cuda.current_stream().cuda_stream)
+        assert st == tv.TV_OK
+        k, v = k.flip(0), v.flip(0)
+    else:
+        tv.cache_read_fp4(kc, vc, *args, out=(k, v))
+    assert torch.equal(k, want[0]) and torch.equal(v, want[1])
+
+
 def test_lengths_far_beyond_the_outputs():
     """Positions whose rows the outputs do not have cost nothing, however many: the rows there are hold
     theirs, NaN behind the table."""

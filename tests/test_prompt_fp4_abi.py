@@ -133,6 +133,40 @@ def test_read_empty_calls(kw):
     assert call_read(**kw, length=None, k_out=None, block_table=None) == tv.TV_OK
 
 
+def rows_meet(layers, layer, rows, row, size, at):
+    """Whether two rows of ``size`` bytes of k_out at 0 and v_out at ``at`` share bytes."""
+    begins = sorted(a + x * layer + r * row for a in (0, at) for x in range(layers) for r in range(rows))
+    return any(b - a < size for a, b in zip(begins, begins[1:]))
+
+
+# (strides in elements, ``at`` the bytes from k_out to v_out)
+OVERLAPS = [dict(out_layer_stride=0), dict(out_layer_stride=8), dict(out_layer_stride=99 * 128),
+            dict(out_layer_stride=-1024), dict(out_layer_stride=120, row_stride=256),
+            dict(out_layer_stride=136, row_stride=256),
+            dict(out_layer_stride=128, row_stride=256, layers=3),
+            dict(at=16), dict(at=240), dict(at=-240), dict(at=99 * 256), dict(at=128, layers=1, num_rows=3),
+            dict(at=(1 << 17) + 99 * 256), dict(at=-(1 << 17)),
+            dict(at=512, out_layer_stride=128, row_stride=512, layers=3),
+            dict(at=240, out_layer_stride=512 * 100, row_stride=256)]
+
+
+@pytest.mark.parametrize("kw", OVERLAPS)
+def test_read_refuses_outputs_that_overlap(kw):
+    """Layers, or keys and values, whose rows share bytes were written in any order."""
+    kw = dict(kw)
+    at = kw.pop("at", 1 << 22)
+    size = 2 * 2 * 64
+    full = dict(layers=2, out_layer_stride=1 << 16, row_stride=128, num_rows=100)
+    full.update(kw)
+    assert rows_meet(full["layers"], 2 * full["out_layer_stride"], full["num_rows"], 2 * full["row_stride"],
+                     size, at)
+    assert call_read(**kw, k_out=WS, v_out=WS + at) == BAD
+
+
+def test_read_refuses_one_output_for_two_caches():
+    assert call_read(k_cache=A, v_cache=A + 16) == BAD
+
+
 def call_attention(**kw):
     args = dict(batch=2, num_nodes=5, heads=8, kv_heads=2, head_dim=64, dtype=tv.TV_DTYPE_BF16,
                 parents=A, q=A, q_stride=512, k_new=A, v_new=A, kv_stride=128, k_cache=A,
