@@ -937,8 +937,8 @@ def cache_read_fp4(k_cache, v_cache, page_size, block_table, length, row_start, 
     """Positions first[b] .. first[b] + length[b] - 1 of every request (``first`` None: from 0) out of
     a cache of 4 bits [layers, pages, kv_heads, bytes] into rows row_start[b] .. of two tensors
     [layers, ``rows``, kv_heads, D] (``tv_cache_read_fp4``; int32 tensors [B], block_table
-    [B, width]): new ones of ``dtype`` (bfloat16 by default), or ``out`` = (k, v), whose rows may
-    lie apart. Returns them; rows that no request names are left as they were (new tensors hold
+    [B, width]): new ones of ``dtype`` (bfloat16 by default), or ``out`` = (k, v) (of ``dtype`` if
+    that is given), whose rows may lie apart. Returns them; rows that no request names are left as they were (new tensors hold
     nothing there). Raises on a non-OK return."""
     import torch
     dev, i32 = k_cache.device, torch.int32
@@ -957,6 +957,8 @@ def cache_read_fp4(k_cache, v_cache, page_size, block_table, length, row_start, 
             out = tuple(torch.empty((L, rows, KH, D), dtype=dtype, device=dev) for _ in range(2))
         k, v = out
         dt = k.dtype
+        if dtype is not None and dtype != dt:
+            raise TypeError(f"out is of {dt}, not of {dtype}")
         code = _code16("k", dt)
         if k.dim() != 4 or v.dim() != 4 or k.shape[0] != L or v.shape[0] != L:
             raise ValueError(f"the outputs have four dimensions and {L} layers")

@@ -293,6 +293,17 @@ def test_cache_binding_checks():
     assert tv.cache_read_fp4(**dict(args, rows=0))[0].shape == (2, 0, 2, 32)
 
 
+def test_read_into_outputs_of_another_type():
+    c = torch.zeros((2,) + tv.fp4_cache_shape(5, 2, 16, 32), dtype=torch.uint8)
+    n = torch.ones(3, **I32)
+    for dt, other in ((BF, torch.float16), (torch.float16, BF)):
+        out = tuple(torch.zeros(2, 0, 2, 32, dtype=dt) for _ in range(2))
+        args = (c, c.clone(), 16, torch.zeros(3, 2, **I32), n, n, 0)
+        assert tv.cache_read_fp4(*args, out=out) is out and tv.cache_read_fp4(*args, dtype=dt, out=out) is out
+        with pytest.raises(TypeError):
+            tv.cache_read_fp4(*args, dtype=other, out=out)
+
+
 def test_empty_calls_on_tensors_that_are_not_on_a_gpu():
     a = prompt_tensors()
     assert tv.prompt_attention(**dict(a, q_start=a["q_start"][:1])).shape == (9, 4, 32)
