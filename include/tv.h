@@ -391,8 +391,8 @@ int tv_commit_paths(int32_t batch, int32_t num_nodes, const int32_t* parents,
  * with a shorter context is computed from its own entries alone.
  *
  * A tree whose block table names a page outside [0, num_pages) for a position
- * below ctx_len, or whose ctx_len exceeds table_width * page_size, gets NaN in
- * every output. The order of a tree's sums, and so its last bits, depends on the
+ * below ctx_len, or whose ctx_len exceeds table_width * page_size or 2^31 - 1024,
+ * gets NaN in every output. The order of a tree's sums, and so its last bits, depends on the
  * lengths of all trees of the call, and on nothing else of the others; the same
  * call gives the same bits.
  *
