@@ -584,7 +584,8 @@ size_t tv_fp4_page_bytes(int32_t page_size, int32_t head_dim);
  * above, ties to the even code, beyond 6 to 6. A block with an element that is not finite is NaN.
  * dtype (TV_DTYPE_BF16 or TV_DTYPE_F16) is that of k_new and v_new, whose strides are in elements and
  * multiples of 8; the caches' strides are in bytes and multiples of 16, pages page_stride apart, each
- * [kv_heads][tv_fp4_page_bytes()]. No two layers' pages may share bytes. Pointers 16-byte aligned. No
+ * [kv_heads][tv_fp4_page_bytes()]. No two layers' pages may share bytes, nor the slots' rows of the two
+ * caches (but for one buffer as both, where k_new and v_new are one, too). Pointers 16-byte aligned. No
  * workspace; nothing is allocated. Returns a tv_status_t; argument errors launch nothing.
  */
 int tv_cache_commit_fp4(int32_t layers, int32_t batch, int32_t num_nodes, int32_t kv_heads,

@@ -245,7 +245,8 @@ int validate(const tv::Fp4CommitArgs& a) {
     if (bits(p) % 16) return TV_ERR_INVALID_ARG;
   for (const int32_t* p : {a.new_len, a.slots, a.path_nodes})
     if (bits(p) % 4) return TV_ERR_INVALID_ARG;
-  return TV_OK;
+  // (of keys and values to the same places either could stay)
+  return a.k_cache == a.v_cache && a.k_new != a.v_new ? TV_ERR_INVALID_ARG : TV_OK;
 }
 
 int validate(const tv::Fp4ReadArgs& a) {

@@ -97,6 +97,13 @@ def test_commit_refusals(kw, want):
     assert call_commit(**kw) == want
 
 
+def test_commit_refuses_one_cache_for_keys_and_values():
+    """Every row would be written twice, in any order."""
+    assert call_commit(v_new=A + (1 << 20)) == BAD
+    for none in (dict(layers=0), dict(batch=0), dict(max_new=0), dict(num_pages=0)):
+        assert call_commit(v_new=A + (1 << 20), **none) == tv.TV_OK
+
+
 @pytest.mark.parametrize("kw", [dict(layers=0), dict(batch=0), dict(max_new=0), dict(num_pages=0)])
 def test_commit_empty_calls(kw):
     assert call_commit(**kw, k_new=None, new_len=None, slots=None) == tv.TV_OK
