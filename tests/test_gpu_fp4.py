@@ -68,6 +68,40 @@ def test_commit(layers, batch, n1, heads, dim, ps, dtype):
             np.testing.assert_array_equal(got.cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("heads,dim,dtype", [(16, 128, "bf16"), (16, 128, "f16"), (32, 128, "bf16"),
+                                             (24, 96, "f16"), (24, 96, "bf16"), (5, 96, "f16"), (40, 64, "bf16")])
+def test_wide_rows(heads, dim, dtype):
+    """Rows of 256 pieces of eight and more, of which threads have several, numbers of pieces that 256 is
+    no multiple of, and more rows than a workgroup takes at a time: written, with nodes, slots and pages
+    that are none, and read back from any place."""
+    ps, pages, B, n1, most = 16, 4, 2, 13, 15
+    new, cache, rng = commit_inputs(1, B, n1, heads, dim, ps, pages, dtype, seed=3)
+    path = rng.integers(-1, n1 + 1, (B, most - 1))
+    slots = np.stack(np.array_split(rng.permutation(pages * ps)[:B * most], B))
+    slots[0, 4], slots[1, 9], slots[1, 2] = -1, pages * ps, -2 ** 31
+    n = [most + 3, 11]
+    kc, vc = (torch.as_tensor(c, device=DEV) for c in cache)
+    tv.cache_commit_fp4(new[0].to(DEV), new[1].to(DEV), kc, vc, ps, i32(n), i32(slots), path_nodes=i32(path))
+    held = [D.cache_commit_fp4(x.double().numpy(), c, ps, n, slots, path, largest(dtype))
+            for x, c in zip(new, cache)]
+    for got, want in zip((kc, vc), held):
+        np.testing.assert_array_equal(got.cpu().numpy(), want)
+    table, first, length, start = np.array([[2, -1, 0], [3, 1, pages]]), [5, 0], [30, 41], [3, 40]
+    rows = 79                                # (of the second the last two are behind it)
+    at = cache.shape[-1] // 17 * 16
+    if dtype == "f16":                       # exponents around those fp16 holds, where others were
+        held = [c.copy() for c in held]
+        for c in held:
+            c[..., at:] = np.where(c[..., at:] == 255, 255, 100 + c[..., at:] % 41)
+        kc, vc = (torch.as_tensor(c, device=DEV) for c in held)
+    out = tuple(torch.full((1, rows, heads, dim), 7.0, dtype=TYPES[dtype], device=DEV) for _ in range(2))
+    tv.cache_read_fp4(kc, vc, ps, i32(table), i32(length), i32(start), rows, first=i32(first), out=out)
+    for got, c in zip(out, held):
+        want = D.cache_read_fp4(c, ps, dim, table, first, length, start, np.full((1, rows, heads, dim), 7.0))
+        want = torch.tensor(want).to(TYPES[dtype]).double().numpy()
+        np.testing.assert_array_equal(got.double().cpu().numpy(), want)
+
+
 def special_blocks(dtype):
     """Ties, zeros of both signs, numbers below the normal ones, the largest ones, blocks around the
     borders of their exponent, and blocks with a number that is not finite."""
@@ -227,6 +261,31 @@ def test_outputs_between_each_other(order):
     else:
         tv.cache_read_fp4(kc, vc, *args, out=(k, v))
     assert torch.equal(k, want[0]) and torch.equal(v, want[1])
+
+
+def test_widest_rows():
+    """512 heads of 128, the most there are, against a table lookup of all bytes, and back again."""
+    ps, KH, dim, n = 16, 512, 128, 20
+    g = torch.Generator(device=DEV).manual_seed(5)
+    cache = torch.randint(0, 256, (2, 1) + tv.fp4_cache_shape(2, KH, ps, dim), dtype=torch.uint8, generator=g,
+                          device=DEV)
+    at = cache.shape[-1] // 17 * 16
+    cache[..., at:] = 120 + cache[..., at:] % 16
+    table = i32([[1, 0]])
+    k, v = tv.cache_read_fp4(cache[0], cache[1], ps, table, i32([n]), i32([0]), n)
+    values = torch.tensor(D.FP4_VALUES + tuple(-x for x in D.FP4_VALUES), device=DEV)
+    for x, c in ((k, cache[0, 0]), (v, cache[1, 0])):
+        code = torch.stack([c[..., :at] & 15, c[..., :at] >> 4], -1).flatten(-2).int()
+        rows = values[code].view(2, KH, ps, dim // 32, 32) * \
+            torch.exp2(c[..., at:].float() - 127).view(2, KH, ps, dim // 32, 1)
+        want = rows.flatten(-2).to(torch.bfloat16)[[1, 0]].transpose(1, 2).reshape(-1, KH, dim)[:n]
+        assert torch.equal(x[0], want)
+    # values of the grid keep theirs, though not always their exponent
+    other = torch.zeros_like(cache)
+    slots = (16 * (1 - torch.arange(n, device=DEV) // 16) + torch.arange(n, device=DEV) % 16).int()[None]
+    tv.cache_commit_fp4(k[:, None], v[:, None], other[0], other[1], ps, i32([n]), slots)
+    k2, v2 = tv.cache_read_fp4(other[0], other[1], ps, table, i32([n]), i32([0]), n)
+    assert torch.equal(k2, k) and torch.equal(v2, v)
 
 
 def test_lengths_far_beyond_the_outputs():
