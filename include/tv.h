@@ -578,10 +578,13 @@ int tv_prompt_attention(int32_t batch, int32_t num_queries, int32_t num_keys, in
 size_t tv_fp4_page_bytes(int32_t page_size, int32_t head_dim);
 
 /*
- * tv_cache_commit into a cache of 4 bits: the same rows to the same slots. The exponent of a block is
- * the least with amax <= 7 * 2^(e - 127), amax its largest magnitude, and at least 1 and at most 252 (from
- * fp16 140), so that it reads back as finite numbers; elements are rounded to the nearest of the values
- * above, ties to the even code, beyond 6 to 6. A block with an element that is not finite is NaN.
+ * tv_cache_commit into a cache of 4 bits: the same rows to the same slots. Packed prompts, as
+ * tv_prompt_attention takes them, are one request (batch 1, path_nodes NULL): num_nodes, new_len and
+ * max_new are the number of their rows (TV_MAX_NEW at most), slots those of all prompts in the rows'
+ * order. The exponent of a block is the least with amax <= 7 * 2^(e - 127), amax its largest magnitude,
+ * and at least 1 and at most 252 (from fp16 140), so that it reads back as finite numbers; elements are
+ * rounded to the nearest of the values above, ties to the even code, beyond 6 to 6. A block with an
+ * element that is not finite is NaN.
  * dtype (TV_DTYPE_BF16 or TV_DTYPE_F16) is that of k_new and v_new, whose strides are in elements and
  * multiples of 8; the caches' strides are in bytes and multiples of 16, pages page_stride apart, each
  * [kv_heads][tv_fp4_page_bytes()]. No two layers' pages may share bytes, nor the slots' rows of the two

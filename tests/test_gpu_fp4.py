@@ -693,6 +693,47 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(far, want) and bool(far.isfinite().all())
 
 
+# --- a prompt's packed rows ---------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_packed_prompts_without_a_copy(dtype):
+    """Prompts as tv_prompt_attention takes them, packed one behind the other in a projection's output, are
+    one request of the commit: its nodes the rows, their slots those of all prompts in that order. The
+    same cache as that of one request a prompt, rows of no prompt written nowhere."""
+    H, KH, dim, ps, pages, n, before = 4, 2, 64, 16, 12, [40, 1, 0, 33, 17], 3
+    B, T = len(n), sum(n)
+    g = torch.Generator(device=DEV).manual_seed(2)
+    qkv = torch.randn((before + T + 4, H + 2 * KH, dim), generator=g, device=DEV).to(TYPES[dtype])
+    k, v = qkv[:, H:H + KH], qkv[:, H + KH:]
+    q_start = before + np.concatenate([[0], np.cumsum(n)])
+    out = tv.prompt_attention(qkv[:, :H], k, v, i32(q_start), 0.125)
+    assert bool(out[before:before + T].isfinite().all())
+    table = torch.full((B, 3), -1, dtype=torch.int32, device=DEV)
+    free = i32(np.random.default_rng(1).permutation(pages))
+    grown = tv.cache_extend(i32(n), i32([0] * B), table, free, i32([pages]), ps, max(n))
+    assert not grown.status.any()
+    prompt = torch.as_tensor(np.repeat(np.arange(B), n), device=DEV)        # of every row, and which of it
+    row = torch.as_tensor(np.concatenate([np.arange(x) for x in n]), device=DEV)
+    empty = torch.zeros((2, 1) + tv.fp4_cache_shape(pages, KH, ps, dim), dtype=torch.uint8, device=DEV)
+    packed, apart = empty.clone(), empty.clone()
+    slots = grown.slots[prompt, row][None]
+    rows = slice(before, before + T)
+    tv.cache_commit_fp4(k[rows][None, None], v[rows][None, None], packed[0], packed[1], ps, i32([T]), slots)
+    k_pad, v_pad = (torch.zeros((1, B, max(n), KH, dim), dtype=TYPES[dtype], device=DEV) for _ in range(2))
+    k_pad[0, prompt, row], v_pad[0, prompt, row] = k[rows], v[rows]
+    tv.cache_commit_fp4(k_pad, v_pad, apart[0], apart[1], ps, i32(n), grown.slots)
+    assert torch.equal(packed, apart) and int((packed != 0).flatten(2).any(-1).sum()) > 0
+    back = tv.cache_read_fp4(packed[0], packed[1], ps, table, grown.seq_len, i32(q_start[:-1] - before), T,
+                             dtype=TYPES[dtype])
+    for got, x in zip(back, (k[rows], v[rows])):
+        want = np.empty((T, KH, dim))
+        for at in np.ndindex(T, KH):
+            for i in range(0, dim, 32):
+                want[at][i:i + 32] = D.fp4_values(*D.fp4_encode(x[at][i:i + 32].double().cpu().numpy(), largest(dtype)))
+        np.testing.assert_array_equal(got[0].double().cpu().numpy(), want)
+
+
 # --- a request's life --------------------------------------------------------
 
 

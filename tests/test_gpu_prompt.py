@@ -2,6 +2,10 @@
 earlier keys, more queries than keys, grouped heads, odd head sizes, strides, garbage in places
 that a query does not see (needs an MI355X)."""
 
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -355,6 +359,48 @@ def test_captured_and_replayed():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want), at
+
+
+def test_no_keys_at_all():
+    """Queries without any key are zeros, whatever the sequences."""
+    q = torch.randn((90, 4, 64), device=DEV).to(torch.bfloat16)
+    none = torch.empty((0, 2, 64), dtype=torch.bfloat16, device=DEV)
+    for at in ([0, 90], [0, 33, 33, 90]):
+        q_start = torch.tensor(at, dtype=torch.int32, device=DEV)
+        got = tv.prompt_attention(q, none, none, q_start, 0.125, k_start=torch.zeros_like(q_start))
+        assert not got.any()
+
+
+def test_first_launch_by_a_graph():
+    """The kernel's stack is the runtime's, reserved at a stream's first launch of it: a process whose
+    first launch is a graph's replay, on the path that uses the stack, too."""
+    code = '''
+import torch, paper_2505_12398_amd as tv
+g = torch.Generator(device="cuda").manual_seed(1)
+qkv = torch.randn((900, 12, 128), generator=g, device="cuda").to(torch.bfloat16)
+q, k, v = qkv[:, :8], qkv[:, 8:10], qkv[:, 10:]
+v[500, :, 7] = float("inf")
+at = torch.tensor([0, 900], dtype=torch.int32, device="cuda")
+out = torch.zeros((900, 8, 128), dtype=torch.bfloat16, device="cuda")
+ws = torch.empty(tv.tv_prompt_attention_workspace_size(1, 900, 900, 8, 2, 128), dtype=torch.uint8, device="cuda")
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    tv.prompt_attention(q, k, v, at, 0.09, out=out, workspace=ws)
+got = []
+for _ in range(3):
+    out.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    got.append(out.clone())
+want = tv.prompt_attention(q, k, v, at, 0.09)
+assert bool((want[500:, :, 7] == float("inf")).all()) and bool(want[:500].isfinite().all())
+assert all(torch.equal(x, want) for x in got)
+print("equal")
+'''
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    run = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=100)
+    assert run.returncode == 0 and "equal" in run.stdout, run.stderr[-2000:]
 
 
 def test_offsets_beyond_32_bits():
