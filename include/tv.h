@@ -391,14 +391,15 @@ int tv_commit_paths(int32_t batch, int32_t num_nodes, const int32_t* parents,
  * with a shorter context is computed from its own entries alone.
  *
  * A tree whose block table names a page outside [0, num_pages) for a position
- * below ctx_len, or whose ctx_len exceeds table_width * page_size or 2^31 - 1024,
- * gets NaN in every output. The order of a tree's sums, and so its last bits, depends on the
+ * below ctx_len, or whose ctx_len exceeds table_width * page_size, gets NaN in
+ * every output. The order of a tree's sums, and so its last bits, depends on the
  * lengths of all trees of the call, and on nothing else of the others; the same
  * call gives the same bits.
  *
  * head_dim: a multiple of 8 up to TV_MAX_HEAD_DIM; heads a multiple of
  * kv_heads; heads * head_dim at most TV_MAX_HIDDEN; page_size a power of two
- * from TV_MIN_PAGE to TV_MAX_PAGE; scale positive and at most 2^127, scores s
+ * from TV_MIN_PAGE to TV_MAX_PAGE; table_width * page_size at most 2^31 - 1024;
+ * scale positive and at most 2^127, scores s
  * of up to 2^22 either way (beyond them an fp32 exponent does not tell weights
  * apart, and a row may be NaN); q, k_new, v_new, caches and out 16-byte aligned,
  * strides multiples of 8; the nodes of a tree, and the distance of two pages, at

@@ -21,6 +21,10 @@ bool page_size_ok(int32_t page_size) {
 constexpr int64_t kMaxBytes = int64_t{1} << 29;   // of a tree's nodes, and of a page
 constexpr float kMaxScale = 0x1p127f;             // its product with log2(e) is finite
 
+// Keys of a sequence: the kernels' tiles of 32 keys, rounded up and a few further ones of idle key
+// groups, end below 2^31.
+constexpr int32_t kMaxKeys = INT32_MAX - 1023;
+
 // TV_OK if an attention call of these sizes is taken
 int attention_sizes(int32_t batch, int32_t num_nodes, int32_t heads, int32_t kv_heads,
                     int32_t head_dim, int32_t prefix_len) {
@@ -53,7 +57,8 @@ int validate(const tv::AttentionArgs& a, void* workspace, size_t workspace_bytes
   if (!(a.scale > 0.0f) || !isfinite(a.scale)) return TV_ERR_INVALID_ARG;
   if (!page_size_ok(a.page_size) || a.scale > kMaxScale) return TV_ERR_UNSUPPORTED;
   if (a.prefix_len % a.page_size) return TV_ERR_INVALID_ARG;
-  if (a.table_width > INT32_MAX / a.page_size) return TV_ERR_UNSUPPORTED;
+  // (so that the first keys of a context's tiles of 32, rounded up, end below 2^31)
+  if (a.table_width > kMaxKeys / a.page_size) return TV_ERR_UNSUPPORTED;
   const int64_t kv_row = static_cast<int64_t>(a.kv_heads) * a.head_dim;
   if (a.q_stride < static_cast<int64_t>(a.heads) * a.head_dim || a.kv_stride < kv_row)
     return TV_ERR_INVALID_ARG;
@@ -267,10 +272,6 @@ int validate(const tv::Fp4ReadArgs& a) {
     if (bits(p) % 4) return TV_ERR_INVALID_ARG;
   return outputs_overlap(a) ? TV_ERR_INVALID_ARG : TV_OK;
 }
-
-// Keys of a prompt attention: the kernel's tiles of 32 keys, rounded up and a few further ones
-// of idle key groups, end below 2^31.
-constexpr int32_t kMaxKeys = INT32_MAX - 1023;
 
 // TV_OK if a prompt attention of these sizes is taken
 int prompt_sizes(int32_t batch, int32_t num_queries, int32_t num_keys, int32_t heads,

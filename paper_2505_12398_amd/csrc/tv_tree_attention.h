@@ -88,7 +88,6 @@ struct Pass {
   int64_t q_stride, kv_stride;  // elements
   int64_t page_stride;          // bytes
   int num_pages, page_shift, table_width;
-  int most;                     // positions that a table holds and tiles can be counted of
   int batch, num_nodes, heads, kv_heads, head_dim;
   int group;                    // query heads of a key head
   int rows;                     // query rows of a tree and key head
@@ -146,8 +145,7 @@ struct Shape {
 };
 
 // Positions of tree b that this pass reads from pages, where they start, and whether
-// its table cannot hold its context, or 32 bits its tiles' first keys.
-constexpr int kMostPositions = 0x7fffffff - 1023;
+// its table cannot hold its context.
 struct Reach {
   int from, len, tiles;   // first position, positions, tiles with those of the nodes
   bool bad, shared;
@@ -162,7 +160,8 @@ __device__ __forceinline__ Reach reach(const Pass& P, int ctx) {
   if (ctx < 0) return r;
   r.shared = P.prefix_len > 0 && ctx >= P.prefix_len;
   r.from = r.shared ? P.prefix_len : 0;
-  r.bad = ctx > P.most || (ctx > r.from && P.num_pages == 0);
+  r.bad = ctx > static_cast<long long>(P.table_width) << P.page_shift ||
+          (ctx > r.from && P.num_pages == 0);
   r.len = r.bad ? 0 : ctx - r.from;
   r.tiles = (r.len + kKeys - 1) / kKeys + (P.num_nodes + kKeys - 1) / kKeys;
   return r;
@@ -1264,7 +1263,6 @@ int launch(const tv::AttentionArgs& a, void* workspace, hipStream_t stream) {
   P.num_pages = a.num_pages;
   P.page_shift = 31 - __builtin_clz(static_cast<unsigned>(a.page_size));
   P.table_width = a.table_width;
-  P.most = min(a.table_width * a.page_size, kMostPositions);
   P.batch = a.batch;
   P.num_nodes = a.num_nodes;
   P.heads = a.heads;
@@ -1274,7 +1272,7 @@ int launch(const tv::AttentionArgs& a, void* workspace, hipStream_t stream) {
   P.rows = a.num_nodes * P.group;
   // (without pages a tree that has a context has bad ones, the prefix among them, and so has
   // a tree with a prefix that its table cannot hold)
-  P.prefix_len = a.num_pages > 0 && a.prefix_len <= P.most ? a.prefix_len : 0;
+  P.prefix_len = a.num_pages > 0 && a.prefix_len <= a.table_width * a.page_size ? a.prefix_len : 0;
   P.k = static_cast<float>(static_cast<double>(a.scale) * 1.4426950408889634);
   const double slack = 8.0 / static_cast<double>(P.k);
   P.slack = slack < 3.0e38 ? static_cast<float>(slack) : 3.0e38f;

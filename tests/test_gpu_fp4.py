@@ -577,47 +577,6 @@ def test_pages_that_are_none_and_inactive_trees(n1):
     check(host, call, out=got)
 
 
-@pytest.mark.parametrize("n1,prefix", [(1, 0), (9, 0), (1, 16), (70, 16), (1, 2 ** 31 - 16)])
-@pytest.mark.parametrize("bits", [4, 16])
-def test_contexts_that_32_bits_cannot_count(bits, n1, prefix):
-    """A table may hold 2^31 - 16 positions, of which no tile's end is counted in 32 bits: such a tree is
-    NaN, and the others are what they are without it."""
-    ps, KH, H, dim, width = 16, 1, 2, 32, (2 ** 31 - 1) // 16
-    free, _ = torch.cuda.mem_get_info()
-    if free < 8 << 30:
-        pytest.skip("needs 8 GB")
-    g = torch.Generator(device=DEV).manual_seed(n1)
-    if bits == 4:
-        kc, vc = (torch.randint(0, 256, tv.fp4_cache_shape(3, KH, ps, dim), dtype=torch.uint8, generator=g,
-                                device=DEV) for _ in range(2))
-        for c in (kc, vc):
-            c[..., c.shape[-1] // 17 * 16:] = 126
-    else:
-        kc, vc = torch.randn((2, 3, KH, ps, dim), generator=g, device=DEV).to(torch.bfloat16)
-    table = torch.zeros((3, width), dtype=torch.int32, device=DEV)
-    table[:, :2] = i32([[0, 1], [2, 0], [1, 2]])
-    qkv = torch.randn((3, n1, H + 2 * KH, dim), generator=g, device=DEV).to(torch.bfloat16)
-    new = qkv[:, :, :H], qkv[:, :, H:H + KH], qkv[:, :, H + KH:], i32(trees("tree", 3, n1, np.random.default_rng(1)))
-
-    def go(ctx, table, prefix):
-        if bits == 4:
-            return tv.tree_attention_fp4(*new, kc, vc, ps, table, ctx, 0.2, prefix_len=prefix)
-        return tv.tree_attention(*new, kc, vc, table, ctx, 0.2, prefix_len=prefix)
-    few = table[:, :2].contiguous()
-    few_prefix = prefix if prefix <= 16 else 0
-    # parts are cut by all lengths, those of NaN trees their nodes'. Each side is off by its output's
-    # rounding and by that of its weights, half a step of sum p |v - out| <= 2 max |v| (1.1: of the second
-    # order); fp32's roundings of 100 keys are below 2^-14
-    most = max(3.0 if bits == 4 else float(vc.abs().max()), float(new[2].abs().max()))
-    atol = 2 * (1.1 * 2.0 ** -8 * 2 * most + 2.0 ** -14)
-    want = go(i32([31, -1, 20]), few, few_prefix)
-    for much in (2 ** 31 - 1023, 2 ** 31 - 32, 2 ** 31 - 16, 2 ** 31 - 1):
-        got = go(i32([31, much, 20]), table, prefix)
-        assert bool(got[1].isnan().all()), much
-        np.testing.assert_allclose(got[[0, 2]].double().cpu(), want[[0, 2]].double().cpu(), rtol=2.0 ** -7,
-                                   atol=atol)
-
-
 def test_no_pages_at_all():
     host, call = inputs(2, 5, 4, 2, 64, 16, [0, 0])
     call["block_table"] = call["block_table"][:, :0].contiguous()

@@ -199,6 +199,20 @@ def test_attention_refusals(kw, want):
     assert call_attention(**kw) == want
 
 
+@pytest.mark.parametrize("page_size", [16, 64, 512])
+def test_tables_whose_positions_32_bits_cannot_count(page_size):
+    """A context within 32 of 2^31 overflowed the count of its tiles, and was read before the table."""
+    most, stride = (2 ** 31 - 1024) // page_size, tv.tv_fp4_page_bytes(page_size, 64) * 2
+    for width in (most + 1, (2 ** 31 - 1) // page_size):
+        assert call_attention(page_size=page_size, page_stride=stride, table_width=width) == UNS
+        # (of 16 bits)
+        assert tv.tv_tree_attention(
+            2, 5, 8, 2, 64, tv.TV_DTYPE_BF16, A, A, 512, A, A, 128, A, A, 128 * page_size, 10, page_size, A,
+            width, A, A, 0, 0.125, A, WS, tv.tv_tree_attention_workspace_size(2, 5, 8, 2, 64, 0)) == UNS
+    # the widest table is taken (as far as its missing workspace)
+    assert call_attention(page_size=page_size, page_stride=stride, table_width=most, workspace=None) == WSP
+
+
 def test_page_bytes():
     for ps in (16, 64, 1024):
         for dim in (32, 64, 96, 128):
