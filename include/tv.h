@@ -542,7 +542,10 @@ int tv_cache_commit(int32_t layers, int32_t batch, int32_t num_nodes, int32_t kv
  * head h reading key head h / (heads / kv_heads),
  *   out[i][h] = sum_j exp(s(i, j)) value j / sum_j exp(s(i, j)),  s(i, j) = scale * <q[i][h], key j>
  * over the keys that query i sees; a query that sees none (nq > nk) gets zeros. Sums are formed in
- * fp32 from products on the matrix cores; weights are rounded as by tv_tree_attention.
+ * fp32 from products on the matrix cores; weights are rounded as by tv_tree_attention. An infinite value
+ * makes its element of the queries that see it infinite, or NaN where its weight rounds to 0; sums
+ * overflow where 2^8 sum_j |value j| does (bf16 values near 2^118 and beyond). A piece of up to some 128
+ * tokens behind a cache of 4 bits takes less time as chains of tv_tree_attention_fp4, a longer one here.
  *
  * Inputs (device): q [num_queries][heads][head_dim], k and v [num_keys][kv_heads][head_dim] of type
  * dtype (TV_DTYPE_BF16 or TV_DTYPE_F16), consecutive rows q_stride and kv_stride elements apart (so
@@ -557,7 +560,9 @@ int tv_cache_commit(int32_t layers, int32_t batch, int32_t num_nodes, int32_t kv
  * below 2^22; kv_stride at most 2^24; scale as for tv_tree_attention; q, k, v and out 16-byte aligned, strides multiples of 8.
  * out dtype [num_queries][heads][head_dim], apart from all inputs; rows of no sequence are left as
  * they were. workspace: tv_prompt_attention_workspace_size() bytes (0 for invalid sizes), 256-byte
- * aligned. Nothing is allocated. Returns a tv_status_t; argument errors launch nothing.
+ * aligned. Nothing is allocated by the call; the kernel has a stack for values that are not finite, for
+ * which the HIP runtime keeps 330 MB a hardware queue from its first launch there on (by a graph, its first
+ * replay). Returns a tv_status_t; argument errors launch nothing.
  */
 size_t tv_prompt_attention_workspace_size(int32_t batch, int32_t num_queries, int32_t num_keys,
                                           int32_t heads, int32_t kv_heads, int32_t head_dim);
@@ -621,7 +626,8 @@ int tv_cache_read_fp4(int32_t layers, int32_t batch, int32_t kv_heads, int32_t h
 /*
  * tv_tree_attention over a cache of 4 bits (page_stride in bytes, a multiple of 16): as that of the
  * cache's values in dtype. q, k_new and v_new are of type dtype; workspace:
- * tv_tree_attention_workspace_size() bytes.
+ * tv_tree_attention_workspace_size() bytes. (In heads of 96 and 128 some registers of 33 rows of a key head
+ * and more are kept in memory, for which the HIP runtime holds 40 MB a hardware queue.)
  */
 int tv_tree_attention_fp4(int32_t batch, int32_t num_nodes, int32_t heads, int32_t kv_heads,
                           int32_t head_dim, int32_t dtype, const int32_t* parents, const void* q,

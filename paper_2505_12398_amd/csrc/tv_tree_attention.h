@@ -40,10 +40,12 @@
 // 1.8, the first loads' issue 1.6, links and words 1, the key groups' merge and the part's
 // way out 10), and one that goes on in the next key head's item all but the cut again.
 //
-// Over a cache of 4 bits, which is 3.76 times smaller: 256 trees of 65 nodes 847 us, bound as
-// above (widened values are written to LDS, keys go into the products from registers). Single
-// tokens of 64 sequences, whose contexts are as long as those above are not: 173 us, 5.2 TB/s of
-// blocks and exponents in the kernel itself; one tree 36, bound as above.
+// Over a cache of 4 bits, which is 3.76 times smaller: 256 trees of 65 nodes 843 us, bound as
+// above (widened values are written to LDS, keys go into the products from registers) and by 7
+// registers that do not fit into a lane's 256 and are spilled (in heads of 128: 17 for 48 rows of a
+// workgroup, 7 for 96, 2 for 192; in heads of 64, and over 16 bits, none). Single tokens of 64
+// sequences, whose contexts are as long as those above are not: 174 us, 5.2 TB/s of blocks and
+// exponents in the kernel itself; one tree 36, bound as above, with 17 registers spilled.
 //
 // Heads of 72 to 120 are computed as heads of 128, padded with zeros in LDS (what they
 // read is not): where instructions bound it they cost what 128 cost.
@@ -681,8 +683,8 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
       // Keys through LDS too: single tokens of 64 sequences 190 us, 256 trees of 65 nodes 870, four
       // chains of 6 in heads of 64 with a prefix 89; so 173, 847 and 83. Rounds ahead 1 / 2 / 3 / 4:
       // the first 173 / 175 / 176 / 178, the last, whose tiles are half as large, 87 / 83 / 83 / 84;
-      // rows of 48 in heads of 128 have registers for one. (Four wavefronts of 16 rows on a SIMD,
-      // in 128 registers each, spill: 254 us.)
+      // rows of 48 in heads of 128 spill 17 registers with one, and 77 with two (one tree 37 and 47 us).
+      // (Four wavefronts of 16 rows on a SIMD, in 128 registers each, spill: 254 us.)
       constexpr int kDeep = SH::DP == 64 ? 2 : 1;
       constexpr int kAll = kKeys * SH::DP / 8 / 64;          // a lane's words of the tile
       constexpr int kWords = kAll >= 4 * RW ? 4 : 2;
@@ -862,7 +864,7 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
       // that shares with none issues before it waits, the others after the barrier). All
       // but the YOUNGER newest have landed when tile i's are there.
       constexpr int kSteady = SH::YOUNGER * SH::MINE;
-  #pragma unroll 1
+#pragma unroll 1
       for (int j = 0; j < SH::S; ++j) {
         fetch(tile0 + j * KW);
         place(tile0 + j * KW);
@@ -883,7 +885,7 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
             issue(stage, values);
           } else {
             const int to = lds0 + stage + h0 * SH::HALF + in0 * 1024 + (values ? SH::MAT : 0);
-  #pragma unroll
+#pragma unroll
             for (int hh = 0; hh < kHalves; ++hh) {
               const uint64_t a = at_k[hh] + (values ? v_base - k_base : 0);
               load_to_lds<kIn>(i32x4{static_cast<int>(a), static_cast<int>(a >> 32) & 0xffff, kRange,
@@ -901,7 +903,7 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
           load(before, true);
         }
         if constexpr (kHot) {
-  #pragma unroll
+#pragma unroll
           for (int hh = 0; hh < kHalves; ++hh)
             page[hh] = pages[first_key(t + SH::S * KW, h0 + hh) >> P.page_shift];
         } else {
@@ -909,7 +911,7 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
         }
         scores(stage, s);           // (of a tile that is none, behind this group's last: unused)
         if constexpr (kHot) {
-  #pragma unroll
+#pragma unroll
           for (int hh = 0; hh < kHalves; ++hh)
             at_k[hh] = key_at(page[hh], first_key(t + SH::S * KW, h0 + hh));
         } else {
@@ -929,11 +931,11 @@ __global__ void __launch_bounds__(SH::THREADS, 2) attention_kernel(Pass P) {
         stage = stage == ring + kLast ? ring : stage + SH::STAGE;
       };
       int i = 0, t = tile0;
-  #pragma unroll 1
+#pragma unroll 1
       for (const int lim = min(nfull, tile_end) - SH::S * KW; t < lim; ++i, t += KW)
         round(std::true_type{}, i, t);
       // (what the first of these loads is placed by the last round above, or before them)
-  #pragma unroll 1
+#pragma unroll 1
       for (; i < rounds; ++i, t += KW) round(std::false_type{}, i, t);
       wait_loads<0>();            // (zeros for tiles that are none)
     }
