@@ -25,6 +25,10 @@ constexpr float kMaxScale = 0x1p127f;             // its product with log2(e) is
 // groups, end below 2^31.
 constexpr int32_t kMaxKeys = INT32_MAX - 1023;
 
+// Query rows of a call: over a prefix they are one item's, whose last team of 32 workgroups of 192
+// rows ends below 2^31.
+constexpr int32_t kMaxRows = INT32_MAX - 16383;
+
 // TV_OK if an attention call of these sizes is taken
 int attention_sizes(int32_t batch, int32_t num_nodes, int32_t heads, int32_t kv_heads,
                     int32_t head_dim, int32_t prefix_len) {
@@ -33,7 +37,7 @@ int attention_sizes(int32_t batch, int32_t num_nodes, int32_t heads, int32_t kv_
   if (heads % kv_heads) return TV_ERR_INVALID_ARG;
   if (batch > TV_MAX_BATCH || num_nodes > TV_MAX_NODES || head_dim > TV_MAX_HEAD_DIM ||
       head_dim % 8 || static_cast<int64_t>(heads) * head_dim > TV_MAX_HIDDEN ||
-      static_cast<int64_t>(batch) * num_nodes * heads > INT32_MAX)
+      static_cast<int64_t>(batch) * num_nodes * heads > kMaxRows)
     return TV_ERR_UNSUPPORTED;
   return TV_OK;
 }

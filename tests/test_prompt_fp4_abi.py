@@ -199,6 +199,20 @@ def test_attention_refusals(kw, want):
     assert call_attention(**kw) == want
 
 
+def test_rows_that_32_bits_cannot_count():
+    """Over a prefix the rows of all trees are one item's: of nearly 2^31 of them, the indexes of the
+    last team's rows overflowed, and queries were read before their tensor."""
+    size = tv.tv_tree_attention_workspace_size
+    assert size(16384 * 64 - 8, 1024, 2, 1, 8, 16) > 0             # 2^31 - 2^14 rows
+    for batch, nodes, heads in ((2 ** 20 - 7, 1024, 2), (2 ** 20 - 1, 1024, 2), (46340, 46, 1007)):
+        assert batch * nodes * heads <= 2 ** 31 - 1
+        few = batch * nodes * heads <= 2 ** 31 - 2 ** 14
+        assert (size(batch, nodes, heads, 1, 8, 16) > 0) == few
+        if not few:
+            assert call_attention(batch=batch, num_nodes=nodes, heads=heads, kv_heads=1, head_dim=32, q_stride=64,
+                                  kv_stride=32, prefix_len=16) == UNS
+
+
 @pytest.mark.parametrize("page_size", [16, 64, 512])
 def test_tables_whose_positions_32_bits_cannot_count(page_size):
     """A context within 32 of 2^31 overflowed the count of its tiles, and was read before the table."""
