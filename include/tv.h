@@ -545,7 +545,8 @@ int tv_cache_commit(int32_t layers, int32_t batch, int32_t num_nodes, int32_t kv
  * fp32 from products on the matrix cores; weights are rounded as by tv_tree_attention. An infinite value
  * makes its element of the queries that see it infinite, or NaN where its weight rounds to 0; sums
  * overflow where 2^8 sum_j |value j| does (bf16 values near 2^118 and beyond). A piece of up to some 128
- * tokens behind a cache of 4 bits takes less time as chains of tv_tree_attention_fp4, a longer one here.
+ * tokens behind a cache of 4 bits takes less time as a chain of nodes of tv_tree_attention_fp4, a longer one
+ * here. (A cache of 16 bits has no such reading: pieces behind it are chains of tv_tree_attention.)
  *
  * Inputs (device): q [num_queries][heads][head_dim], k and v [num_keys][kv_heads][head_dim] of type
  * dtype (TV_DTYPE_BF16 or TV_DTYPE_F16), consecutive rows q_stride and kv_stride elements apart (so
@@ -557,8 +558,8 @@ int tv_cache_commit(int32_t layers, int32_t batch, int32_t num_nodes, int32_t kv
  *
  * head_dim: a multiple of 8 up to TV_MAX_HEAD_DIM; heads a multiple of kv_heads; heads * head_dim at
  * most TV_MAX_HIDDEN; num_queries * heads below 2^29, num_keys at most 2^31 - 1024 and batch * kv_heads
- * below 2^22; kv_stride at most 2^24; scale as for tv_tree_attention; q, k, v and out 16-byte aligned, strides multiples of 8.
- * out dtype [num_queries][heads][head_dim], apart from all inputs; rows of no sequence are left as
+ * below 2^22; kv_stride at most 2^24; scale as for tv_tree_attention; q, k, v and out 16-byte aligned,
+ * strides multiples of 8. out dtype [num_queries][heads][head_dim], apart from all inputs; rows of no sequence are left as
  * they were. workspace: tv_prompt_attention_workspace_size() bytes (0 for invalid sizes), 256-byte
  * aligned. Nothing is allocated by the call; the kernel has a stack for values that are not finite, for
  * which the HIP runtime keeps 330 MB a hardware queue from its first launch there on (by a graph, its first

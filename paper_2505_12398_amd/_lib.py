@@ -938,8 +938,8 @@ def cache_read_fp4(k_cache, v_cache, page_size, block_table, length, row_start, 
     a cache of 4 bits [layers, pages, kv_heads, bytes] into rows row_start[b] .. of two tensors
     [layers, ``rows``, kv_heads, D] (``tv_cache_read_fp4``; int32 tensors [B], block_table
     [B, width]): new ones of ``dtype`` (bfloat16 by default), or ``out`` = (k, v) (of ``dtype`` if
-    that is given), whose rows may lie apart. Returns them; rows that no request names are left as they were (new tensors hold
-    nothing there). Raises on a non-OK return."""
+    that is given), whose rows may lie apart. Returns them; rows that no request names are left as
+    they were (new tensors hold nothing there). Raises on a non-OK return."""
     import torch
     dev, i32 = k_cache.device, torch.int32
     if k_cache.dim() != 4 or block_table.dim() != 2:

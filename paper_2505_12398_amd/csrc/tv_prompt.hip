@@ -16,14 +16,14 @@
 // cycles a step of 32 keys, row sums among them, as products with ones (dot products in the vector unit
 // would hold up the matrix unit). Tiles come into LDS three steps ahead.
 //
-// What bounds it. One prompt of 16384 tokens, 32 heads over 8 of 128: 1855 us (1855 to 1980 on four
-// cards), 1185 TFLOP/s of the 1612 that a large product reaches: a step takes 1550 to 1650 cycles of
-// which the matrix unit is busy 1152 (the clock falls to 1.8 or 1.9 GHz meanwhile). An item costs 13
-// thousand cycles before its first step, nine of them the queries' loads, and 6 behind its last: 32
-// prompts of 20 to 3000 tokens 1056 us (to 1109), 795 TFLOP/s. Few items are bound by the longest: four
-// pieces behind long contexts have 350 items for 256 CUs, 214 us (to 241), and a piece of 16 tokens behind
-// 16000 has 8 that walk all keys, 178 us. One prompt of 100 tokens: 13 us, waits for queries, first keys
-// and the other key group's part.
+// What bounds it. One prompt of 16384 tokens, 32 heads over 8 of 128: 1855 us (in other runs, on other
+// cards, up to 1980), 1185 TFLOP/s of the 1612 that a large product reaches: a step takes 1550 to 1650
+// cycles of which the matrix unit is busy 1152 (the clock falls to 1.8 or 1.9 GHz meanwhile). An item
+// costs 13 thousand cycles before its first step, nine of them the queries' loads, and 6 behind its
+// last: 32 prompts of 20 to 3000 tokens 1056 us (to 1109), 795 TFLOP/s. Few items are bound by the
+// longest: four pieces behind long contexts have 350 items for 256 CUs, 214 us (to 241), and a piece of
+// 16 tokens behind 16000 has 8 that walk all keys, 178 us. One prompt of 100 tokens: 13 us, waits for
+// queries, first keys and the other key group's part.
 //
 // The call of careful_item gives the kernel a stack, 264 to 644 bytes a lane that no other path touches;
 // the runtime reserves them for all lanes of the device, 330 MB, at a hardware queue's first launch.

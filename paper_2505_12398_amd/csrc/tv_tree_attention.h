@@ -41,11 +41,11 @@
 // way out 10), and one that goes on in the next key head's item all but the cut again.
 //
 // Over a cache of 4 bits, which is 3.76 times smaller: 256 trees of 65 nodes 843 us, bound as
-// above (widened values are written to LDS, keys go into the products from registers) and by 7
-// registers that do not fit into a lane's 256 and are spilled (in heads of 128: 17 for 48 rows of a
-// workgroup, 7 for 96, 2 for 192; in heads of 64, and over 16 bits, none). Single tokens of 64
-// sequences, whose contexts are as long as those above are not: 174 us, 5.2 TB/s of blocks and
-// exponents in the kernel itself; one tree 36, bound as above, with 17 registers spilled.
+// above (widened values are written to LDS, keys go into the products from registers). Single
+// tokens of 64 sequences, whose contexts are as long as those above are not: 174 us, 5.2 TB/s of
+// blocks and exponents in the kernel itself; one tree 36, bound as above. In heads of 128 some
+// registers do not fit into a lane's 256 and are spilled: 17 for 48 rows of a workgroup (one tree), 7
+// for 96 (256 trees), 2 for 192; in heads of 64, and over 16 bits, none.
 //
 // Heads of 72 to 120 are computed as heads of 128, padded with zeros in LDS (what they
 // read is not): where instructions bound it they cost what 128 cost.
