@@ -392,7 +392,9 @@ int tv_commit_paths(int32_t batch, int32_t num_nodes, const int32_t* parents,
  *
  * A tree whose block table names a page outside [0, num_pages) for a position
  * below ctx_len, or whose ctx_len exceeds table_width * page_size, gets NaN in
- * every output. The order of a tree's sums, and so its last bits, depends on the
+ * every output. An infinite value of a node makes its element of the nodes that
+ * see it infinite; one in the cache makes it infinite or, where its weight rounds
+ * to 0, NaN. The order of a tree's sums, and so its last bits, depends on the
  * lengths of all trees of the call, and on nothing else of the others; the same
  * call gives the same bits.
  *
@@ -543,8 +545,8 @@ int tv_cache_commit(int32_t layers, int32_t batch, int32_t num_nodes, int32_t kv
  *   out[i][h] = sum_j exp(s(i, j)) value j / sum_j exp(s(i, j)),  s(i, j) = scale * <q[i][h], key j>
  * over the keys that query i sees; a query that sees none (nq > nk) gets zeros. Sums are formed in
  * fp32 from products on the matrix cores; weights are rounded as by tv_tree_attention. An infinite value
- * makes its element of the queries that see it infinite, or NaN where its weight rounds to 0; sums
- * overflow where 2^8 sum_j |value j| does (bf16 values near 2^118 and beyond). A piece of up to some 128
+ * makes its element of the queries that see it infinite; sums overflow where 2^8 sum_j |value j| does
+ * (bf16 values near 2^118 and beyond). A piece of up to some 128
  * tokens behind a cache of 4 bits takes less time as a chain of nodes of tv_tree_attention_fp4, a longer one
  * here. (A cache of 16 bits has no such reading: pieces behind it are chains of tv_tree_attention.)
  *

@@ -25,7 +25,7 @@
 // 16 tokens behind 16000 has 8 that walk all keys, 178 us. One prompt of 100 tokens: 13 us, waits for
 // queries, first keys and the other key group's part.
 //
-// The call of careful_item gives the kernel a stack, 264 to 644 bytes a lane that no other path touches;
+// The call of careful_item gives the kernel a stack, 264 to 652 bytes a lane that no other path touches;
 // the runtime reserves them for all lanes of the device, 330 MB, at a hardware queue's first launch.
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -121,7 +121,7 @@ struct Shape {
   static constexpr int ACC = (KW - 1) * RW * MT * DB * 4096;
   static constexpr int MERGE = ACC + (KW - 1) * RW * MT * 64 * 8;
   static constexpr int MAIN = RING > MERGE ? RING : MERGE;
-  static constexpr int FLAGS = MAIN, BYTES = FLAGS + 4 * kWaves;
+  static constexpr int FLAGS = MAIN, MARKS = FLAGS + 4 * kWaves, BYTES = MARKS + kWaves * DP * 4;
   static constexpr int PER_CU = 1;        // workgroups
   static_assert(BYTES <= 160 * 1024, "LDS of a CU");
   static_assert(WAIT < 64, "the count of loads in flight");
@@ -151,23 +151,26 @@ __device__ __forceinline__ int swizzle(int r) {
   return DP == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
 }
 
-// The end of an item: the key groups' parts merged by group 0, and its rows written; odd: with what is
-// not finite of the values v (those of the item's first key and key head) from key `from` on.
-template <class T, class SH>
+// The end of an item: the key groups' parts merged by group 0, and its rows written. CAREFUL: the sums are
+// without what is not finite of the values v (those of the item's first key and key head), which is added
+// here, whatever its weight rounds to. odd: 1 if some key from `from` on, which not all rows of the
+// wavefront see, has such values, 2 if one before it, whose sums are the marks in LDS.
+template <class T, class SH, bool CAREFUL>
 __device__ __forceinline__ void finish(lds_byte* lds, f32x16 (&acc)[SH::DB + 1][SH::MT], float (&m)[SH::MT],
-                                       const int (&limit)[SH::MT], bool odd, const uint16_t* v, int64_t kv_stride,
+                                       const int (&limit)[SH::MT], int odd, const uint16_t* v, int64_t kv_stride,
                                        uint16_t* out, int heads, int head_dim, int group, float k2, int kh, int q0,
                                        int rows, int rbase, int from) {
   constexpr int MT = SH::MT, RW = SH::RW, KW = SH::KW, DB = SH::DB;
   const int lane = threadIdx.x & 63, wave = uniform(static_cast<int>(threadIdx.x >> 6));
   const int rg = wave % RW, kg = wave / RW, n = lane & 31, h = lane >> 5;
   LDS(int)* const flags = (LDS(int)*)(lds + SH::FLAGS);
+  LDS(float)* const marks = (LDS(float)*)(lds + SH::MARKS);
   float l[MT];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) l[mt] = acc[DB][mt][0];
   if constexpr (KW > 1) {
     barrier();                            // (all have read the flags)
-    if (lane == 0) flags[wave] = odd;
+    if (CAREFUL && lane == 0) flags[wave] = odd;
     if (kg > 0) {
       const int w = (kg - 1) * RW + rg;
 #pragma unroll
@@ -184,7 +187,7 @@ __device__ __forceinline__ void finish(lds_byte* lds, f32x16 (&acc)[SH::DB + 1][
     barrier();
     if (kg > 0) return;
 #pragma unroll
-    for (int j = 1; j < KW; ++j) odd |= flags[j * RW + rg] != 0;
+    for (int j = 1; CAREFUL && j < KW; ++j) odd |= flags[j * RW + rg];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       f32x2 o[KW];
@@ -230,7 +233,16 @@ __device__ __forceinline__ void finish(lds_byte* lds, f32x16 (&acc)[SH::DB + 1][
         float o[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] = acc[db][mt][4 * i + e] * inv;
-        if (odd) {
+        if (CAREFUL && odd & 2) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float x = 0.0f;
+#pragma unroll
+            for (int j = 0; j < KW; ++j) x += marks[(j * RW + rg) * SH::DP + d + e];
+            if (x != 0.0f) o[e] += x;     // (-0 stays)
+          }
+        }
+        if (CAREFUL && odd & 1) {
 #pragma unroll 1
           for (int j = from; j <= limit[mt]; ++j) {
             const u32x2 w = *reinterpret_cast<const u32x2*>(v + static_cast<int64_t>(j) * kv_stride + d);
@@ -246,11 +258,11 @@ __device__ __forceinline__ void finish(lds_byte* lds, f32x16 (&acc)[SH::DB + 1][
   }
 }
 
-// An item whose keys or values hold what is not finite, a tile of each key group at a time: values in
-// tiles that some rows do not see whole are taken as 0 where they are not finite, and added to the rows
-// that see them when these are written. The same sums in the same order as in the kernel, so that the
-// rows that see none of it keep their bits. Not inlined: the registers of the kernel are laid out for
-// the other path.
+// An item whose keys or values hold what is not finite, a tile of each key group at a time: values are
+// taken as 0 where they are not finite, and added to the rows that see them when these are written. (A
+// weight that rounds to 0 would make NaN of an infinite one.) The same sums in the same order as in the
+// kernel, so that the rows and the elements that see none of it keep their bits. Not inlined: the
+// registers of the kernel are laid out for the other path.
 template <class T, class SH>
 __device__ __attribute__((noinline))
 void careful_item(lds_byte* lds, const uint16_t* pq, const uint16_t* pk, const uint16_t* pv, uint16_t* out,
@@ -291,7 +303,11 @@ void careful_item(lds_byte* lds, const uint16_t* pq, const uint16_t* pk, const u
 #pragma unroll
     for (int db = 0; db <= DB; ++db) acc[db][mt] = f32x16{};
   }
-  bool odd = false;
+  int odd = 0;
+  // sums of what the wavefront's tiles that all its rows see hold, an element of the head each
+  LDS(float)* const marks = (LDS(float)*)(lds + SH::MARKS) + wave * SH::DP;
+#pragma unroll
+  for (int i = 0; i < SH::DP / 64; ++i) marks[64 * i + lane] = 0.0f;
 #pragma unroll 1
   for (int t0 = 0; t0 < tiles; t0 += KW) {
     const int t = t0 + kg;
@@ -326,7 +342,7 @@ void careful_item(lds_byte* lds, const uint16_t* pq, const uint16_t* pk, const u
       u = fmaxf(u, __shfl_xor(u, 32, 64));
       u = u > above ? u : m[mt];
       const float f = to_frame<T>(m[mt], u, k2);
-      if (u > m[mt]) {                    // (a frame that stays multiplies nothing: infinity stays)
+      if (u > m[mt]) {
 #pragma unroll
         for (int db = 0; db <= DB; ++db) acc[db][mt] *= f;
       }
@@ -345,15 +361,20 @@ void careful_item(lds_byte* lds, const uint16_t* pq, const uint16_t* pk, const u
       const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
           (LDS(s16x4)*)(lds + at + 8 * SH::ROW + ((ch + vchunk) ^ swizzle<SH::DP>(vrow + 8)) * 16));
       u32x4 w = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-      if (t >= nfull) {
-        bool some = false;
+      bool some = false;
+      float mark = 0.0f;                  // (this lane's eight values are of one element)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const bool a = (w[e] & T::kExponent) == T::kExponent, b = (w[e] >> 16 & T::kExponent) == T::kExponent;
-          some |= a | b;
-          w[e] = (a ? 0 : w[e] & 0xffffu) | (b ? 0 : w[e] & 0xffff0000u);
-        }
-        odd |= __builtin_amdgcn_ballot_w64(some) != 0;
+      for (int e = 0; e < 4; ++e) {
+        const bool a = (w[e] & T::kExponent) == T::kExponent, b = (w[e] >> 16 & T::kExponent) == T::kExponent;
+        some |= a | b;
+        mark += a ? T::value(static_cast<uint16_t>(w[e])) : 0.0f;
+        mark += b ? T::value(static_cast<uint16_t>(w[e] >> 16)) : 0.0f;
+        w[e] = (a ? 0 : w[e] & 0xffffu) | (b ? 0 : w[e] & 0xffff0000u);
+      }
+      if (__builtin_amdgcn_ballot_w64(some)) {
+        odd |= t < nfull ? 2 : 1;
+        mark += __shfl_xor(mark, 32, 64);
+        if (t < nfull && h == 0) marks[32 * (i >> 1) + n] += mark;
       }
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
@@ -366,7 +387,7 @@ void careful_item(lds_byte* lds, const uint16_t* pq, const uint16_t* pk, const u
         acc[DB][mt] = mfma32<T>(ones, __builtin_bit_cast(s16x8, p[mt][i]), acc[DB][mt]);
   }
   __syncthreads();
-  finish<T, SH>(lds, acc, m, limit, odd, pv + first, kv_stride, out, heads, head_dim, group, k2, kh, q0, rows,
+  finish<T, SH, true>(lds, acc, m, limit, odd, pv + first, kv_stride, out, heads, head_dim, group, k2, kh, q0, rows,
                 rbase, nfull * kKeys);
 }
 
@@ -733,7 +754,7 @@ __global__ void __launch_bounds__(kThreads, SH::PER_CU) prompt_kernel(Pass P) {
     return;
   }
 
-  finish<T, SH>(lds, acc, m, limit, false, nullptr, 0, P.out, P.heads, P.head_dim, P.group, P.k2, kh, I.q0, rows,
+  finish<T, SH, false>(lds, acc, m, limit, 0, nullptr, 0, P.out, P.heads, P.head_dim, P.group, P.k2, kh, I.q0, rows,
                 rbase, 0);
 }
 

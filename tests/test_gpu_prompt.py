@@ -239,6 +239,37 @@ def test_infinite_values(nk):
         assert torch.equal(got[..., rest], clean[..., rest])
 
 
+@pytest.mark.parametrize("dtype,dim,heads,n,earlier", [
+    ("bf16", 64, 4, 40, 160), ("f16", 64, 4, 200, 0), ("f16", 64, 32, 30, 3001), ("f16", 64, 32, 512, 1490),
+    ("f16", 64, 32, 2500, 0), ("bf16", 128, 8, 100, 400), ("f16", 128, 8, 300, 700), ("f16", 80, 32, 1100, 0)])
+def test_infinite_values_of_hardly_any_weight(dtype, dim, heads, n, earlier):
+    """A value's weight is above 0 however low its score: infinity and NaN reach their own element of the
+    queries that see them, and no other bit, where the weight rounds to 0 as well, and where later keys
+    score much higher."""
+    call = inputs([n, 9], [n + earlier, 9], heads, 2, dim, dtype, seed=n)
+    q, k = call["q"].clone(), call["k"].clone()
+    q[..., 0] = 1.0 / call["scale"]
+    low = [0, 5, earlier // 2, earlier + n // 3, earlier + n - 1]
+    nk = n + earlier
+    k[:nk, :, 0] = torch.linspace(0.0, 70.0, nk, device=DEV)[:, None].to(k.dtype)   # 70 apart and
+    k[low, :, 0] = -200.0                                                           # 200
+    call = dict(call, q=q, k=k)
+    clean = tv.prompt_attention(**dict(call, v=call["v"].clone()))
+    assert bool(clean.isfinite().all())
+    bad = ((0, 3, "inf"), (5, 4, "-inf"), (earlier // 2, 3, "inf"), (earlier + n // 3, 6, "nan"),
+           (earlier + n - 1, 7, "inf"), (nk // 3, 0, "-inf"), (1, dim - 1, "nan"))
+    for some in [(x,) for x in bad] + [bad]:
+        v = call["v"].clone()
+        want = clean.clone()
+        for at, d, x in some:
+            v[at, :, d] = float(x)
+            sees = torch.arange(n, device=DEV) + earlier >= at
+            want[:n, :, d][sees] += float(x)
+        got = tv.prompt_attention(**dict(call, v=v))
+        assert torch.equal(got.isnan(), want.isnan()), some
+        assert torch.equal(got.nan_to_num(9.0), want.nan_to_num(9.0)), some
+
+
 @pytest.mark.parametrize("n,earlier", [(30, 3001), (500, 0), (512, 1490), (700, 333), (2500, 0)])
 def test_heights_of_heads_of_64(n, earlier):
     """Workgroups of 64, 128 and 256 rows: an infinite value and keys that are not numbers reach the
